@@ -42,6 +42,16 @@ from .binding import (  # noqa: F401
 )
 
 
+# the operators around the head (layer norm, policy and preference losses, Muon); their binding needs torch
+_TRAINING_OPS = frozenset((
+    "layer_norm", "policy_loss", "preference_loss",
+    "vp_ln_forward", "vp_ln_backward", "vp_ln_workspace_bytes",
+    "vp_policy_loss", "vp_policy_loss_backward", "vp_policy_loss_workspace_bytes",
+    "vp_preference_loss", "vp_preference_loss_backward", "vp_preference_loss_workspace_bytes",
+    "muon_step", "muon_orthogonalize", "muon_workspace_bytes", "muon_device_status", "muon_rms_scale",
+))
+
+
 def __getattr__(name):
     # the autograd front end needs torch; import it lazily so the C-ABI binding works without it
     if name in ("vocab_proj_cross_entropy", "vocab_proj_cross_entropy_mean"):
@@ -50,6 +60,10 @@ def __getattr__(name):
     if name == "HostStepPipeline":
         from . import host_pipeline as _hp
         return _hp.HostStepPipeline
+    if name in _TRAINING_OPS:
+        from . import training_ops as _ops
+        value = globals()[name] = getattr(_ops, name)
+        return value
     if name in ("RingDTP", "DistTransport", "CudaMeetings", "choose_schedule", "shard_interval"):
         from . import ring as _ring
         return getattr(_ring, name)
