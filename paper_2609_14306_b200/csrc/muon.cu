@@ -33,7 +33,7 @@ int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
 
 struct Layout {
     int64_t R, C, lda, ldx, parts;
-    size_t sumsq, X0, X1, A, B, total;
+    size_t done, sumsq, X0, X1, A, B, total;
 };
 
 bool layout(int64_t batch, int64_t rows, int64_t cols, Layout* L) {
@@ -42,10 +42,11 @@ bool layout(int64_t batch, int64_t rows, int64_t cols, Layout* L) {
     if (batch > 65535 || L->C > (1 << 22) || L->R > (1 << 17)) return false;
     L->lda = up64(L->R); L->ldx = up64(L->C);
     const int64_t row_tiles = (L->R + 127) / 128, col_tiles = (L->C + 127) / 128;
-    if (batch * row_tiles * col_tiles > (int64_t{1} << 30)) return false;
-    L->parts = std::max<int64_t>(1, std::min<int64_t>(MAX_PARTS, rows * cols / (16 * PREP_THREADS)));
+    if (batch * row_tiles * col_tiles > (int64_t{1} << 20)) return false;   // work-list positions and counts fit 31 bits
+    L->parts = std::max<int64_t>(1, std::min<int64_t>(MAX_PARTS, (rows * cols + 16 * PREP_THREADS - 1) / (16 * PREP_THREADS)));
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-    size_t off = 256;                                                      // the status word
+    size_t off = 256;                                                      // the status word, the work list's counter
+    L->done = off;  off = up(off + sizeof(int) * batch);
     L->sumsq = off; off = up(off + sizeof(double) * batch * L->parts);
     L->X0 = off;    off = up(off + 2 * static_cast<size_t>(batch) * L->R * L->ldx);
     L->X1 = off;    off = up(off + 2 * static_cast<size_t>(batch) * L->R * L->ldx);
@@ -125,18 +126,11 @@ bool encode(CUtensorMap* map, void* ptr, int rank, const cuuint64_t* dims, const
     return enc && enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, ptr, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// [batch][rows][ld] read along its rows: boxes of 64 rows x 64 elements.
-bool map_k(CUtensorMap* map, __half* ptr, int64_t batch, int64_t rows, int64_t ld) {
-    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(ld), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(batch)};
-    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(2 * ld), static_cast<cuuint64_t>(2 * ld * rows)};
-    const cuuint32_t box[3] = {64, 64, 1};
-    return encode(map, ptr, 3, dims, strides, box);
-}
-// The same array as right operand with its rows as K: boxes of 64 rows (K) x 64 columns, column chunks as a dimension of their own.
-bool map_mn(CUtensorMap* map, __half* ptr, int64_t batch, int64_t rows, int64_t ld) {
+// [batch][rows][ld] fp16, ld a multiple of 64; see Maps.
+bool map_operand(CUtensorMap* map, __half* ptr, int64_t batch, int64_t rows, int64_t ld, cuuint32_t box_rows, cuuint32_t box_chunks) {
     const cuuint64_t dims[4] = {64, static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(ld / 64), static_cast<cuuint64_t>(batch)};
     const cuuint64_t strides[3] = {static_cast<cuuint64_t>(2 * ld), 128, static_cast<cuuint64_t>(2 * ld * rows)};
-    const cuuint32_t box[4] = {64, 64, 1, 1};
+    const cuuint32_t box[4] = {64, box_rows, box_chunks, 1};
     return encode(map, ptr, 4, dims, strides, box);
 }
 
@@ -157,28 +151,33 @@ cudaError_t ensure_smem() {
     int dev = 0;
     if (cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64 && done[dev].load(std::memory_order_acquire)) return cudaSuccess;
-    const cudaError_t e = cudaFuncSetAttribute(muon_gemm_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GEMM_SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(muon_products_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GEMM_SMEM);
     if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_release);
     return e;
 }
 
 // Tiles of one matrix in a product.
-int tiles_of(int mode, int64_t R, int64_t C, int bn) {
+int tiles_of(int mode, int64_t R, int64_t C) {
     const int64_t mt = (R + TM - 1) / TM;
-    if (mode == APPLY) return static_cast<int>(mt * ((C + bn - 1) / bn));
-    const int64_t nj = (R + bn - 1) / bn, f = TM / bn;
-    int64_t n = 0;
-    for (int64_t i = 0; i < mt; ++i) n += nj - i * f;
-    return static_cast<int>(n);
+    return static_cast<int>(mode == APPLY ? mt * ((C + TN - 1) / TN) : mt * (mt + 1) / 2);
 }
 
-// Whichever tile width needs less time: rounds of the work list over the CTA pairs, a 128-wide tile at 0.55 of a 256-wide one.
-int pick_bn(int mode, int64_t batch, int64_t R, int64_t C, int pairs) {
-    auto cost = [&](int bn, double per) {
-        const int64_t t = batch * tiles_of(mode, R, C, bn);
-        return static_cast<double>((t + pairs - 1) / pairs) * per;
-    };
-    return cost(128, 0.55) < cost(256, 1.0) ? 128 : 256;
+bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+template <typename G, int V> void launch_prep_v(const PrepParams& p, cudaStream_t st) {
+    const unsigned nb = static_cast<unsigned>(p.batch);
+    muon_momentum_kernel<G, V><<<dim3(p.parts, nb), PREP_THREADS, 0, st>>>(p);
+    if (p.rows > p.cols) {
+        muon_start_tall_kernel<G, V><<<dim3(p.ldx / 64, (p.R + 63) / 64, nb), PREP_THREADS, 0, st>>>(p);
+    } else {
+        const int64_t blocks = (static_cast<int64_t>(p.R) * (p.ldx / 8) + PREP_THREADS - 1) / PREP_THREADS;
+        const int64_t most = std::max<int64_t>(1, 8 * sm_count() / p.batch);    // eight blocks fit an SM
+        muon_start_kernel<G, V><<<dim3(static_cast<unsigned>(std::min(blocks, most)), nb), PREP_THREADS, 0, st>>>(p);
+    }
+}
+template <typename G> void launch_prep(const PrepParams& p, bool four, cudaStream_t st) {
+    if (four) launch_prep_v<G, 4>(p, st);
+    else launch_prep_v<G, 1>(p, st);
 }
 
 struct Target {                                 // what the last product writes
@@ -204,34 +203,36 @@ int run(const void* g, int g_dtype, float* m, float mu, int nesterov, int64_t ba
     q.A = reinterpret_cast<__half*>(base + L.A); q.B = reinterpret_cast<__half*>(base + L.B);
     q.transposed = rows > cols;
     q.out = tgt.out; q.out_dtype = tgt.out_dtype; q.p = tgt.p; q.w = tgt.w; q.decay = tgt.decay; q.step = tgt.step;
-    q.status = reinterpret_cast<int*>(base);
+    q.status = reinterpret_cast<int*>(base); q.next = q.status + 16; q.done = reinterpret_cast<int*>(base + L.done);
     q.wait_limit_ns = static_cast<unsigned long long>(vp_ce_set_wait_limit_ns(0));
     Maps maps;
-    bool ok = map_k(&maps.a_k, q.A, batch, L.R, L.lda) && map_k(&maps.b_k, q.B, batch, L.R, L.lda);
-    for (int i = 0; i < 2; ++i) ok = ok && map_k(&maps.x_k[i], q.X[i], batch, L.R, L.ldx) && map_mn(&maps.x_mn[i], q.X[i], batch, L.R, L.ldx);
+    bool ok = map_operand(&maps.a, q.A, batch, L.R, L.lda, 128, 1) && map_operand(&maps.b, q.B, batch, L.R, L.lda, 128, 1);
+    for (int i = 0; i < 2; ++i)
+        ok = ok && map_operand(&maps.x_k[i], q.X[i], batch, L.R, L.ldx, 128, 1) && map_operand(&maps.x_mn[i], q.X[i], batch, L.R, L.ldx, 64, 2);
     if (!ok || ensure_smem() != cudaSuccess) return VPCE_CUDA_ERROR;
 
     PrepParams pp{};
-    pp.g = g; pp.g_dtype = g_dtype; pp.m = m; pp.mu = mu; pp.nesterov = nesterov;
+    pp.g = g; pp.m = m; pp.mu = mu; pp.nesterov = nesterov;
     pp.batch = q.batch; pp.rows = rows; pp.cols = cols; pp.parts = static_cast<int>(L.parts);
     pp.sumsq = reinterpret_cast<double*>(base + L.sumsq);
     pp.eps = static_cast<float>(eps); pp.scale = static_cast<float>(plan.scale0);
-    pp.X = q.X[0]; pp.R = q.R; pp.C = q.C; pp.ldx = q.ldx; pp.status = q.status;
-    const unsigned nb = static_cast<unsigned>(batch);
-    muon_momentum_kernel<<<dim3(pp.parts, nb), PREP_THREADS, 0, st>>>(pp);
-    muon_start_kernel<<<dim3(q.ldx / 64, (q.R + 63) / 64, nb), PREP_THREADS, 0, st>>>(pp);
+    pp.X = q.X[0]; pp.R = q.R; pp.C = q.C; pp.ldx = q.ldx; pp.status = q.status; pp.next = q.next; pp.done = q.done;
+    // four elements per access where every matrix (and every row, for the start) begins on a boundary of four elements
+    const bool four = cols % 4 == 0 && aligned(g, g_dtype == VPCE_F32 ? 16 : 8) && aligned(m, 16);
+    if (g_dtype == VPCE_F32) launch_prep<float>(pp, four, st);
+    else if (g_dtype == VPCE_F16) launch_prep<__half>(pp, four, st);
+    else launch_prep<__nv_bfloat16>(pp, four, st);
 
     const int pairs = sm_count() / 2;
-    for (int k = 0; k < 3 * steps; ++k) {
-        const int mode = k % 3;
-        q.phase = k;
-        q.bn = pick_bn(mode, batch, L.R, L.C, pairs);
-        q.tiles = tiles_of(mode, L.R, L.C, q.bn);
-        q.alpha = plan.alpha[k]; q.beta = plan.beta[k];
-        q.last = k + 1 == 3 * steps;
-        const int grid = 2 * std::min<int64_t>(pairs, batch * q.tiles);
-        muon_gemm_kernel<<<grid, GEMM_THREADS, GEMM_SMEM, st>>>(maps, q);
+    int most = 0;
+    for (int mode = 0; mode < 3; ++mode) {
+        q.tiles[mode] = tiles_of(mode, L.R, L.C);
+        most = std::max<int64_t>(most, std::min<int64_t>(pairs, batch * q.tiles[mode]));
     }
+    q.steps = steps;
+    std::copy(plan.alpha, plan.alpha + 3 * steps, q.alpha);
+    std::copy(plan.beta, plan.beta + 3 * steps, q.beta);
+    muon_products_kernel<<<2 * most, GEMM_THREADS, GEMM_SMEM, st>>>(maps, q);
     return cudaGetLastError() == cudaSuccess ? VPCE_OK : VPCE_CUDA_ERROR;
 }
 

@@ -12,16 +12,15 @@ namespace vpmuon {
 
 using namespace vpce;
 
-constexpr int TM = 256;                     // rows of a tile: one CTA pair, 128 rows per CTA
-constexpr int TN = 256;                     // most columns of a tile; a launch runs 256 or 128
+constexpr int TM = 256, TN = 256;           // a tile: one CTA pair, 128 rows and 128 columns' worth of operands per CTA
 constexpr int KB = 64;                      // K per pipeline stage: one 128-byte swizzle row of fp16
-constexpr int BOX_BYTES = 64 * 128;         // one TMA box: 64 rows of 128 bytes
-constexpr int A_BYTES = 2 * BOX_BYTES;      // per CTA: its 128 rows of the left operand
-constexpr int STAGE_BYTES = 2 * A_BYTES;    // and its half (128 at most) of the right operand's columns
+constexpr int A_BYTES = 128 * 128;          // 128 rows of the left operand
+constexpr int STAGE_BYTES = 2 * A_BYTES;
 constexpr int STAGES = 6;
-constexpr int GEMM_THREADS = 192;           // warp 0 TMA, warp 1 MMA, warps 2..5 epilogue
-constexpr int EPI_PITCH = 33;               // floats: a 32 x 32 block per epilogue warp, read back by columns
-constexpr int EPI_BYTES = 4 * 32 * EPI_PITCH * 4;
+constexpr int EPI_WARPS = 8;                // two per quarter of the tensor memory's lanes, each every other 32 columns
+constexpr int GEMM_THREADS = 64 + 32 * EPI_WARPS;   // warp 0 TMA, warp 1 MMA, the others epilogue
+constexpr int EPI_WARP_BYTES = 2560;        // of shared memory per epilogue warp, for transposing a 32 x 32 block
+constexpr int EPI_BYTES = EPI_WARPS * EPI_WARP_BYTES;
 constexpr int GEMM_SMEM = STAGES * STAGE_BYTES + EPI_BYTES + 2048;
 constexpr int MAX_STEPS = 32;
 constexpr int PREP_THREADS = 256;
@@ -30,25 +29,25 @@ constexpr int MAX_PARTS = 512;              // partial sums of squares per matri
 // The three products of a step.
 enum Mode { GRAM = 0, POLY = 1, APPLY = 2 };
 
-struct Maps {
-    CUtensorMap x_k[2];                     // X (both buffers) read along its rows: K = columns
-    CUtensorMap x_mn[2];                    // X as right operand of B X: K = rows
-    CUtensorMap a_k, b_k;
-};
+// Operands as 4-D arrays {64 elements, rows, 64-element chunks of a row, batch}.  Along the rows (K = columns) a stage takes one
+// box of 128 rows x 1 chunk, down the columns (X as right operand of B X, K = rows) one of 64 rows x 2 chunks.  The chunk as a
+// dimension of its own matters: boxes at column offsets of a 3-D array {columns, rows, batch} arrived at 48 bytes a cycle and
+// SM, these at 70 (loads alone, 128-row boxes; the products need 64).
+struct Maps { CUtensorMap x_k[2], x_mn[2], a, b; };
 
 struct GemmParams {
     int batch, R, C;                        // matrices R x C with R <= C
     int lda, ldx;                           // row pitches (elements, multiples of 64; columns beyond R / C hold zeros)
-    int phase;                              // 3 step + mode
-    int bn;                                 // 256 or 128
-    int tiles;                              // per matrix
-    float alpha, beta;                      // stored result = alpha acc + beta addend (stored units)
+    int steps;
+    int tiles[3];                           // per mode: tiles of one matrix
+    float alpha[3 * MAX_STEPS], beta[3 * MAX_STEPS];   // stored result = alpha acc + beta addend (stored units)
     __half *X[2], *A, *B;
     // last product: what becomes of X
-    int last, transposed;                   // transposed: the user's matrices are C x R
+    int transposed;                         // the user's matrices are C x R
     void* out; int out_dtype;               // muon_orthogonalize
     float* p; __nv_bfloat16* w; float decay, step; // muon_step: p <- p decay - step X
-    int* status;
+    int *status, *next;                     // next: work-list position to be taken, zero before the launch
+    int* done;                              // [batch] epilogue warps that have finished a tile of this matrix, zero before the launch
     unsigned long long wait_limit_ns;
 };
 
@@ -57,130 +56,15 @@ __device__ __forceinline__ void tma2_load_4d(uint32_t dst, const CUtensorMap* ma
         "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
-__device__ __forceinline__ void tma2_load_3d_plain(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
-}
-
 // ------------------------------------------------------------------------------------ element types
-__device__ __forceinline__ float load_as_float(const void* p, int dtype, size_t i) {
-    if (dtype == VPCE_F32) return static_cast<const float*>(p)[i];
-    if (dtype == VPCE_F16) return __half2float(static_cast<const __half*>(p)[i]);
-    return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-}
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ void store_as(void* p, int dtype, size_t i, float v) {
     if (dtype == VPCE_F32) static_cast<float*>(p)[i] = v;
     else if (dtype == VPCE_F16) static_cast<__half*>(p)[i] = __float2half_rn(v);
     else static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
 }
-
-// ------------------------------------------------------------------------------------ momentum, norm, start
-struct PrepParams {
-    const void* g; int g_dtype;
-    float* m;                               // null: no momentum (U = G)
-    float mu; int nesterov;
-    int batch; long rows, cols;
-    int parts; double* sumsq;               // [batch][parts]
-    float eps, scale;                       // X_0 is stored times `scale`
-    __half* X; int R, C, ldx;
-    int* status;
-};
-
-// M <- mu M + G and the sum of squares of U over one part of one matrix: grid (parts, batch).
-__global__ void __launch_bounds__(PREP_THREADS) muon_momentum_kernel(const PrepParams p) {
-    __shared__ double part[PREP_THREADS / 32];
-    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = 0;
-    const size_t n = static_cast<size_t>(p.rows) * p.cols;
-    const size_t per = (n + p.parts - 1) / p.parts, i0 = blockIdx.x * per, i1 = i0 + per < n ? i0 + per : n;
-    const size_t base = blockIdx.y * n;
-    double s = 0.0;
-    for (size_t i = i0 + threadIdx.x; i < i1; i += PREP_THREADS) {
-        const float g = load_as_float(p.g, p.g_dtype, base + i);
-        float u = g;
-        if (p.m) {
-            const float m = p.mu * p.m[base + i] + g;
-            p.m[base + i] = m;
-            u = p.nesterov ? g + p.mu * m : m;
-        }
-        s += static_cast<double>(u) * u;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < PREP_THREADS / 32; ++i) s += part[i];
-        p.sumsq[static_cast<size_t>(blockIdx.y) * p.parts + blockIdx.x] = s;
-    }
-}
-
-// X_0 = U / max(|U|_F, eps), stored as fp16 times `scale` in the wide orientation with zeros in the padding columns.
-// 64 x 64 blocks through shared memory (the user's matrix may be the transpose): grid (column blocks, row blocks, batch).
-__global__ void __launch_bounds__(PREP_THREADS) muon_start_kernel(const PrepParams p) {
-    __shared__ float blk[64][65];
-    __shared__ float inv_s;
-    const bool tall = p.rows > p.cols;
-    if (threadIdx.x < 32) {
-        double s = 0.0;
-        for (int i = threadIdx.x; i < p.parts; i += 32) s += p.sumsq[static_cast<size_t>(blockIdx.z) * p.parts + i];
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (threadIdx.x == 0) {
-            const float norm = static_cast<float>(sqrt(s));
-            inv_s = p.scale / (norm < p.eps ? p.eps : norm);                // NaN stays NaN
-        }
-    }
-    // the user's block: rows r0.., columns c0.. of [rows, cols]
-    const long x0 = static_cast<long>(blockIdx.x) * 64, y0 = static_cast<long>(blockIdx.y) * 64;   // of X: columns, rows
-    const long r0 = tall ? x0 : y0, c0 = tall ? y0 : x0;
-    const size_t base = static_cast<size_t>(blockIdx.z) * p.rows * p.cols;
-    for (int k = threadIdx.x; k < 64 * 64; k += PREP_THREADS) {
-        const int r = k >> 6, c = k & 63;
-        float u = 0.f;
-        if (r0 + r < p.rows && c0 + c < p.cols) {
-            const size_t i = base + static_cast<size_t>(r0 + r) * p.cols + (c0 + c);
-            u = load_as_float(p.g, p.g_dtype, i);
-            if (p.m) u = p.nesterov ? u + p.mu * p.m[i] : p.m[i];
-        }
-        blk[r][c] = u;
-    }
-    __syncthreads();
-    const float inv = inv_s;
-    for (int k = threadIdx.x; k < 64 * 32; k += PREP_THREADS) {
-        const int y = k >> 5, x = (k & 31) * 2;
-        if (y0 + y >= p.R) continue;
-        const float a = (tall ? blk[x][y] : blk[y][x]) * inv, b = (tall ? blk[x + 1][y] : blk[y][x + 1]) * inv;
-        // ldx is a multiple of 64: the whole block lies inside the row; U is 0 beyond the matrix
-        const __half2 h = __floats2half2_rn(x0 + x < p.C ? a : 0.f, x0 + x + 1 < p.C ? b : 0.f);
-        *reinterpret_cast<__half2*>(p.X + (static_cast<size_t>(blockIdx.z) * p.R + y0 + y) * p.ldx + x0 + x) = h;
-    }
-}
-
-// ------------------------------------------------------------------------------------ the products
-struct Tile { int b, i, j; };               // matrix, row tile (256), column tile (bn)
-
-// GRAM and POLY are symmetric: only the tiles that reach the diagonal or lie right of it are listed (the others are
-// written as mirror images).  A row of tiles i starts at column tile i * 256 / bn.
-__device__ __forceinline__ Tile decode(const GemmParams& p, int t) {
-    Tile w;
-    w.b = t / p.tiles;
-    int r = t - w.b * p.tiles;
-    if (p.phase % 3 == APPLY) {
-        const int nj = (p.C + p.bn - 1) / p.bn;
-        w.i = r / nj;
-        w.j = r - w.i * nj;
-    } else {
-        const int nj = (p.R + p.bn - 1) / p.bn, f = TM / p.bn;
-        w.i = 0;
-        while (r >= nj - w.i * f) { r -= nj - w.i * f; ++w.i; }
-        w.j = w.i * f + r;
-    }
-    return w;
-}
-
-// Whether the tile that holds element (row, col) is listed in a symmetric product.
-__device__ __forceinline__ bool listed(const GemmParams& p, int row, int col) { return (col / p.bn + 1) * p.bn > (row / TM) * TM; }
 
 __device__ __forceinline__ void unpack8(uint4 q, float* f) {
     const __half2* h = reinterpret_cast<const __half2*>(&q);
@@ -195,67 +79,331 @@ __device__ __forceinline__ uint4 pack8(const float* f) {
     return q;
 }
 
-// One warp's 32 x 32 block of the accumulator: result rows row0 + lane, columns col0 .. col0 + 31.
-__device__ __forceinline__ void epilogue_block(const GemmParams& p, int b, int row0, int col0, int lane, float* v, float* stage) {
-    const int mode = p.phase % 3, row = row0 + lane;
-    const int ld = mode == APPLY ? p.ldx : p.lda;
-    const size_t at = (static_cast<size_t>(b) * p.R + row) * ld + col0;
-    if (mode == GRAM) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] *= p.alpha;
+// ------------------------------------------------------------------------------------ momentum, norm, start
+struct PrepParams {
+    const void* g;
+    float* m;                               // null: no momentum (U = G)
+    float mu; int nesterov;
+    int batch; long rows, cols;
+    int parts; double* sumsq;               // [batch][parts]
+    float eps, scale;                       // X_0 is stored times `scale`
+    __half* X; int R, C, ldx;
+    int *status, *next, *done;
+};
+
+// Four consecutive elements (one load of 16 or 8 bytes) or one.
+template <typename G, int V>
+__device__ __forceinline__ void load_v(const G* p, float* f) {
+    if constexpr (V == 1) {
+        f[0] = to_float(*p);
+    } else if constexpr (sizeof(G) == 4) {
+        const float4 q = *reinterpret_cast<const float4*>(p);
+        f[0] = q.x; f[1] = q.y; f[2] = q.z; f[3] = q.w;
     } else {
-        const __half* add = (mode == POLY ? p.A : p.X[(p.phase / 3) & 1]) + at;
+        const uint2 q = *reinterpret_cast<const uint2*>(p);
+        const G* h = reinterpret_cast<const G*>(&q);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (row < p.R) unpack8(__ldcg(reinterpret_cast<const uint4*>(add) + q), f);
+        for (int i = 0; i < 4; ++i) f[i] = to_float(h[i]);
+    }
+}
+template <int V> __device__ __forceinline__ void store_v(float* p, const float* f) {
+    if constexpr (V == 1) *p = f[0];
+    else *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+}
+
+// M <- mu M + G and the sum of squares of U over one part of one matrix: grid (parts, batch).  V: elements per access, 4
+// where every matrix starts on a 16-byte boundary.  Each thread has UNROLL accesses in flight.
+template <typename G, int V>
+__global__ void __launch_bounds__(PREP_THREADS) muon_momentum_kernel(const PrepParams p) {
+    constexpr int UNROLL = V == 4 ? 4 : 8;
+    __shared__ double part[PREP_THREADS / 32];
+    if (blockIdx.x == 0 && threadIdx.x == 0) {                              // the products' bookkeeping starts at zero
+        p.done[blockIdx.y] = 0;
+        if (blockIdx.y == 0) { *p.status = 0; *p.next = 0; }
+    }
+    const long n = p.rows * p.cols / V;                                     // accesses of a matrix
+    const long per = (n + p.parts - 1) / p.parts, i0 = blockIdx.x * per, i1 = i0 + per < n ? i0 + per : n;
+    const G* g = static_cast<const G*>(p.g) + static_cast<size_t>(blockIdx.y) * p.rows * p.cols;
+    float* m = p.m ? p.m + static_cast<size_t>(blockIdx.y) * p.rows * p.cols : nullptr;
+    double s = 0.0;
+    for (long i = i0 + threadIdx.x; i < i1; i += UNROLL * PREP_THREADS) {
+        float gv[UNROLL][V], mv[UNROLL][V];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[8 * q + j] = p.alpha * v[8 * q + j] + p.beta * f[j];
+        for (int k = 0; k < UNROLL; ++k) {
+            const long at = i + k * PREP_THREADS;
+            if (at < i1) {
+                load_v<G, V>(g + at * V, gv[k]);
+                if (m) load_v<float, V>(m + at * V, mv[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < UNROLL; ++k) {
+            const long at = i + k * PREP_THREADS;
+            if (at < i1) {
+                float q = 0.f;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    float u = gv[k][j];
+                    if (m) {
+                        mv[k][j] = p.mu * mv[k][j] + u;
+                        u = p.nesterov ? u + p.mu * mv[k][j] : mv[k][j];
+                    }
+                    q += u * u;
+                }
+                s += q;
+                if (m) store_v<V>(m + at * V, mv[k]);
+            }
         }
     }
-    if (mode == APPLY && p.last) {
-        // to the caller's arrays: coalesced along their rows, through a transpose in shared memory where X's rows are theirs
-        const size_t base = static_cast<size_t>(b) * p.R * p.C;
-        if (!p.transposed) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) stage[lane * EPI_PITCH + j] = v[j];
-            __syncwarp();
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < PREP_THREADS / 32; ++i) s += part[i];
+        p.sumsq[static_cast<size_t>(blockIdx.y) * p.parts + blockIdx.x] = s;
+    }
+}
+
+// scale / max(|U|_F, eps) of matrix b, by every block that needs it (the parts in a fixed order).
+__device__ __forceinline__ float start_factor(const PrepParams& p, int b) {
+    __shared__ float inv_s;
+    if (threadIdx.x < 32) {
+        double s = 0.0;
+        for (int i = threadIdx.x; i < p.parts; i += 32) s += p.sumsq[static_cast<size_t>(b) * p.parts + i];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = stage[j * EPI_PITCH + lane];   // now row row0 + j, column col0 + lane
-            __syncwarp();
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (threadIdx.x == 0) {
+            const float norm = static_cast<float>(sqrt(s));
+            inv_s = p.scale / (norm < p.eps ? p.eps : norm);                // NaN stays NaN
         }
+    }
+    __syncthreads();
+    return inv_s;
+}
+
+template <typename G, int V>
+__device__ __forceinline__ void load_u(const PrepParams& p, size_t at, float* u) {
+    load_v<G, V>(static_cast<const G*>(p.g) + at, u);
+    if (p.m) {
+        float m[V];
+        load_v<float, V>(p.m + at, m);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const int r = p.transposed ? row : row0 + j, c = p.transposed ? col0 + j : col0 + lane;
-            if (r < p.R && c < p.C) {
-                const size_t i = base + (p.transposed ? static_cast<size_t>(c) * p.R + r : static_cast<size_t>(r) * p.C + c);
-                if (p.p) {
-                    const float n = p.p[i] * p.decay - p.step * v[j];
-                    p.p[i] = n;
-                    if (p.w) p.w[i] = __float2bfloat16_rn(n);
-                } else {
-                    store_as(p.out, p.out_dtype, i, v[j]);
-                }
+        for (int j = 0; j < V; ++j) u[j] = p.nesterov ? u[j] + p.mu * m[j] : m[j];
+    }
+}
+
+// X_0 = U / max(|U|_F, eps), stored as fp16 times `scale` with zeros in the padding columns, where the user's matrices are
+// wide already: grid (blocks, batch), eight columns a thread.
+template <typename G, int V>
+__global__ void __launch_bounds__(PREP_THREADS) muon_start_kernel(const PrepParams p) {
+    const float inv = start_factor(p, blockIdx.y);
+    const size_t base = static_cast<size_t>(blockIdx.y) * p.rows * p.cols;
+    const int chunks = p.ldx / 8;
+    const long n = static_cast<long>(p.R) * chunks;
+    for (long k = static_cast<long>(blockIdx.x) * PREP_THREADS + threadIdx.x; k < n; k += static_cast<long>(gridDim.x) * PREP_THREADS) {
+        const long r = k / chunks;
+        const int c = static_cast<int>(k - r * chunks) * 8;
+        float u[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 8; j += V)
+            if (c + j < p.C) load_u<G, V>(p, base + r * p.C + c + j, u + j);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] *= inv;
+        *reinterpret_cast<uint4*>(p.X + (static_cast<size_t>(blockIdx.y) * p.R + r) * p.ldx + c) = pack8(u);
+    }
+}
+
+// The same where they are tall: 64 x 64 blocks pass through shared memory.  Grid (column blocks of X, row blocks, batch).
+template <typename G, int V>
+__global__ void __launch_bounds__(PREP_THREADS) muon_start_tall_kernel(const PrepParams p) {
+    __shared__ float blk[64][65];                                           // [column of X][row of X]
+    const float inv = start_factor(p, blockIdx.z);
+    const long x0 = static_cast<long>(blockIdx.x) * 64, y0 = static_cast<long>(blockIdx.y) * 64;
+    const size_t base = static_cast<size_t>(blockIdx.z) * p.rows * p.cols;
+#pragma unroll
+    for (int q = 0; q < 64 * 64 / V / PREP_THREADS; ++q) {
+        const int k = q * PREP_THREADS + threadIdx.x, x = k / (64 / V), y = k % (64 / V) * V;
+        float u[V] = {};
+        if (x0 + x < p.rows && y0 + y < p.cols) load_u<G, V>(p, base + (x0 + x) * p.cols + y0 + y, u);
+#pragma unroll
+        for (int j = 0; j < V; ++j) blk[x][y + j] = u[j];
+    }
+    __syncthreads();
+    for (int k = threadIdx.x; k < 64 * 8; k += PREP_THREADS) {
+        const int y = k >> 3, x = (k & 7) * 8;
+        if (y0 + y >= p.R) continue;
+        float u[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = blk[x + j][y] * inv;             // columns beyond the matrix hold zeros
+        *reinterpret_cast<uint4*>(p.X + (static_cast<size_t>(blockIdx.z) * p.R + y0 + y) * p.ldx + x0 + x) = pack8(u);
+    }
+}
+
+// ------------------------------------------------------------------------------------ the products
+// Entry of the work list: the tiles of every product of every matrix, product by product, inside a product matrix by matrix.
+struct Tile {
+    int k, mode, b, i, j;                   // product number 3 step + mode, matrix, row tile, column tile
+    int need;                           // need: value of done[b] from which on this product's inputs are complete
+    bool last;
+};
+
+// GRAM and POLY are symmetric: only the tiles on the diagonal and right of it are listed (the others are written as mirror
+// images).
+__device__ __forceinline__ Tile decode(const GemmParams& p, int e) {
+    Tile w;
+    const int per_step = p.tiles[0] + p.tiles[1] + p.tiles[2];
+    const int step = e / (per_step * p.batch);
+    int r = e - step * per_step * p.batch;
+    w.mode = 0;
+    int before = step * per_step;                                           // tiles of the matrix in earlier products
+    while (r >= p.tiles[w.mode] * p.batch) { r -= p.tiles[w.mode] * p.batch; before += p.tiles[w.mode]; ++w.mode; }
+    w.k = 3 * step + w.mode;
+    w.last = w.k + 1 == 3 * p.steps;
+    w.need = before * 2 * EPI_WARPS;
+    w.b = r / p.tiles[w.mode];
+    r -= w.b * p.tiles[w.mode];
+    const int nj = ((w.mode == APPLY ? p.C : p.R) + TN - 1) / TN;
+    if (w.mode == APPLY) {
+        w.i = r / nj;
+        w.j = r - w.i * nj;
+    } else {
+        w.i = 0;
+        while (r >= nj - w.i) { r -= nj - w.i; ++w.i; }
+        w.j = w.i + r;
+    }
+    return w;
+}
+
+// Adds to a counter after everything this warp has written: the writes are made visible to the TMA loads (async proxy) and
+// the generic loads of whoever sees the counter's new value.  Called by the whole warp.
+__device__ __forceinline__ void warp_signal(int* counter, int lane) {
+    asm volatile("fence.proxy.async;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+        __threadfence();
+        asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(counter) : "memory");
+    }
+}
+
+__device__ __forceinline__ int steps_of_k(const GemmParams& p, const Tile& w) { return ((w.mode == GRAM ? p.ldx : p.lda) + KB - 1) / KB; }
+
+// Addend of one warp's 32 x 32 block: 32 consecutive columns of result row `row`, read past the L1 (a buffer is written and
+// read again by other SMs within a call).
+__device__ __forceinline__ void load_addend(const GemmParams& p, const Tile& w, int row, int col0, uint4* q) {
+    const bool apply = w.mode == APPLY;
+    const int ld = apply ? p.ldx : p.lda;
+    const uint4* src = reinterpret_cast<const uint4*>((apply ? p.X[(w.k / 3) & 1] : p.A) + (static_cast<size_t>(w.b) * p.R + row) * ld + col0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = row < p.R && col0 < ld ? __ldcg(src + i) : make_uint4(0u, 0u, 0u, 0u);
+}
+
+// The caller's element that a result element becomes.  All loads of a block are issued before its stores (the compiler may
+// not move them across: p.p could alias itself), so a block costs one memory latency, not sixteen.
+template <int N, typename Index>
+__device__ __forceinline__ void write_last(const GemmParams& p, const float* v, Index index) {
+    if (p.p) {
+        float old[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) { const long at = index(i); old[i] = at >= 0 ? p.p[at] : 0.f; }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const long at = index(i);
+            const float n = old[i] * p.decay - p.step * v[i];
+            if (at >= 0) {
+                p.p[at] = n;
+                if (p.w) p.w[at] = __float2bfloat16_rn(n);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) { const long at = index(i); if (at >= 0) store_as(p.out, p.out_dtype, at, v[i]); }
+    }
+}
+
+// One warp's 32 x 32 block of the accumulator: result rows row0 + lane, columns col0 .. col0 + 31.
+__device__ __forceinline__ void epilogue_block(const GemmParams& p, const Tile& w, int row0, int col0, int lane, float* v,
+                                               const uint4* add, uint8_t* stage) {
+    const int mode = w.mode, row = row0 + lane;
+    const float alpha = p.alpha[w.k], beta = p.beta[w.k];
+    const int ld = mode == APPLY ? p.ldx : p.lda;
+    if (mode == GRAM) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] *= alpha;
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float f[8];
+            unpack8(add[q], f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[8 * q + j] = alpha * v[8 * q + j] + beta * f[j];
+        }
+    }
+    if (w.last) {
+        // to the caller's arrays, coalesced along their rows: X's columns where they hold its transpose, else its rows, for
+        // which 16 columns at a time pass through shared memory
+        const long base = static_cast<long>(w.b) * p.R * p.C;
+        if (p.transposed) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                write_last<16>(p, v + 16 * h, [&](int i) {
+                    const int c = col0 + 16 * h + i;
+                    return row < p.R && c < p.C ? base + static_cast<long>(c) * p.R + row : -1L;
+                });
+        } else {
+            float* t = reinterpret_cast<float*>(stage);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) t[lane * 17 + j] = v[16 * h + j];
+                __syncwarp();
+                float u[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) u[i] = t[(2 * i + (lane >> 4)) * 17 + (lane & 15)];
+                write_last<16>(p, u, [&](int i) {
+                    const int r = row0 + 2 * i + (lane >> 4), c = col0 + 16 * h + (lane & 15);
+                    return r < p.R && c < p.C ? base + static_cast<long>(r) * p.C + c : -1L;
+                });
             }
         }
         return;
     }
-    __half* out = mode == GRAM ? p.A : mode == POLY ? p.B : p.X[((p.phase / 3) & 1) ^ 1];
+    __half* out = (mode == GRAM ? p.A : mode == POLY ? p.B : p.X[((w.k / 3) & 1) ^ 1]) + static_cast<size_t>(w.b) * p.R * ld;
+    uint4 h[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) h[q] = pack8(v + 8 * q);
     if (row < p.R) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) reinterpret_cast<uint4*>(out + at)[q] = pack8(v + 8 * q);
+        for (int q = 0; q < 4; ++q) reinterpret_cast<uint4*>(out + static_cast<size_t>(row) * ld + col0)[q] = h[q];
     }
-    if (mode != APPLY && !listed(p, col0, row0)) {                          // the mirror image: row col0 + j, column `row`
+    if (mode != APPLY && w.j > w.i) {
+        // the mirror image (row col0 + j, column row0 + i) through shared memory: rows of 32 halves, 80 bytes apart
+        __half* t = reinterpret_cast<__half*>(stage);
+        const __half* hv = reinterpret_cast<const __half*>(h);
+        __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (col0 + j < p.R && row < p.lda) out[(static_cast<size_t>(b) * p.R + col0 + j) * ld + row] = __float2half_rn(v[j]);
+        for (int j = 0; j < 32; ++j) t[j * 40 + lane] = hv[j];
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int j = 8 * k + (lane >> 2), part = lane & 3;
+            const uint4 q = *reinterpret_cast<const uint4*>(t + j * 40 + part * 8);
+            if (col0 + j < p.R) *reinterpret_cast<uint4*>(out + static_cast<size_t>(col0 + j) * ld + row0 + part * 8) = q;
+        }
     }
 }
 
-// One product for the whole batch on CTA pairs (tcgen05 cta_group::2, 256 x bn tiles, fp32 accumulators in tensor memory,
-// two of them so that a tile's epilogue overlaps the next tile's products).
+// All products of all matrices in one launch, on CTA pairs (tcgen05 cta_group::2, 256 x 256 tiles, fp32 accumulators in tensor
+// memory, two of them so that a tile's epilogue overlaps the next tile's products).
+//
+// Pairs take the entries of the work list in order from a counter.  An entry whose inputs other pairs are still writing waits
+// for its matrix's `done` count; an entry only ever waits for entries before it in the list, which running pairs hold, so
+// there is always one that can finish, however many pairs the GPU runs at a time.
+constexpr int SCHED_DEPTH = 4;
+
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1)
-muon_gemm_kernel(const __grid_constant__ Maps maps, const __grid_constant__ GemmParams p) {
+muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ GemmParams p) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;                          // swizzle atoms need 1024-byte alignment
@@ -266,25 +414,28 @@ muon_gemm_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Gemm
     auto tfull_bar = [&](int a) { return bars + 8u * (2 * STAGES + a); };
     auto tempty_bar = [&](int a) { return bars + 8u * (2 * STAGES + 2 + a); };   // the leader's is used
     const uint32_t drain_bar = bars + 8u * (2 * STAGES + 4);
-    constexpr int NUM_BARS = 2 * STAGES + 5;
+    auto sfull_bar = [&](int s) { return bars + 8u * (2 * STAGES + 5 + s); };
+    auto sempty_bar = [&](int s) { return bars + 8u * (2 * STAGES + 5 + SCHED_DEPTH + s); };   // the leader's is used
+    constexpr int NUM_BARS = 2 * STAGES + 5 + 2 * SCHED_DEPTH;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + STAGES * STAGE_BYTES + 8 * NUM_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    float* epi = reinterpret_cast<float*>(smem + STAGES * STAGE_BYTES + 256);
+    volatile int* sched_slot = reinterpret_cast<volatile int*>(tmem_slot + 2);   // [SCHED_DEPTH] list positions
+    const uint32_t sched_slot_addr = bars + 8u * NUM_BARS + 8u;
+    uint8_t* epi = smem + STAGES * STAGE_BYTES + 512;
+    static_assert(8 * NUM_BARS + 8 + 4 * SCHED_DEPTH <= 512, "barriers before the epilogue's staging");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const bool leader = rank == 0;
-    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int total = p.tiles * p.batch;
-    const int mode = p.phase % 3, xb = (p.phase / 3) & 1;
-    const int num_kb = (mode == GRAM ? p.ldx : p.lda) / KB;
-    const int b_boxes = p.bn / 128;                                          // boxes of 64 columns in this CTA's half of a tile
+    const int total = p.steps * (p.tiles[0] + p.tiles[1] + p.tiles[2]) * p.batch;
 
     if (threadIdx.x == 0) {
         *abort_flag = 0;
         for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 8); }
+        for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 2 * EPI_WARPS); }
         mbar_init(drain_bar, 1);
+        // a slot is free again when the leader's MMA lane and epilogue warps and the peer's producer and epilogue warps have read it
+        for (int s = 0; s < SCHED_DEPTH; ++s) { mbar_init(sfull_bar(s), 1); mbar_init(sempty_bar(s), 2 + 2 * EPI_WARPS); }
         fence_barrier_init();
         fence_proxy_async();
     }
@@ -297,29 +448,55 @@ muon_gemm_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Gemm
     cluster_sync_all();                                                      // the peer's barriers exist before any remote signal
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    auto sched_ack = [&](int ss) { mbar_arrive_cluster(mapa_shared(sempty_bar(ss), 0)); };
 
     if (warp == 0) {
+        // ---------------------------------------------------------------- scheduler (leader) + TMA producer (both CTAs)
         if (lane == 0) {
-            const CUtensorMap* ma = mode == GRAM ? &maps.x_k[xb] : mode == POLY ? &maps.a_k : &maps.b_k;
-            const CUtensorMap* mb = mode == GRAM ? &maps.x_k[xb] : mode == POLY ? &maps.a_k : &maps.x_mn[xb];
             int stage = 0; uint32_t phase = 0; bool ok = true;
+            int ss = 0; uint32_t sphase = 0;
             long issued = 0;
-            for (int t = pair; t < total && ok; t += pairs) {
+            bool exhausted = false;
+            auto publish = [&]() -> int {                                    // takes the next list position for both CTAs
+                if (exhausted) return -1;
+                if (!mbar_wait_cluster(sempty_bar(ss), sphase ^ 1u, abort_flag, p.wait_limit_ns)) { ok = false; return -1; }
+                int t = atomicAdd(p.next, 1);
+                if (t >= total) { t = -1; exhausted = true; }
+                sched_slot[ss] = t;
+                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(mapa_shared(sched_slot_addr + 4u * ss, 1)), "r"(t) : "memory");
+                mbar_arrive(sfull_bar(ss));
+                mbar_arrive_cluster(mapa_shared(sfull_bar(ss), 1));          // release.cluster: the peer sees its slot
+                if (++ss == SCHED_DEPTH) { ss = 0; sphase ^= 1u; }
+                return t;
+            };
+            while (ok) {
+                int t;
+                if (leader) {
+                    t = publish();
+                    if (!ok) break;
+                } else {
+                    if (!mbar_wait_cluster(sfull_bar(ss), sphase, abort_flag, p.wait_limit_ns)) { ok = false; break; }
+                    t = sched_slot[ss];
+                    sched_ack(ss);
+                    if (++ss == SCHED_DEPTH) { ss = 0; sphase ^= 1u; }
+                }
+                if (t < 0) break;
                 const Tile w = decode(p, t);
-                const int arow = w.i * TM + static_cast<int>(rank) * 128;
-                const int bcol = w.j * p.bn + static_cast<int>(rank) * (p.bn / 2);
+                if (w.k > 0 && !flag_wait_ge(p.done + w.b, w.need, abort_flag, p.wait_limit_ns)) { ok = false; break; }
+                const int xb = (w.k / 3) & 1;
+                const CUtensorMap* ma = w.mode == GRAM ? &maps.x_k[xb] : w.mode == POLY ? &maps.a : &maps.b;
+                const CUtensorMap* mb = w.mode == GRAM ? &maps.x_k[xb] : w.mode == POLY ? &maps.a : &maps.x_mn[xb];
+                const int num_kb = steps_of_k(p, w);
+                const int arow = w.i * TM + static_cast<int>(rank) * 128, bcol = w.j * TN + static_cast<int>(rank) * 128;
                 for (int kb = 0; kb < num_kb; ++kb) {
                     if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, p.wait_limit_ns)) { ok = false; break; }
-                    if (leader) mbar_arrive_expect_tx(full_bar(stage), 2 * (A_BYTES + b_boxes * BOX_BYTES));
+                    if (leader) mbar_arrive_expect_tx(full_bar(stage), 2 * STAGE_BYTES);
                     const uint32_t bar = mapa_shared(full_bar(stage), 0);
-                    const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + A_BYTES;
-                    // rows beyond the matrix arrive as zeros
-                    tma2_load_3d_plain(sa, ma, bar, kb * KB, arow, w.b);
-                    tma2_load_3d_plain(sa + BOX_BYTES, ma, bar, kb * KB, arow + 64, w.b);
-                    for (int q = 0; q < b_boxes; ++q) {
-                        if (mode == APPLY) tma2_load_4d(sb + q * BOX_BYTES, mb, bar, 0, kb * KB, bcol / 64 + q, w.b);
-                        else tma2_load_3d_plain(sb + q * BOX_BYTES, mb, bar, kb * KB, bcol + 64 * q, w.b);
-                    }
+                    const uint32_t sa = base + stage * STAGE_BYTES;
+                    // rows and chunks beyond the matrix arrive as zeros
+                    tma2_load_4d(sa, ma, bar, 0, arow, kb, w.b);
+                    if (w.mode == APPLY) tma2_load_4d(sa + A_BYTES, mb, bar, 0, kb * KB, bcol / 64, w.b);
+                    else tma2_load_4d(sa + A_BYTES, mb, bar, 0, bcol, kb, w.b);
                     ++issued;
                     if (++stage == STAGES) { stage = 0; phase ^= 1u; }
                 }
@@ -336,11 +513,20 @@ muon_gemm_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Gemm
             }
         }
     } else if (warp == 1) {
+        // ---------------------------------------------------------------- MMA issuer (leader CTA only)
         if (lane == 0 && leader) {
-            const uint32_t idesc = make_idesc(p.bn, false, mode == APPLY, TM, 0u);    // fp16 operands
             int stage = 0; uint32_t phase = 0; bool ok = true;
-            int it = 0;
-            for (int t = pair; t < total && ok; t += pairs, ++it) {
+            int ss = 0; uint32_t sphase = 0;
+            for (int it = 0; ok; ++it) {
+                if (!mbar_wait(sfull_bar(ss), sphase, abort_flag, p.wait_limit_ns)) { ok = false; break; }
+                const int t = sched_slot[ss];
+                sched_ack(ss);
+                if (++ss == SCHED_DEPTH) { ss = 0; sphase ^= 1u; }
+                if (t < 0) break;
+                const Tile w = decode(p, t);
+                const bool apply = w.mode == APPLY;
+                const uint32_t idesc = make_idesc(TN, false, apply, TM, 0u);       // fp16 operands
+                const int num_kb = steps_of_k(p, w);
                 const int ab = it & 1;
                 if (!mbar_wait_cluster(tempty_bar(ab), ((it >> 1) & 1u) ^ 1u, abort_flag, p.wait_limit_ns)) { ok = false; break; }
                 tc_fence_after();
@@ -350,12 +536,12 @@ muon_gemm_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Gemm
                     tc_fence_after();
                     const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + A_BYTES;
                     const uint64_t adesc = make_smem_desc(sa, 16, 1024);
-                    const uint64_t bdesc = mode == APPLY ? make_smem_desc(sb, BOX_BYTES, 1024) : make_smem_desc(sb, 16, 1024);
+                    const uint64_t bdesc = make_smem_desc(sb, apply ? 64 * 128 : 16, 1024);
 #pragma unroll
                     for (int k = 0; k < KB / 16; ++k) {
                         // K-major: 16 elements = 32 bytes along the swizzled row; MN-major: 16 rows of 128 bytes
-                        const uint64_t boff = static_cast<uint64_t>((mode == APPLY ? k * 16 * 128 : k * 32) >> 4);
-                        umma2_f16(tmem_d, adesc + static_cast<uint64_t>((k * 32) >> 4), bdesc + boff, idesc, (kb | k) != 0 ? 1u : 0u);
+                        const uint32_t along = k * 32, down = k * 16 * 128;
+                        umma2_f16(tmem_d, adesc + (along >> 4), bdesc + ((apply ? down : along) >> 4), idesc, (kb | k) != 0 ? 1u : 0u);
                     }
                     umma2_commit_both(empty_bar(stage));
                     if (++stage == STAGES) { stage = 0; phase ^= 1u; }
@@ -369,30 +555,53 @@ muon_gemm_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Gemm
             }
         }
     } else {
-        const int quad = warp & 3;
-        float* stage = epi + (warp - 2) * 32 * EPI_PITCH;
-        int it = 0;
-        for (int t = pair; t < total; t += pairs, ++it) {
+        // ---------------------------------------------------------------- epilogue warps (both CTAs)
+        const int quad = warp & 3, half = (warp - 2) >> 2;
+        uint8_t* stage = epi + (warp - 2) * EPI_WARP_BYTES;
+        int ss = 0; uint32_t sphase = 0;
+        for (int it = 0;; ++it) {
+            int t = -2;
+            if (lane == 0 && mbar_wait_cluster(sfull_bar(ss), sphase, abort_flag, p.wait_limit_ns)) {
+                t = sched_slot[ss];
+                sched_ack(ss);
+            }
+            t = __shfl_sync(0xffffffffu, t, 0);
+            if (++ss == SCHED_DEPTH) { ss = 0; sphase ^= 1u; }
+            if (t < 0) break;                                                // -1: list exhausted, -2: gave up
             const Tile w = decode(p, t);
             const int ab = it & 1;
-            const bool ok = mbar_wait(tfull_bar(ab), (it >> 1) & 1u, abort_flag, p.wait_limit_ns);
+            const int row0 = w.i * TM + static_cast<int>(rank) * 128 + quad * 32;
+            const int ncols = w.mode == APPLY ? p.ldx : p.lda;
+            // the addend of a block is fetched while the block before it is worked on; the first as soon as it is complete
+            uint4 add[4];
+            int ok = 1;
+            if (w.mode != GRAM) {
+                if (lane == 0) ok = flag_wait_ge(p.done + w.b, w.need, abort_flag, p.wait_limit_ns);
+                ok = __shfl_sync(0xffffffffu, ok, 0);
+                if (!ok) break;
+                load_addend(p, w, row0 + lane, w.j * TN + half * 32, add);
+            }
+            ok = mbar_wait(tfull_bar(ab), (it >> 1) & 1u, abort_flag, p.wait_limit_ns);
             if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
             const uint32_t tmem_row = tmem_base + ab * TN + (static_cast<uint32_t>(quad * 32) << 16);
-            const int row0 = w.i * TM + static_cast<int>(rank) * 128 + quad * 32;
-            const int ncols = mode == APPLY ? p.ldx : p.lda;
-            for (int c = 0; c < p.bn / 32; ++c) {
-                const int col0 = w.j * p.bn + c * 32;
+            for (int c = half; c < TN / 32; c += 2) {
+                const int col0 = w.j * TN + c * 32;
                 if (row0 >= p.R || col0 >= ncols) break;                     // uniform in the warp
                 float v[32];
                 __syncwarp();
                 tmem_ld32(tmem_row + c * 32, v);
+                uint4 next[4];
+                if (w.mode != GRAM && c + 2 < TN / 32) load_addend(p, w, row0 + lane, col0 + 64, next);
                 tmem_ld_wait();
-                epilogue_block(p, w.b, row0, col0, lane, v, stage);
+                epilogue_block(p, w, row0, col0, lane, v, add, stage);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) add[q] = next[q];
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(mapa_shared(tempty_bar(ab), 0));
+            if (!w.last) warp_signal(p.done + w.b, lane);
         }
     }
 
