@@ -124,13 +124,14 @@ bool encode(CUtensorMap* map, void* ptr, int rank, const cuuint64_t* dims, const
     auto enc = get_encode();
     const cuuint32_t ones[4] = {1, 1, 1, 1};
     return enc && enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, ptr, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                      box[0] == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // [batch][rows][ld] fp16, ld a multiple of 64; see Maps.
-bool map_operand(CUtensorMap* map, __half* ptr, int64_t batch, int64_t rows, int64_t ld, cuuint32_t box_rows, cuuint32_t box_chunks) {
+bool map_operand(CUtensorMap* map, __half* ptr, int64_t batch, int64_t rows, int64_t ld, cuuint32_t box_rows, cuuint32_t box_chunks,
+                 cuuint32_t box_elems = 64) {
     const cuuint64_t dims[4] = {64, static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(ld / 64), static_cast<cuuint64_t>(batch)};
     const cuuint64_t strides[3] = {static_cast<cuuint64_t>(2 * ld), 128, static_cast<cuuint64_t>(2 * ld * rows)};
-    const cuuint32_t box[4] = {64, box_rows, box_chunks, 1};
+    const cuuint32_t box[4] = {box_elems, box_rows, box_chunks, 1};
     return encode(map, ptr, 4, dims, strides, box);
 }
 
@@ -206,9 +207,11 @@ int run(const void* g, int g_dtype, float* m, float mu, int nesterov, int64_t ba
     q.status = reinterpret_cast<int*>(base); q.next = q.status + 16; q.done = reinterpret_cast<int*>(base + L.done);
     q.wait_limit_ns = static_cast<unsigned long long>(vp_ce_set_wait_limit_ns(0));
     Maps maps;
-    bool ok = map_operand(&maps.a, q.A, batch, L.R, L.lda, 128, 1) && map_operand(&maps.b, q.B, batch, L.R, L.lda, 128, 1);
+    bool ok = map_operand(&maps.a, q.A, batch, L.R, L.lda, 128, 1) && map_operand(&maps.b, q.B, batch, L.R, L.lda, 128, 1) &&
+              map_operand(&maps.a_blk, q.A, batch, L.R, L.lda, 32, 1, 32) && map_operand(&maps.b_blk, q.B, batch, L.R, L.lda, 32, 1, 32);
     for (int i = 0; i < 2; ++i)
-        ok = ok && map_operand(&maps.x_k[i], q.X[i], batch, L.R, L.ldx, 128, 1) && map_operand(&maps.x_mn[i], q.X[i], batch, L.R, L.ldx, 64, 2);
+        ok = ok && map_operand(&maps.x_k[i], q.X[i], batch, L.R, L.ldx, 128, 1) && map_operand(&maps.x_mn[i], q.X[i], batch, L.R, L.ldx, 64, 2) &&
+             map_operand(&maps.x_blk[i], q.X[i], batch, L.R, L.ldx, 32, 1, 32);
     if (!ok || ensure_smem() != cudaSuccess) return VPCE_CUDA_ERROR;
 
     PrepParams pp{};

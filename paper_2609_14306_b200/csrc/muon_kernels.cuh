@@ -16,12 +16,15 @@ constexpr int TM = 256, TN = 256;           // a tile: one CTA pair, 128 rows an
 constexpr int KB = 64;                      // K per pipeline stage: one 128-byte swizzle row of fp16
 constexpr int A_BYTES = 128 * 128;          // 128 rows of the left operand
 constexpr int STAGE_BYTES = 2 * A_BYTES;
-constexpr int STAGES = 6;
+constexpr int STAGES = 5;
 constexpr int EPI_WARPS = 8;                // two per quarter of the tensor memory's lanes, each every other 32 columns
 constexpr int GEMM_THREADS = 64 + 32 * EPI_WARPS;   // warp 0 TMA, warp 1 MMA, the others epilogue
-constexpr int EPI_WARP_BYTES = 2560;        // of shared memory per epilogue warp, for transposing a 32 x 32 block
+constexpr int BLOCK_BYTES = 32 * 64;        // a 32 x 32 block of fp16: 64-byte rows, 64-byte swizzle
+constexpr int WARP_BLOCKS = TN / 32 / 2;    // blocks of one warp in a tile
+constexpr int EPI_WARP_BYTES = WARP_BLOCKS * BLOCK_BYTES;   // see the epilogue
 constexpr int EPI_BYTES = EPI_WARPS * EPI_WARP_BYTES;
-constexpr int GEMM_SMEM = STAGES * STAGE_BYTES + EPI_BYTES + 2048;
+constexpr int GEMM_SMEM = STAGES * STAGE_BYTES + EPI_BYTES + 2048;   // barriers (1024) and alignment slack
+static_assert(GEMM_SMEM <= 227 * 1024, "shared memory per CTA");
 constexpr int MAX_STEPS = 32;
 constexpr int PREP_THREADS = 256;
 constexpr int MAX_PARTS = 512;              // partial sums of squares per matrix
@@ -33,7 +36,8 @@ enum Mode { GRAM = 0, POLY = 1, APPLY = 2 };
 // box of 128 rows x 1 chunk, down the columns (X as right operand of B X, K = rows) one of 64 rows x 2 chunks.  The chunk as a
 // dimension of its own matters: boxes at column offsets of a 3-D array {columns, rows, batch} arrived at 48 bytes a cycle and
 // SM, these at 70 (loads alone, 128-row boxes; the products need 64).
-struct Maps { CUtensorMap x_k[2], x_mn[2], a, b; };
+// The epilogue moves boxes of 32 rows x 32 elements of the same arrays (*_blk).
+struct Maps { CUtensorMap x_k[2], x_mn[2], a, b, x_blk[2], a_blk, b_blk; };
 
 struct GemmParams {
     int batch, R, C;                        // matrices R x C with R <= C
@@ -56,16 +60,37 @@ __device__ __forceinline__ void tma2_load_4d(uint32_t dst, const CUtensorMap* ma
         "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+__device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2, int c3) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+__device__ __forceinline__ void bulk_wait_read_all() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float ld_shared_f32(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void st_shared_f32(uint32_t addr, float v) {
+    asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+__device__ __forceinline__ void st_shared_b16(uint32_t addr, uint16_t v) {
+    asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"(v) : "memory");
+}
+
 // ------------------------------------------------------------------------------------ element types
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void store_as(void* p, int dtype, size_t i, float v) {
-    if (dtype == VPCE_F32) static_cast<float*>(p)[i] = v;
-    else if (dtype == VPCE_F16) static_cast<__half*>(p)[i] = __float2half_rn(v);
-    else static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
-}
-
 __device__ __forceinline__ void unpack8(uint4 q, float* f) {
     const __half2* h = reinterpret_cast<const __half2*>(&q);
 #pragma unroll
@@ -275,122 +300,114 @@ __device__ __forceinline__ Tile decode(const GemmParams& p, int e) {
     return w;
 }
 
-// Adds to a counter after everything this warp has written: the writes are made visible to the TMA loads (async proxy) and
-// the generic loads of whoever sees the counter's new value.  Called by the whole warp.
-__device__ __forceinline__ void warp_signal(int* counter, int lane) {
+// Adds to a counter once this lane's TMA stores have been performed, for whoever loads the written data after seeing the new
+// value (the fences order the copies of the async proxy and the counter on both sides).
+__device__ __forceinline__ void signal_stored(int* counter) {
+    bulk_wait_all();
     asm volatile("fence.proxy.async;" ::: "memory");
-    __syncwarp();
-    if (lane == 0) {
-        __threadfence();
-        asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(counter) : "memory");
-    }
+    asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(counter) : "memory");
 }
 
 __device__ __forceinline__ int steps_of_k(const GemmParams& p, const Tile& w) { return ((w.mode == GRAM ? p.ldx : p.lda) + KB - 1) / KB; }
 
-// Addend of one warp's 32 x 32 block: 32 consecutive columns of result row `row`, read past the L1 (a buffer is written and
-// read again by other SMs within a call).
-__device__ __forceinline__ void load_addend(const GemmParams& p, const Tile& w, int row, int col0, uint4* q) {
-    const bool apply = w.mode == APPLY;
-    const int ld = apply ? p.ldx : p.lda;
-    const uint4* src = reinterpret_cast<const uint4*>((apply ? p.X[(w.k / 3) & 1] : p.A) + (static_cast<size_t>(w.b) * p.R + row) * ld + col0);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) q[i] = row < p.R && col0 < ld ? __ldcg(src + i) : make_uint4(0u, 0u, 0u, 0u);
-}
+// Byte offset of 16-byte chunk c (8 halves) of row r in a 64-byte-swizzled block.
+__device__ __forceinline__ uint32_t block_at(int r, int c) { return static_cast<uint32_t>(r * 64 + ((c ^ ((r >> 1) & 3)) << 4)); }
 
-// The caller's element that a result element becomes.  All loads of a block are issued before its stores (the compiler may
-// not move them across: p.p could alias itself), so a block costs one memory latency, not sixteen.
-template <int N, typename Index>
-__device__ __forceinline__ void write_last(const GemmParams& p, const float* v, Index index) {
-    if (p.p) {
-        float old[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) { const long at = index(i); old[i] = at >= 0 ? p.p[at] : 0.f; }
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const long at = index(i);
-            const float n = old[i] * p.decay - p.step * v[i];
-            if (at >= 0) {
-                p.p[at] = n;
-                if (p.w) p.w[at] = __float2bfloat16_rn(n);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) { const long at = index(i); if (at >= 0) store_as(p.out, p.out_dtype, at, v[i]); }
-    }
-}
-
-// One warp's 32 x 32 block of the accumulator: result rows row0 + lane, columns col0 .. col0 + 31.
-__device__ __forceinline__ void epilogue_block(const GemmParams& p, const Tile& w, int row0, int col0, int lane, float* v,
-                                               const uint4* add, uint8_t* stage) {
-    const int mode = w.mode, row = row0 + lane;
+// One warp's 32 x 32 block of the accumulator (result rows row0 + lane, columns col0 ..): the addend lies in `blk`, the result
+// takes its place and leaves by TMA store, as does its mirror image through `mir`.
+__device__ __forceinline__ void epilogue_block(const GemmParams& p, const Maps& maps, const Tile& w, int row0, int col0, int lane,
+                                               float* v, uint32_t blk, uint32_t mir) {
     const float alpha = p.alpha[w.k], beta = p.beta[w.k];
-    const int ld = mode == APPLY ? p.ldx : p.lda;
-    if (mode == GRAM) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] *= alpha;
-    } else {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float f[8];
-            unpack8(add[q], f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[8 * q + j] = alpha * v[8 * q + j] + beta * f[j];
-        }
-    }
-    if (w.last) {
-        // to the caller's arrays, coalesced along their rows: X's columns where they hold its transpose, else its rows, for
-        // which 16 columns at a time pass through shared memory
-        const long base = static_cast<long>(w.b) * p.R * p.C;
-        if (p.transposed) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                write_last<16>(p, v + 16 * h, [&](int i) {
-                    const int c = col0 + 16 * h + i;
-                    return row < p.R && c < p.C ? base + static_cast<long>(c) * p.R + row : -1L;
-                });
-        } else {
-            float* t = reinterpret_cast<float*>(stage);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                __syncwarp();
-#pragma unroll
-                for (int j = 0; j < 16; ++j) t[lane * 17 + j] = v[16 * h + j];
-                __syncwarp();
-                float u[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) u[i] = t[(2 * i + (lane >> 4)) * 17 + (lane & 15)];
-                write_last<16>(p, u, [&](int i) {
-                    const int r = row0 + 2 * i + (lane >> 4), c = col0 + 16 * h + (lane & 15);
-                    return r < p.R && c < p.C ? base + static_cast<long>(r) * p.C + c : -1L;
-                });
-            }
-        }
-        return;
-    }
-    __half* out = (mode == GRAM ? p.A : mode == POLY ? p.B : p.X[((w.k / 3) & 1) ^ 1]) + static_cast<size_t>(w.b) * p.R * ld;
     uint4 h[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) h[q] = pack8(v + 8 * q);
-    if (row < p.R) {
+    for (int q = 0; q < 4; ++q) {
+        float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (w.mode != GRAM) unpack8(ld_shared_v4(blk + block_at(lane, q)), f);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) reinterpret_cast<uint4*>(out + static_cast<size_t>(row) * ld + col0)[q] = h[q];
+        for (int j = 0; j < 8; ++j) f[j] = alpha * v[8 * q + j] + beta * f[j];
+        h[q] = pack8(f);
+        st_shared_v4(blk + block_at(lane, q), h[q]);
     }
-    if (mode != APPLY && w.j > w.i) {
-        // the mirror image (row col0 + j, column row0 + i) through shared memory: rows of 32 halves, 80 bytes apart
-        __half* t = reinterpret_cast<__half*>(stage);
-        const __half* hv = reinterpret_cast<const __half*>(h);
-        __syncwarp();
+    const bool mirror = w.mode != APPLY && w.j > w.i && col0 < p.R;
+    if (mirror) {
+        const uint16_t* hv = reinterpret_cast<const uint16_t*>(h);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) t[j * 40 + lane] = hv[j];
-        __syncwarp();
+        for (int j = 0; j < 32; ++j) st_shared_b16(mir + block_at(j, lane >> 3) + (lane & 7) * 2, hv[j]);
+    }
+    fence_proxy_async();
+    __syncwarp();
+    if (lane == 0) {
+        const CUtensorMap* out = w.mode == GRAM ? &maps.a_blk : w.mode == POLY ? &maps.b_blk : &maps.x_blk[((w.k / 3) & 1) ^ 1];
+        tma_store_4d(out, blk, col0 & 63, row0, col0 >> 6, w.b);
+        if (mirror) tma_store_4d(out, mir, row0 & 63, col0, row0 >> 6, w.b);
+        bulk_commit();
+    }
+}
+
+// One warp's block of the last product, to the caller's arrays: coalesced along their rows.  Where those are X's columns
+// (TRANSPOSED) a lane keeps its row of X and element i is column col0 + i; else 16 columns at a time pass through shared memory
+// (`blk`, whose addend is read first) and element i is row row0 + 2 (i % 16) + lane / 16, column col0 + 16 (i / 16) + lane % 16.
+// All loads of a block are issued before its stores (p could alias itself for all the compiler knows): one memory latency a
+// block, not 32.  Nothing here is used again soon: evict-first, so that the operands stay in the L2.
+template <bool TRANSPOSED>
+__device__ __forceinline__ void epilogue_last(const GemmParams& p, const Tile& w, int row0, int col0, int lane, uint32_t tmem, uint32_t blk) {
+    const int r = row0 + (TRANSPOSED ? lane : lane >> 4), c = col0 + (TRANSPOSED ? 0 : lane & 15);
+    const long at = static_cast<long>(w.b) * p.R * p.C + (TRANSPOSED ? static_cast<long>(c) * p.R + r : static_cast<long>(r) * p.C + c);
+    const int pitch = TRANSPOSED ? p.R : 2 * p.C;
+    auto offset = [&](int i) { return TRANSPOSED ? i * pitch : (i & 15) * pitch + (i & 16); };
+    auto inside = [&](int i) { return TRANSPOSED ? r < p.R && c + i < p.C : r + 2 * (i & 15) < p.R && c + (i & 16) < p.C; };
+    float old[32];
+    if (p.p) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int j = 8 * k + (lane >> 2), part = lane & 3;
-            const uint4 q = *reinterpret_cast<const uint4*>(t + j * 40 + part * 8);
-            if (col0 + j < p.R) *reinterpret_cast<uint4*>(out + static_cast<size_t>(col0 + j) * ld + row0 + part * 8) = q;
+        for (int i = 0; i < 32; ++i) old[i] = inside(i) ? __ldcs(p.p + at + offset(i)) : 0.f;
+    }
+    float v[32];
+    __syncwarp();
+    tmem_ld32(tmem, v);
+    tmem_ld_wait();
+    const float alpha = p.alpha[w.k], beta = p.beta[w.k];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float f[8];
+        unpack8(ld_shared_v4(blk + block_at(lane, q)), f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[8 * q + j] = alpha * v[8 * q + j] + beta * f[j];
+    }
+    if (!TRANSPOSED) {
+        // element (row, j) of 16 columns at word 16 row + (j ^ row % 16): no bank is hit more than twice
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) st_shared_f32(blk + 4 * (16 * lane + (j ^ (lane & 15))), v[16 * h + j]);
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int row = 2 * i + (lane >> 4);
+                v[16 * h + i] = ld_shared_f32(blk + 4 * (16 * row + ((lane & 15) ^ (row & 15))));
+            }
         }
+    }
+    if (p.p) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            v[i] = old[i] * p.decay - p.step * v[i];
+            if (inside(i)) __stcs(p.p + at + offset(i), v[i]);
+        }
+        if (p.w) {
+            unsigned short* wp = reinterpret_cast<unsigned short*>(p.w) + at;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) if (inside(i)) __stcs(wp + offset(i), __bfloat16_as_ushort(__float2bfloat16_rn(v[i])));
+        }
+    } else if (p.out_dtype == VPCE_F32) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) if (inside(i)) __stcs(static_cast<float*>(p.out) + at + offset(i), v[i]);
+    } else {
+        unsigned short* o = static_cast<unsigned short*>(p.out) + at;
+        const bool f16 = p.out_dtype == VPCE_F16;
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (inside(i)) __stcs(o + offset(i), f16 ? __half_as_ushort(__float2half_rn(v[i])) : __bfloat16_as_ushort(__float2bfloat16_rn(v[i])));
     }
 }
 
@@ -416,13 +433,14 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
     const uint32_t drain_bar = bars + 8u * (2 * STAGES + 4);
     auto sfull_bar = [&](int s) { return bars + 8u * (2 * STAGES + 5 + s); };
     auto sempty_bar = [&](int s) { return bars + 8u * (2 * STAGES + 5 + SCHED_DEPTH + s); };   // the leader's is used
-    constexpr int NUM_BARS = 2 * STAGES + 5 + 2 * SCHED_DEPTH;
+    auto add_bar = [&](int q) { return bars + 8u * (2 * STAGES + 5 + 2 * SCHED_DEPTH + q); };   // one per epilogue warp
+    constexpr int NUM_BARS = 2 * STAGES + 5 + 2 * SCHED_DEPTH + EPI_WARPS;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + STAGES * STAGE_BYTES + 8 * NUM_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     volatile int* sched_slot = reinterpret_cast<volatile int*>(tmem_slot + 2);   // [SCHED_DEPTH] list positions
     const uint32_t sched_slot_addr = bars + 8u * NUM_BARS + 8u;
-    uint8_t* epi = smem + STAGES * STAGE_BYTES + 512;
-    static_assert(8 * NUM_BARS + 8 + 4 * SCHED_DEPTH <= 512, "barriers before the epilogue's staging");
+    const uint32_t epi = bars + 1024u;                                       // 1024-byte aligned
+    static_assert(8 * NUM_BARS + 8 + 4 * SCHED_DEPTH <= 1024, "barriers before the epilogue's staging");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
@@ -436,6 +454,7 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
         mbar_init(drain_bar, 1);
         // a slot is free again when the leader's MMA lane and epilogue warps and the peer's producer and epilogue warps have read it
         for (int s = 0; s < SCHED_DEPTH; ++s) { mbar_init(sfull_bar(s), 1); mbar_init(sempty_bar(s), 2 + 2 * EPI_WARPS); }
+        for (int q = 0; q < EPI_WARPS; ++q) mbar_init(add_bar(q), 1);
         fence_barrier_init();
         fence_proxy_async();
     }
@@ -557,7 +576,12 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
     } else {
         // ---------------------------------------------------------------- epilogue warps (both CTAs)
         const int quad = warp & 3, half = (warp - 2) >> 2;
-        uint8_t* stage = epi + (warp - 2) * EPI_WARP_BYTES;
+        // A warp has four blocks of shared memory.  A block of the result takes the place of its addend, which was loaded there.
+        // APPLY has one for each of a tile's four blocks, all loaded while the products run.  The symmetric products need half
+        // of them for the mirror images: their blocks take turns in two, and the addends of POLY's last two blocks arrive
+        // while the blocks before them are worked on.
+        const uint32_t blocks = epi + (warp - 2) * EPI_WARP_BYTES, abar = add_bar(warp - 2);
+        uint32_t aphase = 0;
         int ss = 0; uint32_t sphase = 0;
         for (int it = 0;; ++it) {
             int t = -2;
@@ -572,37 +596,73 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
             const int ab = it & 1;
             const int row0 = w.i * TM + static_cast<int>(rank) * 128 + quad * 32;
             const int ncols = w.mode == APPLY ? p.ldx : p.lda;
-            // the addend of a block is fetched while the block before it is worked on; the first as soon as it is complete
-            uint4 add[4];
+            // blocks of this warp: columns w.j * TN + 64 n + 32 half
+            const int col_first = w.j * TN + half * 32;
+            int blocks_here = row0 < p.R && col_first < ncols ? (ncols - col_first + 63) / 64 : 0;
+            if (blocks_here > WARP_BLOCKS) blocks_here = WARP_BLOCKS;
+            // the addends of all its blocks arrive while the products run
+            const bool addend = w.mode != GRAM && blocks_here > 0;
+            const CUtensorMap* from = w.mode == POLY ? &maps.a_blk : &maps.x_blk[(w.k / 3) & 1];
+            auto place = [&](int n) { return blocks + (w.mode == APPLY ? n : n & 1) * BLOCK_BYTES; };
+            auto load_block = [&](int n) { tma_load_4d(place(n), from, abar, half * 32, row0, w.j * (TN / 64) + n, w.b); };
+            auto await_addend = [&]() {
+                const bool got = mbar_wait(abar, aphase, abort_flag, p.wait_limit_ns);
+                aphase ^= 1u;
+                if (__all_sync(0xffffffffu, got)) return true;
+                const unsigned long long t0 = globaltimer_ns();              // give-up path: the copies in flight land first
+                while (!mbar_try_wait(abar, aphase ^ 1u) && globaltimer_ns() - t0 < p.wait_limit_ns) {}
+                return false;
+            };
             int ok = 1;
-            if (w.mode != GRAM) {
-                if (lane == 0) ok = flag_wait_ge(p.done + w.b, w.need, abort_flag, p.wait_limit_ns);
-                ok = __shfl_sync(0xffffffffu, ok, 0);
-                if (!ok) break;
-                load_addend(p, w, row0 + lane, w.j * TN + half * 32, add);
+            if (lane == 0) {
+                if (addend) ok = flag_wait_ge(p.done + w.b, w.need, abort_flag, p.wait_limit_ns);
+                bulk_wait_read_all();                                        // the stores of the tile before have left the blocks
+                if (addend && ok) {
+                    const int now = w.mode == POLY ? min(blocks_here, 2) : blocks_here;
+                    mbar_arrive_expect_tx(abar, now * BLOCK_BYTES);
+                    for (int n = 0; n < now; ++n) load_block(n);
+                }
             }
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+            if (!ok) break;
+            if (addend && !await_addend()) break;
             ok = mbar_wait(tfull_bar(ab), (it >> 1) & 1u, abort_flag, p.wait_limit_ns);
             if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
-            const uint32_t tmem_row = tmem_base + ab * TN + (static_cast<uint32_t>(quad * 32) << 16);
-            for (int c = half; c < TN / 32; c += 2) {
-                const int col0 = w.j * TN + c * 32;
-                if (row0 >= p.R || col0 >= ncols) break;                     // uniform in the warp
-                float v[32];
-                __syncwarp();
-                tmem_ld32(tmem_row + c * 32, v);
-                uint4 next[4];
-                if (w.mode != GRAM && c + 2 < TN / 32) load_addend(p, w, row0 + lane, col0 + 64, next);
-                tmem_ld_wait();
-                epilogue_block(p, w, row0, col0, lane, v, add, stage);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) add[q] = next[q];
+            const uint32_t tmem_row = tmem_base + ab * TN + (static_cast<uint32_t>(quad * 32) << 16) + half * 32;
+            for (int n = 0; n < blocks_here; ++n) {
+                const int col0 = col_first + 64 * n;
+                if (w.last) {
+                    if (p.transposed) epilogue_last<true>(p, w, row0, col0, lane, tmem_row + 64 * n, place(n));
+                    else epilogue_last<false>(p, w, row0, col0, lane, tmem_row + 64 * n, place(n));
+                } else {
+                    float v[32];
+                    __syncwarp();
+                    tmem_ld32(tmem_row + 64 * n, v);
+                    if (w.mode == POLY) {
+                        if (n >= 2 && !await_addend()) { ok = 0; break; }
+                        if (n >= 1 && lane == 0) {
+                            bulk_wait_read_all();                            // block n - 1 has left its places:
+                            if (n + 1 < blocks_here) {                       // the addend of block n + 1 may come
+                                mbar_arrive_expect_tx(abar, BLOCK_BYTES);
+                                load_block(n + 1);
+                            }
+                        }
+                    } else if (w.mode == GRAM && n >= 2 && lane == 0) {
+                        bulk_wait_read_1();                                  // block n - 2 has left its places
+                    }
+                    __syncwarp();
+                    tmem_ld_wait();
+                    epilogue_block(p, maps, w, row0, col0, lane, v, place(n), blocks + (2 + (n & 1)) * BLOCK_BYTES);
+                }
             }
+            if (!ok) break;
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(mapa_shared(tempty_bar(ab), 0));
-            if (!w.last) warp_signal(p.done + w.b, lane);
+            if (!w.last && lane == 0) signal_stored(p.done + w.b);
         }
+        if (lane == 0) bulk_wait_all();                                      // nothing reads this CTA's shared memory any more
     }
 
     tc_fence_before();
