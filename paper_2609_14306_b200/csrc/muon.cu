@@ -41,7 +41,7 @@ bool layout(int64_t batch, int64_t rows, int64_t cols, Layout* L) {
     L->R = std::min(rows, cols); L->C = std::max(rows, cols);
     if (batch > 65535 || L->C > (1 << 22) || L->R > (1 << 17)) return false;
     L->lda = up64(L->R); L->ldx = up64(L->C);
-    const int64_t row_tiles = (L->R + 127) / 128, col_tiles = (L->C + 127) / 128;
+    const int64_t row_tiles = (L->R + TM - 1) / TM, col_tiles = (L->C + 63) / 64;
     if (batch * row_tiles * col_tiles > (int64_t{1} << 20)) return false;   // work-list positions and counts fit 31 bits
     L->parts = std::max<int64_t>(1, std::min<int64_t>(MAX_PARTS, (rows * cols + 16 * PREP_THREADS - 1) / (16 * PREP_THREADS)));
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
@@ -127,11 +127,10 @@ bool encode(CUtensorMap* map, void* ptr, int rank, const cuuint64_t* dims, const
                       box[0] == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // [batch][rows][ld] fp16, ld a multiple of 64; see Maps.
-bool map_operand(CUtensorMap* map, __half* ptr, int64_t batch, int64_t rows, int64_t ld, cuuint32_t box_rows, cuuint32_t box_chunks,
-                 cuuint32_t box_elems = 64) {
+bool map_operand(CUtensorMap* map, __half* ptr, int64_t batch, int64_t rows, int64_t ld, int box_rows, int box_chunks, int box_elems) {
     const cuuint64_t dims[4] = {64, static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(ld / 64), static_cast<cuuint64_t>(batch)};
     const cuuint64_t strides[3] = {static_cast<cuuint64_t>(2 * ld), 128, static_cast<cuuint64_t>(2 * ld * rows)};
-    const cuuint32_t box[4] = {box_elems, box_rows, box_chunks, 1};
+    const cuuint32_t box[4] = {static_cast<cuuint32_t>(box_elems), static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(box_chunks), 1};
     return encode(map, ptr, 4, dims, strides, box);
 }
 
@@ -158,9 +157,19 @@ cudaError_t ensure_smem() {
 }
 
 // Tiles of one matrix in a product.
-int tiles_of(int mode, int64_t R, int64_t C) {
-    const int64_t mt = (R + TM - 1) / TM;
-    return static_cast<int>(mode == APPLY ? mt * ((C + TN - 1) / TN) : mt * (mt + 1) / 2);
+int64_t tiles_of(int mode, int64_t R, int64_t C, int bn) {
+    const int64_t mt = (R + TM - 1) / TM, nj = ((mode == APPLY ? C : R) + bn - 1) / bn;
+    return mode == APPLY ? mt * nj : mt * nj - (TM / bn) * (mt * (mt - 1) / 2);
+}
+
+// Tile width of a product.  The tensor cores take as long for a 256 x 64 or 256 x 128 step as for 256 x 256 (the left operand's
+// 128 rows per SM bound it: 494 against 530 cycles per 64 of K), so narrow tiles only pay when they find idle SMs: they then
+// cut the tile's epilogue.  Hence the narrowest width whose tiles all run at once, else 256.
+// APPLY's right operand comes in chunks of 64 columns per CTA, so 128 is its least.
+int pick_bn(int mode, int64_t batch, int64_t R, int64_t C, int pairs) {
+    for (int bn = mode == APPLY ? 128 : 64; bn < TN; bn *= 2)
+        if (batch * tiles_of(mode, R, C, bn) <= pairs) return bn;
+    return TN;
 }
 
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -207,11 +216,21 @@ int run(const void* g, int g_dtype, float* m, float mu, int nesterov, int64_t ba
     q.status = reinterpret_cast<int*>(base); q.next = q.status + 16; q.done = reinterpret_cast<int*>(base + L.done);
     q.wait_limit_ns = static_cast<unsigned long long>(vp_ce_set_wait_limit_ns(0));
     Maps maps;
-    bool ok = map_operand(&maps.a, q.A, batch, L.R, L.lda, 128, 1) && map_operand(&maps.b, q.B, batch, L.R, L.lda, 128, 1) &&
-              map_operand(&maps.a_blk, q.A, batch, L.R, L.lda, 32, 1, 32) && map_operand(&maps.b_blk, q.B, batch, L.R, L.lda, 32, 1, 32);
+    const int pairs = sm_count() / 2;
+    int64_t most = 0;
+    for (int mode = 0; mode < 3; ++mode) {
+        q.bn[mode] = pick_bn(mode, batch, L.R, L.C, pairs);
+        q.tiles[mode] = static_cast<int>(tiles_of(mode, L.R, L.C, q.bn[mode]));
+        most = std::max(most, std::min<int64_t>(pairs, batch * q.tiles[mode]));
+    }
+    auto map = [&](CUtensorMap* m, __half* ptr, int64_t ld, int box_rows, int box_chunks, int box_elems = 64) {
+        return map_operand(m, ptr, batch, L.R, ld, box_rows, box_chunks, box_elems);
+    };
+    bool ok = map(&maps.a_l, q.A, L.lda, 128, 1) && map(&maps.a_r, q.A, L.lda, q.bn[POLY] / 2, 1) && map(&maps.b_l, q.B, L.lda, 128, 1) &&
+              map(&maps.a_blk, q.A, L.lda, 32, 1, 32) && map(&maps.b_blk, q.B, L.lda, 32, 1, 32);
     for (int i = 0; i < 2; ++i)
-        ok = ok && map_operand(&maps.x_k[i], q.X[i], batch, L.R, L.ldx, 128, 1) && map_operand(&maps.x_mn[i], q.X[i], batch, L.R, L.ldx, 64, 2) &&
-             map_operand(&maps.x_blk[i], q.X[i], batch, L.R, L.ldx, 32, 1, 32);
+        ok = ok && map(&maps.x_l[i], q.X[i], L.ldx, 128, 1) && map(&maps.x_r[i], q.X[i], L.ldx, q.bn[GRAM] / 2, 1) &&
+             map(&maps.x_mn[i], q.X[i], L.ldx, 64, q.bn[APPLY] / 128) && map(&maps.x_blk[i], q.X[i], L.ldx, 32, 1, 32);
     if (!ok || ensure_smem() != cudaSuccess) return VPCE_CUDA_ERROR;
 
     PrepParams pp{};
@@ -226,16 +245,10 @@ int run(const void* g, int g_dtype, float* m, float mu, int nesterov, int64_t ba
     else if (g_dtype == VPCE_F16) launch_prep<__half>(pp, four, st);
     else launch_prep<__nv_bfloat16>(pp, four, st);
 
-    const int pairs = sm_count() / 2;
-    int most = 0;
-    for (int mode = 0; mode < 3; ++mode) {
-        q.tiles[mode] = tiles_of(mode, L.R, L.C);
-        most = std::max<int64_t>(most, std::min<int64_t>(pairs, batch * q.tiles[mode]));
-    }
     q.steps = steps;
     std::copy(plan.alpha, plan.alpha + 3 * steps, q.alpha);
     std::copy(plan.beta, plan.beta + 3 * steps, q.beta);
-    muon_products_kernel<<<2 * most, GEMM_THREADS, GEMM_SMEM, st>>>(maps, q);
+    muon_products_kernel<<<2 * static_cast<unsigned>(most), GEMM_THREADS, GEMM_SMEM, st>>>(maps, q);
     return cudaGetLastError() == cudaSuccess ? VPCE_OK : VPCE_CUDA_ERROR;
 }
 

@@ -12,7 +12,7 @@ namespace vpmuon {
 
 using namespace vpce;
 
-constexpr int TM = 256, TN = 256;           // a tile: one CTA pair, 128 rows and 128 columns' worth of operands per CTA
+constexpr int TM = 256, TN = 256;           // a tile: one CTA pair, 128 rows and bn / 2 columns' worth of operands per CTA; bn <= TN
 constexpr int KB = 64;                      // K per pipeline stage: one 128-byte swizzle row of fp16
 constexpr int A_BYTES = 128 * 128;          // 128 rows of the left operand
 constexpr int STAGE_BYTES = 2 * A_BYTES;
@@ -33,17 +33,18 @@ constexpr int MAX_PARTS = 512;              // partial sums of squares per matri
 enum Mode { GRAM = 0, POLY = 1, APPLY = 2 };
 
 // Operands as 4-D arrays {64 elements, rows, 64-element chunks of a row, batch}.  Along the rows (K = columns) a stage takes one
-// box of 128 rows x 1 chunk, down the columns (X as right operand of B X, K = rows) one of 64 rows x 2 chunks.  The chunk as a
+// box of 128 rows x 1 chunk (left operand) or bn / 2 rows x 1 chunk (right, *_r), down the columns (X as right operand of B X,
+// K = rows) one of 64 rows x bn / 128 chunks.  The chunk as a
 // dimension of its own matters: boxes at column offsets of a 3-D array {columns, rows, batch} arrived at 48 bytes a cycle and
 // SM, these at 70 (loads alone, 128-row boxes; the products need 64).
 // The epilogue moves boxes of 32 rows x 32 elements of the same arrays (*_blk).
-struct Maps { CUtensorMap x_k[2], x_mn[2], a, b, x_blk[2], a_blk, b_blk; };
+struct Maps { CUtensorMap x_l[2], x_r[2], x_mn[2], a_l, a_r, b_l, x_blk[2], a_blk, b_blk; };
 
 struct GemmParams {
     int batch, R, C;                        // matrices R x C with R <= C
     int lda, ldx;                           // row pitches (elements, multiples of 64; columns beyond R / C hold zeros)
     int steps;
-    int tiles[3];                           // per mode: tiles of one matrix
+    int bn[3], tiles[3];                    // per mode: tile width (256, 128, 64), tiles of one matrix
     float alpha[3 * MAX_STEPS], beta[3 * MAX_STEPS];   // stored result = alpha acc + beta addend (stored units)
     __half *X[2], *A, *B;
     // last product: what becomes of X
@@ -268,13 +269,13 @@ __global__ void __launch_bounds__(PREP_THREADS) muon_start_tall_kernel(const Pre
 // ------------------------------------------------------------------------------------ the products
 // Entry of the work list: the tiles of every product of every matrix, product by product, inside a product matrix by matrix.
 struct Tile {
-    int k, mode, b, i, j;                   // product number 3 step + mode, matrix, row tile, column tile
-    int need;                           // need: value of done[b] from which on this product's inputs are complete
+    int k, mode, b, i, j;                   // product number 3 step + mode, matrix, row tile, column tile (bn wide)
+    int bn, need;                         // need: value of done[b] from which on this product's inputs are complete
     bool last;
 };
 
-// GRAM and POLY are symmetric: only the tiles on the diagonal and right of it are listed (the others are written as mirror
-// images).
+// GRAM and POLY are symmetric: only the tiles that reach the diagonal or lie right of it are listed (the others are written as
+// mirror images).  A row of tiles i starts at column tile i * 256 / bn.
 __device__ __forceinline__ Tile decode(const GemmParams& p, int e) {
     Tile w;
     const int per_step = p.tiles[0] + p.tiles[1] + p.tiles[2];
@@ -288,17 +289,21 @@ __device__ __forceinline__ Tile decode(const GemmParams& p, int e) {
     w.need = before * 2 * EPI_WARPS;
     w.b = r / p.tiles[w.mode];
     r -= w.b * p.tiles[w.mode];
-    const int nj = ((w.mode == APPLY ? p.C : p.R) + TN - 1) / TN;
+    w.bn = p.bn[w.mode];
+    const int nj = ((w.mode == APPLY ? p.C : p.R) + w.bn - 1) / w.bn, f = TM / w.bn;
     if (w.mode == APPLY) {
         w.i = r / nj;
         w.j = r - w.i * nj;
     } else {
         w.i = 0;
-        while (r >= nj - w.i) { r -= nj - w.i; ++w.i; }
-        w.j = w.i + r;
+        while (r >= nj - w.i * f) { r -= nj - w.i * f; ++w.i; }
+        w.j = w.i * f + r;
     }
     return w;
 }
+
+// Whether the tile that holds element (row, col) is listed in a symmetric product with tiles bn wide.
+__device__ __forceinline__ bool listed(int bn, int row, int col) { return (col / bn + 1) * bn > (row / TM) * TM; }
 
 // Adds to a counter once this lane's TMA stores have been performed, for whoever loads the written data after seeing the new
 // value (the fences order the copies of the async proxy and the counter on both sides).
@@ -328,7 +333,7 @@ __device__ __forceinline__ void epilogue_block(const GemmParams& p, const Maps& 
         h[q] = pack8(f);
         st_shared_v4(blk + block_at(lane, q), h[q]);
     }
-    const bool mirror = w.mode != APPLY && w.j > w.i && col0 < p.R;
+    const bool mirror = w.mode != APPLY && col0 < p.R && !listed(w.bn, col0, row0);
     if (mirror) {
         const uint16_t* hv = reinterpret_cast<const uint16_t*>(h);
 #pragma unroll
@@ -411,7 +416,7 @@ __device__ __forceinline__ void epilogue_last(const GemmParams& p, const Tile& w
     }
 }
 
-// All products of all matrices in one launch, on CTA pairs (tcgen05 cta_group::2, 256 x 256 tiles, fp32 accumulators in tensor
+// All products of all matrices in one launch, on CTA pairs (tcgen05 cta_group::2, 256 x bn tiles, fp32 accumulators in tensor
 // memory, two of them so that a tile's epilogue overlaps the next tile's products).
 //
 // Pairs take the entries of the work list in order from a counter.  An entry whose inputs other pairs are still writing waits
@@ -503,13 +508,13 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
                 const Tile w = decode(p, t);
                 if (w.k > 0 && !flag_wait_ge(p.done + w.b, w.need, abort_flag, p.wait_limit_ns)) { ok = false; break; }
                 const int xb = (w.k / 3) & 1;
-                const CUtensorMap* ma = w.mode == GRAM ? &maps.x_k[xb] : w.mode == POLY ? &maps.a : &maps.b;
-                const CUtensorMap* mb = w.mode == GRAM ? &maps.x_k[xb] : w.mode == POLY ? &maps.a : &maps.x_mn[xb];
+                const CUtensorMap* ma = w.mode == GRAM ? &maps.x_l[xb] : w.mode == POLY ? &maps.a_l : &maps.b_l;
+                const CUtensorMap* mb = w.mode == GRAM ? &maps.x_r[xb] : w.mode == POLY ? &maps.a_r : &maps.x_mn[xb];
                 const int num_kb = steps_of_k(p, w);
-                const int arow = w.i * TM + static_cast<int>(rank) * 128, bcol = w.j * TN + static_cast<int>(rank) * 128;
+                const int arow = w.i * TM + static_cast<int>(rank) * 128, bcol = w.j * w.bn + static_cast<int>(rank) * (w.bn / 2);
                 for (int kb = 0; kb < num_kb; ++kb) {
                     if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, p.wait_limit_ns)) { ok = false; break; }
-                    if (leader) mbar_arrive_expect_tx(full_bar(stage), 2 * STAGE_BYTES);
+                    if (leader) mbar_arrive_expect_tx(full_bar(stage), 2 * (A_BYTES + w.bn / 2 * 128));
                     const uint32_t bar = mapa_shared(full_bar(stage), 0);
                     const uint32_t sa = base + stage * STAGE_BYTES;
                     // rows and chunks beyond the matrix arrive as zeros
@@ -544,7 +549,7 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
                 if (t < 0) break;
                 const Tile w = decode(p, t);
                 const bool apply = w.mode == APPLY;
-                const uint32_t idesc = make_idesc(TN, false, apply, TM, 0u);       // fp16 operands
+                const uint32_t idesc = make_idesc(w.bn, false, apply, TM, 0u);     // fp16 operands
                 const int num_kb = steps_of_k(p, w);
                 const int ab = it & 1;
                 if (!mbar_wait_cluster(tempty_bar(ab), ((it >> 1) & 1u) ^ 1u, abort_flag, p.wait_limit_ns)) { ok = false; break; }
@@ -596,15 +601,15 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
             const int ab = it & 1;
             const int row0 = w.i * TM + static_cast<int>(rank) * 128 + quad * 32;
             const int ncols = w.mode == APPLY ? p.ldx : p.lda;
-            // blocks of this warp: columns w.j * TN + 64 n + 32 half
-            const int col_first = w.j * TN + half * 32;
+            // blocks of this warp: columns w.j * bn + 64 n + 32 half
+            const int col_first = w.j * w.bn + half * 32;
             int blocks_here = row0 < p.R && col_first < ncols ? (ncols - col_first + 63) / 64 : 0;
-            if (blocks_here > WARP_BLOCKS) blocks_here = WARP_BLOCKS;
+            if (blocks_here > w.bn / 64) blocks_here = w.bn / 64;
             // the addends of all its blocks arrive while the products run
             const bool addend = w.mode != GRAM && blocks_here > 0;
             const CUtensorMap* from = w.mode == POLY ? &maps.a_blk : &maps.x_blk[(w.k / 3) & 1];
             auto place = [&](int n) { return blocks + (w.mode == APPLY ? n : n & 1) * BLOCK_BYTES; };
-            auto load_block = [&](int n) { tma_load_4d(place(n), from, abar, half * 32, row0, w.j * (TN / 64) + n, w.b); };
+            auto load_block = [&](int n) { tma_load_4d(place(n), from, abar, half * 32, row0, w.j * (w.bn / 64) + n, w.b); };
             auto await_addend = [&]() {
                 const bool got = mbar_wait(abar, aphase, abort_flag, p.wait_limit_ns);
                 aphase ^= 1u;
