@@ -1,16 +1,29 @@
 // Layer normalisation, forward and backward (layer_norm.h).
 //
-// Generic kernels: one block per row (grid-stride), elements read one at a time in the order of the threads, three passes
-// over a row that the caches hold after the first.  They take any width, stride and alignment.
+// Row kernels (d <= 16384): a group of 1 to 16 warps owns a row at a time, 8 to 32 elements a thread.  Rows arrive by bulk
+// copies into a ring in shared memory, several rows ahead: what is in flight does not depend on registers or on how many warps
+// wait at a reduction.  A thread owns the same columns in every row, so it keeps their weights in registers, and in the backward
+// pass it sums dy xh and dy of its columns in registers over all rows of its group: the weight's gradient costs no second pass
+// over the data, only one partial sum per block.  The variance is taken from the centred values in registers.  At 16-bit types
+// the arithmetic is as scarce as the memory (2 to 3 passes over every element): it runs on pairs (fp32x2 instructions).
+//   VEC      every row starts on a 16-byte boundary: 16-byte accesses
+//   !VEC     any alignment: the copies take the 16-byte granules that a row touches (cut at the tensor's ends, whose few
+//            elements are copied one by one), threads read single elements at the row's offset, neighbours side by side
+//
+// Generic kernels (wider rows): one block per row, elements read one at a time in the order of the threads, three passes over
+// a row that the caches hold after the first.
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
+#include <atomic>
 #include <cstdint>
 #include <type_traits>
 
 #include "layer_norm.h"
+#include "sm100_ptx.cuh"
 #include "vp_ce.h"
 
 namespace {
@@ -26,7 +39,7 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float
 constexpr int GEN_THREADS = 256;
 constexpr int COL_TILE = 32;            // columns per block of the column sums
 constexpr int COL_ROWS = 8;             // rows that a block of the column sums takes at a time
-constexpr int MAX_SLICES = 296;         // row slices of the column sums: two blocks per SM of a 148-SM device
+constexpr int MAX_SLICES = 444;         // partial sums over rows: three blocks per SM of a 148-SM device
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -48,6 +61,410 @@ __device__ __forceinline__ float2 block_sum2(float a, float b, float2* part) {
     return s;
 }
 
+// ------------------------------------------------------------------------------------ row kernels
+constexpr int MAX_GROUP_WARPS = 16;
+constexpr int MAX_GROUPS = 14;                          // per block; a group of more than one warp has a named barrier
+template <int EPT> constexpr int FORWARD_REGS = EPT <= 16 ? 72 : 128;
+template <int EPT> constexpr int BACKWARD_REGS = EPT <= 16 ? 96 : 128;
+constexpr int MAX_EPT = 32;                             // elements per thread
+constexpr int MAX_SMEM = 227 * 1024;
+constexpr int64_t MAX_ROW = 32 * MAX_GROUP_WARPS * MAX_EPT;
+
+struct RowArgs {
+    const void *x, *dy;                                 // dy: backward only
+    long rows, x_stride, dy_stride, out_stride;
+    int d, warps;                                       // warps per group
+    int groups, stages, cap;                            // groups per block, ring depth, bytes of a row in the ring
+    const void *g, *b;
+    float eps;
+    void* out;                                          // y or dx (may be null in the backward pass)
+    float *mean, *rstd;                                 // written (forward, may be null) or read (backward)
+    float* partial;                                     // [blocks][2][d] or null
+};
+
+struct Smem {                                           // of a block: barriers, reduction scratch, ring
+    uint64_t full[MAX_GROUPS][8];                       // [group][stage]
+    float2 part[MAX_GROUPS][2][MAX_GROUP_WARPS];        // [group][pass][warp]
+};
+constexpr int RING_OFFSET = (sizeof(Smem) + 127) / 128 * 128;
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+// Bytes by which row `r` starts behind a 16-byte boundary.
+template <typename T> __device__ __forceinline__ int row_shift(const void* base, long r, long stride) {
+    return static_cast<int>((reinterpret_cast<uintptr_t>(base) + static_cast<size_t>(r) * stride * sizeof(T)) & 15u);
+}
+
+// Starts the copy of row r into `dst` (its first element lands row_shift bytes behind dst); returns the bytes that will be
+// counted on the barrier.  Granules that reach over the tensor's first or last byte are left to plain element copies.
+template <typename T, bool VEC>
+__device__ __forceinline__ uint32_t copy_extent(const void* base, long r, long rows, long stride, int d, const char** from, uint32_t* at,
+                                                uint8_t* dst_generic) {
+    const char* row = static_cast<const char*>(base) + static_cast<size_t>(r) * stride * sizeof(T);
+    const size_t bytes = static_cast<size_t>(d) * sizeof(T);
+    if (VEC) { *from = row; *at = 0; return static_cast<uint32_t>(bytes); }
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(row), hi = lo + bytes;
+    uintptr_t a = lo & ~static_cast<uintptr_t>(15), e = (hi + 15) & ~static_cast<uintptr_t>(15);
+    const uintptr_t origin = a;
+    if (r == 0 && a < lo) a += 16;                      // before the tensor's first element
+    if (r == rows - 1 && e > hi) e -= 16;               // behind its last
+    if (e < a) e = a;
+    if (a > lo || e < hi) {                             // the first or last row's ragged ends, or a row inside one granule
+        const T* src = reinterpret_cast<const T*>(lo);
+        T* dst = reinterpret_cast<T*>(dst_generic + (lo - origin));
+        for (int c = 0; c < d && lo + c * sizeof(T) < a; ++c) dst[c] = src[c];
+        for (int c = d - 1; c >= 0 && lo + c * sizeof(T) >= e; --c) dst[c] = src[c];
+    }
+    *from = reinterpret_cast<const char*>(a);
+    *at = static_cast<uint32_t>(a - origin);
+    return static_cast<uint32_t>(e - a);
+}
+
+// One thread: row r of the NA arrays into ring slot `slot` (generic address), signalled on `bar`.
+template <typename T, bool VEC, int NA>
+__device__ __forceinline__ void fetch_row(const RowArgs& a, long r, uint8_t* slot, uint32_t bar) {
+    const char* from[2];
+    uint32_t at[2], bytes[2] = {0, 0};
+    bytes[0] = copy_extent<T, VEC>(a.x, r, a.rows, a.x_stride, a.d, &from[0], &at[0], slot);
+    if (NA == 2) bytes[1] = copy_extent<T, VEC>(a.dy, r, a.rows, a.dy_stride, a.d, &from[1], &at[1], slot + a.cap);
+    vpce::mbar_arrive_expect_tx(bar, bytes[0] + bytes[1]);
+    const uint32_t dst = vpce::smem_u32(slot);
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+        if (bytes[i]) bulk_load(dst + i * a.cap + at[i], from[i], bytes[i], bar);
+}
+
+// All waits are for bulk copies of this block's own and end; the limit is that of a copy that never lands (a bad pointer).
+__device__ __forceinline__ void wait_row(uint32_t bar, uint32_t parity) {
+    for (int i = 0; i < (1 << 26); ++i)
+        if (vpce::mbar_try_wait(bar, parity)) return;
+}
+
+__device__ __forceinline__ void group_sync(int group, int warps) {
+    if (warps == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(warps * 32) : "memory");
+}
+
+// Sums of two values over the group; `part` is that of one pass (the passes of a row take turns).
+__device__ __forceinline__ float2 group_sum2(float a, float b, float2* part, int group, int warps, int warp, int lane) {
+    a = warp_sum(a);
+    b = warp_sum(b);
+    if (warps == 1) return make_float2(a, b);
+    if (lane == 0) part[warp] = make_float2(a, b);
+    group_sync(group, warps);
+    float2 s = part[0];
+    for (int i = 1; i < warps; ++i) { const float2 t = part[i]; s.x += t.x; s.y += t.y; }
+    return s;
+}
+
+// Pairs of fp32 in one 64-bit register.
+using f2 = unsigned long long;
+__device__ __forceinline__ f2 pair(float a, float b) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float2 split(f2 v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
+__device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+
+template <typename T> __device__ __forceinline__ f2 widen(uint32_t w);      // two 16-bit elements of a word
+template <> __device__ __forceinline__ f2 widen<__nv_bfloat16>(uint32_t w) { return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+template <> __device__ __forceinline__ f2 widen<__half>(uint32_t w) {
+    const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    return pair(t.x, t.y);
+}
+template <typename T> __device__ __forceinline__ uint32_t narrow(float a, float b);
+template <> __device__ __forceinline__ uint32_t narrow<__nv_bfloat16>(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <> __device__ __forceinline__ uint32_t narrow<__half>(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// A thread's EPT columns: a warp owns 32 EPT neighbouring columns, in pieces of 32 N: lane l has N neighbours of each (N = 16 /
+// sizeof(T) where VEC, else 1).  Piece k begins at column first + 32 N k; pairs are neighbours in the thread's order.
+template <typename T, bool VEC, int EPT> struct Columns {
+    static constexpr int N = VEC ? 16 / static_cast<int>(sizeof(T)) : 1;
+    static constexpr int PIECES = EPT / N, PAIRS = EPT / 2, STEP = 32 * N, PART = 8 / N;
+    int first, d;
+    __device__ __forceinline__ Columns(int warp, int lane, int d_) : first(warp * 32 * EPT + lane * N), d(d_) {}
+    __device__ __forceinline__ bool has(int k) const { return first + STEP * k < d; }    // VEC: d is a multiple of N
+
+    // Eight of the thread's elements (part q of EPT / 8) of a row in shared memory (address of its first element); columns beyond
+    // d read as 0.
+    __device__ __forceinline__ void read(uint32_t row, int q, f2* v) const {
+        const uint32_t at = row + (first + STEP * q * PART) * static_cast<int>(sizeof(T));
+        if constexpr (VEC) {
+#pragma unroll
+            for (int k = 0; k < PART; ++k) {
+                uint32_t w[4] = {0u, 0u, 0u, 0u};
+                if (has(q * PART + k)) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at + k * 512));
+                if constexpr (sizeof(T) == 4) {
+                    v[2 * k] = pair(__uint_as_float(w[0]), __uint_as_float(w[1]));
+                    v[2 * k + 1] = pair(__uint_as_float(w[2]), __uint_as_float(w[3]));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[4 * k + i] = widen<T>(w[i]);
+                }
+            }
+        } else if constexpr (sizeof(T) == 4) {
+            float f[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                f[k] = 0.f;
+                if (has(q * PART + k)) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f[k]) : "r"(at + k * 128));
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = pair(f[2 * i], f[2 * i + 1]);
+        } else {
+            uint16_t h[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                h[k] = 0;
+                if (has(q * PART + k)) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h[k]) : "r"(at + k * 64));
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = widen<T>(static_cast<uint32_t>(h[2 * i]) | static_cast<uint32_t>(h[2 * i + 1]) << 16);
+        }
+    }
+
+    // Their weights (W of any alignment), `none` where p is null; columns beyond d as 0.
+    template <typename W> __device__ __forceinline__ void weights(const W* p, float none, f2* v) const {
+        float f[EPT];
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+            for (int j = 0; j < N; ++j) f[k * N + j] = has(k) ? (p ? to_f(p[first + STEP * k + j]) : none) : 0.f;
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) v[i] = pair(f[2 * i], f[2 * i + 1]);
+    }
+
+    __device__ __forceinline__ void store(T* row, int q, const f2* v) const {
+        T* at = row + first + STEP * q * PART;
+        if constexpr (VEC) {
+#pragma unroll
+            for (int k = 0; k < PART; ++k) {
+                uint32_t w[4];
+                if constexpr (sizeof(T) == 4) {
+                    const float2 a = split(v[2 * k]), b = split(v[2 * k + 1]);
+                    w[0] = __float_as_uint(a.x); w[1] = __float_as_uint(a.y); w[2] = __float_as_uint(b.x); w[3] = __float_as_uint(b.y);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { const float2 a = split(v[4 * k + i]); w[i] = narrow<T>(a.x, a.y); }
+                }
+                if (has(q * PART + k)) *reinterpret_cast<uint4*>(at + STEP * k) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 a = split(v[i]);
+                if (has(q * PART + 2 * i)) at[STEP * (2 * i)] = from_f<T>(a.x);
+                if (has(q * PART + 2 * i + 1)) at[STEP * (2 * i + 1)] = from_f<T>(a.y);
+            }
+        }
+    }
+};
+
+// What every row kernel sets up: the group's place and its ring.
+struct Group {
+    int id, warp, lane;
+    bool leads;                                         // this thread issues the group's copies
+    long first, step;                                   // rows of this group: first, first + step, ...
+    uint8_t* ring;
+    uint32_t bars;
+};
+template <typename T, bool VEC, int NA>
+__device__ __forceinline__ Group group_setup(const RowArgs& a, uint8_t* raw) {
+    Smem* sm = reinterpret_cast<Smem*>(raw);
+    Group g;
+    g.id = (threadIdx.x >> 5) / a.warps;
+    g.warp = (threadIdx.x >> 5) - g.id * a.warps;
+    g.lane = threadIdx.x & 31;
+    g.leads = g.warp == 0 && g.lane == 0;
+    g.first = static_cast<long>(blockIdx.x) * a.groups + g.id;
+    g.step = static_cast<long>(gridDim.x) * a.groups;
+    g.ring = raw + RING_OFFSET + static_cast<size_t>(g.id) * a.stages * NA * a.cap;
+    g.bars = vpce::smem_u32(&sm->full[g.id][0]);
+    if (g.leads) {
+        for (int s = 0; s < a.stages; ++s) vpce::mbar_init(g.bars + 8 * s, 1);
+        vpce::fence_barrier_init();
+        vpce::fence_proxy_async();
+    }
+    group_sync(g.id, a.warps);
+    if (g.leads)
+        for (int s = 0; s < a.stages; ++s) {
+            const long r = g.first + s * g.step;
+            if (r < a.rows) fetch_row<T, VEC, NA>(a, r, g.ring + static_cast<size_t>(s) * NA * a.cap, g.bars + 8 * s);
+        }
+    return g;
+}
+
+template <typename T, typename W, bool VEC, int EPT>
+__global__ void __maxnreg__(FORWARD_REGS<EPT>) ln_forward_rows(const RowArgs a) {
+    extern __shared__ __align__(128) uint8_t raw[];
+    const Group g = group_setup<T, VEC, 1>(a, raw);
+    const Columns<T, VEC, EPT> cols(g.warp, g.lane, a.d);
+    using C = Columns<T, VEC, EPT>;
+    float2(*part)[MAX_GROUP_WARPS] = reinterpret_cast<Smem*>(raw)->part[g.id];
+    const float inv_d = 1.f / static_cast<float>(a.d);
+    f2 gw[C::PAIRS], bw[C::PAIRS];
+    cols.weights(static_cast<const W*>(a.g), 1.f, gw);
+    cols.weights(static_cast<const W*>(a.b), 0.f, bw);
+    int s = 0;
+    uint32_t parity = 0;
+    for (long r = g.first; r < a.rows; r += g.step) {
+        uint8_t* slot = g.ring + static_cast<size_t>(s) * a.cap;
+        wait_row(g.bars + 8 * s, parity);
+        f2 v[C::PAIRS];
+        const uint32_t xr = vpce::smem_u32(slot) + (VEC ? 0 : row_shift<T>(a.x, r, a.x_stride));
+#pragma unroll
+        for (int q = 0; q < EPT / 8; ++q) cols.read(xr, q, v + 4 * q);
+        f2 s0 = v[0], s1 = v[1];
+#pragma unroll
+        for (int i = 2; i < C::PAIRS; i += 2) { s0 = add2(s0, v[i]); s1 = add2(s1, v[i + 1]); }
+        const float2 sum = split(add2(s0, s1));
+        const float mu = group_sum2(sum.x + sum.y, 0.f, part[0], g.id, a.warps, g.warp, g.lane).x * inv_d;
+        // everyone has read the slot
+        if (g.leads && r + a.stages * g.step < a.rows) fetch_row<T, VEC, 1>(a, r + a.stages * g.step, slot, g.bars + 8 * s);
+        if (++s == a.stages) { s = 0; parity ^= 1u; }
+        const f2 minus_mu = pair(-mu, -mu);
+#pragma unroll
+        for (int i = 0; i < C::PAIRS; ++i) {
+            v[i] = add2(v[i], minus_mu);
+            // columns beyond d count nothing
+            if constexpr (VEC) {
+                if (!cols.has(i * 2 / C::N)) v[i] = 0ull;
+            } else {
+                if (!cols.has(2 * i + 1)) { const float2 t = split(v[i]); v[i] = pair(cols.has(2 * i) ? t.x : 0.f, 0.f); }
+            }
+        }
+        f2 q0 = mul2(v[0], v[0]), q1 = mul2(v[1], v[1]);
+#pragma unroll
+        for (int i = 2; i < C::PAIRS; i += 2) { q0 = fma2(v[i], v[i], q0); q1 = fma2(v[i + 1], v[i + 1], q1); }
+        const float2 sq = split(add2(q0, q1));
+        const float rs = 1.f / sqrtf(group_sum2(sq.x + sq.y, 0.f, part[1], g.id, a.warps, g.warp, g.lane).x * inv_d + a.eps);
+        const f2 rs2 = pair(rs, rs);
+#pragma unroll
+        for (int i = 0; i < C::PAIRS; ++i) v[i] = fma2(mul2(v[i], rs2), gw[i], bw[i]);
+#pragma unroll
+        for (int q = 0; q < EPT / 8; ++q) cols.store(static_cast<T*>(a.out) + r * a.out_stride, q, v + 4 * q);
+        if (g.leads) {
+            if (a.mean) a.mean[r] = mu;
+            if (a.rstd) a.rstd[r] = rs;
+        }
+    }
+}
+
+template <typename T, typename W, bool VEC, int EPT>
+__global__ void __maxnreg__(BACKWARD_REGS<EPT>) ln_backward_rows(const RowArgs a) {
+    extern __shared__ __align__(128) uint8_t raw[];
+    const Group g = group_setup<T, VEC, 2>(a, raw);
+    const Columns<T, VEC, EPT> cols(g.warp, g.lane, a.d);
+    using C = Columns<T, VEC, EPT>;
+    float2(*part)[MAX_GROUP_WARPS] = reinterpret_cast<Smem*>(raw)->part[g.id];
+    const float inv_d = 1.f / static_cast<float>(a.d);
+    f2 gw[C::PAIRS], dg[C::PAIRS], db[C::PAIRS];
+    cols.weights(static_cast<const W*>(a.g), 1.f, gw);
+#pragma unroll
+    for (int i = 0; i < C::PAIRS; ++i) dg[i] = db[i] = 0ull;
+    // The row is read from the ring twice, before and after the group's sums: the registers that would keep it hold the column
+    // sums.  Weights of columns beyond d are 0, so those columns add nothing to the sums.  The first reading of a row comes
+    // before the second reading of the row before it, so the group's barrier finds everyone with work in between.
+    auto slot_of = [&](int s) { return g.ring + static_cast<size_t>(s) * 2 * a.cap; };
+    auto first_reading = [&](long r, int s, uint32_t parity, float mu, float rs, float2* to) {
+        const uint32_t slot = vpce::smem_u32(slot_of(s));
+        const uint32_t xr = slot + (VEC ? 0 : row_shift<T>(a.x, r, a.x_stride)), dyr = slot + a.cap + (VEC ? 0 : row_shift<T>(a.dy, r, a.dy_stride));
+        const f2 minus_mu = pair(-mu, -mu), rs2 = pair(rs, rs);
+        wait_row(g.bars + 8 * s, parity);
+        f2 sa = 0ull, sax = 0ull;
+#pragma unroll
+        for (int q = 0; q < EPT / 8; ++q) {
+            f2 x[4], u[4];
+            cols.read(xr, q, x);
+            cols.read(dyr, q, u);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f2 t = mul2(u[i], gw[4 * q + i]);
+                sa = add2(sa, t);
+                sax = fma2(t, mul2(add2(x[i], minus_mu), rs2), sax);
+            }
+        }
+        const float2 pa = split(sa), pax = split(sax);
+        const float2 v = make_float2(warp_sum(pa.x + pa.y), warp_sum(pax.x + pax.y));
+        if (g.lane == 0) to[g.warp] = v;
+    };
+    if (g.first < a.rows) {
+        int s = 0, pass = 0;
+        uint32_t parity = 0;
+        float mu = a.mean[g.first], rs = a.rstd[g.first];
+        first_reading(g.first, 0, 0u, mu, rs, part[0]);
+        for (long r = g.first; r < a.rows; r += g.step) {
+            group_sync(g.id, a.warps);
+            float2 t = part[pass][0];
+            for (int i = 1; i < a.warps; ++i) { const float2 o = part[pass][i]; t.x += o.x; t.y += o.y; }
+            pass ^= 1;
+            const int here = s;
+            if (++s == a.stages) { s = 0; parity ^= 1u; }
+            // the slot of the row before is spent: it takes the next row that is not under way yet
+            if (g.leads && r > g.first && r + (a.stages - 1) * g.step < a.rows) {
+                const int before = here == 0 ? a.stages - 1 : here - 1;
+                fetch_row<T, VEC, 2>(a, r + (a.stages - 1) * g.step, slot_of(before), g.bars + 8 * before);
+            }
+            float mu_next = 0.f, rs_next = 0.f;
+            if (r + g.step < a.rows) {
+                mu_next = a.mean[r + g.step];
+                rs_next = a.rstd[r + g.step];
+                first_reading(r + g.step, s, parity, mu_next, rs_next, part[pass]);
+            }
+            const uint32_t slot = vpce::smem_u32(slot_of(here));
+            const uint32_t xr = slot + (VEC ? 0 : row_shift<T>(a.x, r, a.x_stride)), dyr = slot + a.cap + (VEC ? 0 : row_shift<T>(a.dy, r, a.dy_stride));
+            const float ma = -t.x * inv_d, mx = -t.y * inv_d;
+            const f2 minus_mu = pair(-mu, -mu), rs2 = pair(rs, rs), ma2 = pair(ma, ma), mx2 = pair(mx, mx);
+            T* dx = static_cast<T*>(a.out) + r * a.out_stride;
+#pragma unroll
+            for (int q = 0; q < EPT / 8; ++q) {
+                f2 x[4], u[4];
+                cols.read(xr, q, x);
+                cols.read(dyr, q, u);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f2 xh = mul2(add2(x[i], minus_mu), rs2);
+                    dg[4 * q + i] = fma2(u[i], xh, dg[4 * q + i]);
+                    db[4 * q + i] = add2(u[i], db[4 * q + i]);
+                    x[i] = mul2(rs2, fma2(xh, mx2, add2(mul2(u[i], gw[4 * q + i]), ma2)));
+                }
+                if (a.out) cols.store(dx, q, x);
+            }
+            mu = mu_next;
+            rs = rs_next;
+        }
+    }
+    if (!a.partial) return;
+    // The block's sums: every group leaves its own in the ring (all copies have landed and been read), then all threads add
+    // them, the groups in order.
+    float* sums = reinterpret_cast<float*>(raw + RING_OFFSET);
+    __syncthreads();
+    float* mine = sums + static_cast<size_t>(g.id) * 2 * a.d;
+#pragma unroll
+    for (int i = 0; i < C::PAIRS; ++i) {
+        const float2 p = split(dg[i]), q = split(db[i]);
+        const int c0 = cols.first + C::STEP * (2 * i / C::N) + 2 * i % C::N, c1 = cols.first + C::STEP * ((2 * i + 1) / C::N) + (2 * i + 1) % C::N;
+        if (c0 < a.d) { mine[c0] = p.x; mine[a.d + c0] = q.x; }
+        if (c1 < a.d) { mine[c1] = p.y; mine[a.d + c1] = q.y; }
+    }
+    __syncthreads();
+    float* out = a.partial + static_cast<size_t>(blockIdx.x) * 2 * a.d;
+    for (int c = threadIdx.x; c < 2 * a.d; c += blockDim.x) {
+        float v = sums[c];
+        for (int q = 1; q < a.groups; ++q) v += sums[static_cast<size_t>(q) * 2 * a.d + c];
+        out[c] = v;
+    }
+}
+
+// ------------------------------------------------------------------------------------ generic kernels
 template <typename T, typename W>
 __global__ void __launch_bounds__(GEN_THREADS)
 ln_forward_generic(const T* x, long rows, long d, long x_stride, const W* __restrict__ g, const W* __restrict__ b, float eps,
@@ -131,25 +548,31 @@ ln_backward_columns(const T* __restrict__ dy, long dy_stride, const T* __restric
     }
 }
 
-// dweight, dbias = sums of the partial column sums, slices in a fixed order: 32 columns per block, 8 threads a column.
+// dweight, dbias = sums of the partial column sums, slices in a fixed order: 32 columns per block, 32 threads a column.
+constexpr int FIN_ROWS = 32;
 template <typename W>
-__global__ void __launch_bounds__(COL_TILE * COL_ROWS)
+__global__ void __launch_bounds__(COL_TILE * FIN_ROWS)
 ln_backward_finish(const float* __restrict__ partial, int slices, long d, W* __restrict__ dg, W* __restrict__ db) {
-    __shared__ float2 part[COL_ROWS][COL_TILE];
+    __shared__ float2 part[FIN_ROWS][COL_TILE + 1];
     const int cc = threadIdx.x % COL_TILE, rr = threadIdx.x / COL_TILE;
     const long c = static_cast<long>(blockIdx.x) * COL_TILE + cc;
     float sg = 0.f, sb = 0.f;
-    if (c < d)
-        for (int s = rr; s < slices; s += COL_ROWS) {
+    if (c < d) {
+#pragma unroll 4
+        for (int s = rr; s < slices; s += FIN_ROWS) {
             sg += partial[static_cast<long>(s) * 2 * d + c];
             sb += partial[static_cast<long>(s) * 2 * d + d + c];
         }
+    }
     part[rr][cc] = make_float2(sg, sb);
     __syncthreads();
-    if (rr == 0 && c < d) {
-        for (int i = 1; i < COL_ROWS; ++i) { sg += part[i][cc].x; sb += part[i][cc].y; }
-        if (dg) dg[c] = from_f<W>(sg);
-        if (db) db[c] = from_f<W>(sb);
+    const float2 v = part[cc][rr];                          // warp rr: the 32 sums of column rr
+    sg = warp_sum(v.x);
+    sb = warp_sum(v.y);
+    const long out = static_cast<long>(blockIdx.x) * COL_TILE + rr;
+    if (cc == 0 && out < d) {
+        if (dg) dg[out] = from_f<W>(sg);
+        if (db) db[out] = from_f<W>(sb);
     }
 }
 
@@ -161,18 +584,94 @@ bool known_type(int t) { return t == VPCE_BF16 || t == VPCE_F16 || t == VPCE_F32
 bool aligned_to(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 int slices_for(int64_t rows) {
-    const int64_t s = (rows + 15) / 16;
+    const int64_t s = rows;
     return static_cast<int>(s < 1 ? 1 : s > MAX_SLICES ? MAX_SLICES : s);
 }
 
 int grid_rows(int64_t rows) { return static_cast<int>(rows < 148 * 8 ? rows : 148 * 8); }
 
+int sm_count() {
+    static std::atomic<int> cached[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+    int n = cached[dev].load(std::memory_order_acquire);
+    if (!n) {
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 148;
+        cached[dev].store(n, std::memory_order_release);
+    }
+    return n;
+}
+
+// Shape of a row kernel's launch: `na` arrays in the ring.
+struct RowShape { int ept, threads, grid, smem; };
+RowShape row_shape(RowArgs* a, size_t elem, int na) {
+    RowShape s;
+    // 16 elements a thread: fewer registers each and more warps to hide a row's latencies than 24 or 32, which are for rows that
+    // 16 warps would not reach; 8 do for the narrowest
+    s.ept = a->d <= 256 ? 8 : a->d <= 16 * 32 * MAX_GROUP_WARPS ? 16 : a->d <= 24 * 32 * MAX_GROUP_WARPS ? 24 : 32;
+    a->warps = (a->d + 32 * s.ept - 1) / (32 * s.ept);
+    a->groups = std::max(1, (na == 1 ? 14 : 10) / a->warps);
+    while (a->groups > 1 && static_cast<int64_t>(a->groups - 1) * sm_count() >= a->rows) --a->groups;   // few rows: spread over the SMs
+    s.threads = 32 * a->warps * a->groups;
+    a->cap = static_cast<int>((a->d * elem + 15) / 16 * 16 + 16);
+    const int regs = na == 1 ? (s.ept <= 16 ? FORWARD_REGS<16> : FORWARD_REGS<32>) : (s.ept <= 16 ? BACKWARD_REGS<16> : BACKWARD_REGS<32>);
+    const int per_sm = std::max(1, std::min(3, 65536 / (regs * s.threads)));    // blocks that share an SM
+    const int budget = 220 * 1024 / per_sm - RING_OFFSET;
+    a->stages = std::max(2, std::min(8, budget / (a->groups * na * a->cap)));
+    s.smem = RING_OFFSET + a->groups * a->stages * na * a->cap;
+    if (na == 2) s.smem = std::max<int>(s.smem, RING_OFFSET + 8 * a->d * a->groups);        // the groups' sums take its place
+    const int64_t blocks = (a->rows + a->groups - 1) / a->groups;
+    s.grid = static_cast<int>(std::min<int64_t>(blocks, std::min(per_sm * sm_count(), MAX_SLICES)));
+    return s;
+}
+
+template <void (*kern)(const RowArgs)> cudaError_t launch_rows(const RowArgs& a, const RowShape& s, cudaStream_t st) {
+    static std::atomic<int> raised[64];                                         // of this kernel, per device
+    int dev = 0;
+    if (cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64 || !raised[dev].load(std::memory_order_acquire)) {
+        if (cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM); e != cudaSuccess) return e;
+        if (dev >= 0 && dev < 64) raised[dev].store(1, std::memory_order_release);
+    }
+    kern<<<s.grid, s.threads, s.smem, st>>>(a);
+    return cudaGetLastError();
+}
+
+bool rows_aligned(const void* p, int64_t stride, size_t e) { return aligned_to(p, 16) && stride * e % 16 == 0; }
+
+template <typename T, typename W, bool VEC> cudaError_t forward_rows(const RowArgs& a, const RowShape& s, cudaStream_t st) {
+    switch (s.ept) {
+        case 8: return launch_rows<ln_forward_rows<T, W, VEC, 8>>(a, s, st);
+        case 16: return launch_rows<ln_forward_rows<T, W, VEC, 16>>(a, s, st);
+        case 24: return launch_rows<ln_forward_rows<T, W, VEC, 24>>(a, s, st);
+        default: return launch_rows<ln_forward_rows<T, W, VEC, 32>>(a, s, st);
+    }
+}
+template <typename T, typename W, bool VEC> cudaError_t backward_rows(const RowArgs& a, const RowShape& s, cudaStream_t st) {
+    switch (s.ept) {
+        case 8: return launch_rows<ln_backward_rows<T, W, VEC, 8>>(a, s, st);
+        case 16: return launch_rows<ln_backward_rows<T, W, VEC, 16>>(a, s, st);
+        case 24: return launch_rows<ln_backward_rows<T, W, VEC, 24>>(a, s, st);
+        default: return launch_rows<ln_backward_rows<T, W, VEC, 32>>(a, s, st);
+    }
+}
+
+int code(cudaError_t e) { return e == cudaSuccess ? VPCE_OK : VPCE_CUDA_ERROR; }
+
 template <typename T, typename W>
 int forward_typed(const void* x, int64_t rows, int64_t d, int64_t xs, const void* g, const void* b, float eps, void* y, int64_t ys,
                   float* mean, float* rstd, cudaStream_t st) {
+    if (d <= MAX_ROW) {
+        RowArgs a{};
+        a.x = x; a.rows = rows; a.x_stride = xs; a.out_stride = ys; a.d = static_cast<int>(d); a.g = g; a.b = b; a.eps = eps; a.out = y;
+        a.mean = mean; a.rstd = rstd;
+        const RowShape s = row_shape(&a, sizeof(T), 1);                // two rows of 16384 fp32 fit the ring
+        const bool vec = d * sizeof(T) % 16 == 0 && rows_aligned(x, xs, sizeof(T)) && rows_aligned(y, ys, sizeof(T));
+        return code(vec ? forward_rows<T, W, true>(a, s, st) : forward_rows<T, W, false>(a, s, st));
+    }
     ln_forward_generic<T, W><<<grid_rows(rows), GEN_THREADS, 0, st>>>(
         static_cast<const T*>(x), rows, d, xs, static_cast<const W*>(g), static_cast<const W*>(b), eps, static_cast<T*>(y), ys, mean, rstd);
-    return cudaGetLastError() == cudaSuccess ? VPCE_OK : VPCE_CUDA_ERROR;
+    return code(cudaGetLastError());
 }
 
 template <typename T, typename W>
@@ -180,15 +679,29 @@ int backward_typed(const void* dy, int64_t dys, const void* x, int64_t xs, int64
                    const float* rstd, void* dx, int64_t dxs, void* dg, void* db, float* partial, cudaStream_t st) {
     const T *dyt = static_cast<const T*>(dy), *xt = static_cast<const T*>(x);
     const unsigned col_tiles = static_cast<unsigned>((d + COL_TILE - 1) / COL_TILE);
+    int slices = slices_for(rows);
+    if (d <= MAX_ROW && rows > 0 && 2 * 2 * (d * sizeof(T) + 32) + RING_OFFSET <= MAX_SMEM) {   // two rows of both arrays fit the ring
+        RowArgs a{};
+        a.x = x; a.dy = dy; a.rows = rows; a.x_stride = xs; a.dy_stride = dys; a.out_stride = dxs; a.d = static_cast<int>(d); a.g = g;
+        a.out = dx; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
+        a.partial = dg || db ? partial : nullptr;
+        const RowShape s = row_shape(&a, sizeof(T), 2);
+        const bool vec = d * sizeof(T) % 16 == 0 && rows_aligned(x, xs, sizeof(T)) && rows_aligned(dy, dys, sizeof(T)) &&
+                         rows_aligned(dx, dxs, sizeof(T));
+        if (cudaError_t e = vec ? backward_rows<T, W, true>(a, s, st) : backward_rows<T, W, false>(a, s, st); e != cudaSuccess)
+            return VPCE_CUDA_ERROR;
+        if (a.partial)
+            ln_backward_finish<W><<<col_tiles, COL_TILE * FIN_ROWS, 0, st>>>(partial, s.grid, d, static_cast<W*>(dg), static_cast<W*>(db));
+        return code(cudaGetLastError());
+    }
     if (dg || db) {
-        const int slices = slices_for(rows);
         ln_backward_columns<T><<<dim3(col_tiles, slices), COL_TILE * COL_ROWS, 0, st>>>(dyt, dys, xt, xs, rows, d, mean, rstd, partial);
-        ln_backward_finish<W><<<col_tiles, COL_TILE * COL_ROWS, 0, st>>>(partial, slices, d, static_cast<W*>(dg), static_cast<W*>(db));
+        ln_backward_finish<W><<<col_tiles, COL_TILE * FIN_ROWS, 0, st>>>(partial, slices, d, static_cast<W*>(dg), static_cast<W*>(db));
     }
     if (dx && rows > 0)                                     // after the column sums: dx may be dy itself
         ln_backward_dx_generic<T, W><<<grid_rows(rows), GEN_THREADS, 0, st>>>(dyt, dys, xt, xs, rows, d, static_cast<const W*>(g), mean,
                                                                             rstd, static_cast<T*>(dx), dxs);
-    return cudaGetLastError() == cudaSuccess ? VPCE_OK : VPCE_CUDA_ERROR;
+    return code(cudaGetLastError());
 }
 
 // Calls f with the element types of (x_dtype, w_dtype) as null pointers.
