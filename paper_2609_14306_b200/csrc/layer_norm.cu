@@ -2,8 +2,7 @@
 //
 // Row kernels (d <= 16384): a group of 1 to 16 warps owns a row at a time, 8 to 32 elements a thread.  Rows arrive by bulk
 // copies into a ring in shared memory, several rows ahead: what is in flight does not depend on registers or on how many warps
-// wait at a reduction.  A thread owns the same columns in every row, so it keeps their weights in registers, and in the backward
-// pass it sums dy xh and dy of its columns in registers over all rows of its group: the weight's gradient costs no second pass
+// wait at a reduction.  A thread owns the same columns in every row: in the backward pass it sums dy xh and dy of its columns in registers over all rows of its group: the weight's gradient costs no second pass
 // over the data, only one partial sum per block.  The variance is taken from the centred values in registers.  At 16-bit types
 // the arithmetic is as scarce as the memory (2 to 3 passes over every element): it runs on pairs (fp32x2 instructions).
 //   VEC      every row starts on a 16-byte boundary: 16-byte accesses
@@ -39,7 +38,7 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float
 constexpr int GEN_THREADS = 256;
 constexpr int COL_TILE = 32;            // columns per block of the column sums
 constexpr int COL_ROWS = 8;             // rows that a block of the column sums takes at a time
-constexpr int MAX_SLICES = 444;         // partial sums over rows: three blocks per SM of a 148-SM device
+constexpr int MAX_SLICES = 256;         // partial sums over rows: at least one block per SM
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -63,9 +62,11 @@ __device__ __forceinline__ float2 block_sum2(float a, float b, float2* part) {
 
 // ------------------------------------------------------------------------------------ row kernels
 constexpr int MAX_GROUP_WARPS = 16;
-constexpr int MAX_GROUPS = 14;                          // per block; a group of more than one warp has a named barrier
-template <int EPT> constexpr int FORWARD_REGS = EPT <= 16 ? 72 : 128;
-template <int EPT> constexpr int BACKWARD_REGS = EPT <= 16 ? 96 : 128;
+// One block per SM.  Forward: 28 warps of 72 registers (a row's 32 elements a thread and what is worked on); backward: 16 warps
+// of 128 (the 64 column sums).
+constexpr int FORWARD_REGS = 72, FORWARD_WARPS = 28, BACKWARD_REGS = 128, BACKWARD_WARPS = 16;
+constexpr int MAX_GROUPS = FORWARD_WARPS;               // per block; a group of more than one warp has a named barrier
+constexpr int MAX_STAGES = 8;
 constexpr int MAX_EPT = 32;                             // elements per thread
 constexpr int MAX_SMEM = 227 * 1024;
 constexpr int64_t MAX_ROW = 32 * MAX_GROUP_WARPS * MAX_EPT;
@@ -75,6 +76,7 @@ struct RowArgs {
     long rows, x_stride, dy_stride, out_stride;
     int d, warps;                                       // warps per group
     int groups, stages, cap;                            // groups per block, ring depth, bytes of a row in the ring
+    int ring;                                           // byte offset of the ring in shared memory
     const void *g, *b;
     float eps;
     void* out;                                          // y or dx (may be null in the backward pass)
@@ -82,55 +84,64 @@ struct RowArgs {
     float* partial;                                     // [blocks][2][d] or null
 };
 
-struct Smem {                                           // of a block: barriers, reduction scratch, ring
-    uint64_t full[MAX_GROUPS][8];                       // [group][stage]
-    float2 part[MAX_GROUPS][2][MAX_GROUP_WARPS];        // [group][pass][warp]
+struct Smem {                                           // of a block: barriers, reduction scratch; then weights, ring
+    uint64_t full[MAX_GROUPS][MAX_STAGES];              // [group][stage]
+    float2 part[MAX_GROUPS][2][MAX_GROUP_WARPS];        // [group][turn][warp]
 };
-constexpr int RING_OFFSET = (sizeof(Smem) + 127) / 128 * 128;
+constexpr int WEIGHTS_OFFSET = (sizeof(Smem) + 127) / 128 * 128;
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
-// Bytes by which row `r` starts behind a 16-byte boundary.
-template <typename T> __device__ __forceinline__ int row_shift(const void* base, long r, long stride) {
-    return static_cast<int>((reinterpret_cast<uintptr_t>(base) + static_cast<size_t>(r) * stride * sizeof(T)) & 15u);
-}
+// One array's rows as a group meets them: the address of the row to be fetched next and of the row in work.
+struct Rows {
+    const char* base;
+    size_t pitch;                                       // bytes between rows
+    __device__ __forceinline__ const char* at(long r) const { return base + static_cast<size_t>(r) * pitch; }
+    // bytes by which row r starts behind a 16-byte boundary
+    __device__ __forceinline__ uint32_t shift(long r) const {
+        return (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base)) + static_cast<uint32_t>(r) * static_cast<uint32_t>(pitch)) & 15u;
+    }
+};
 
-// Starts the copy of row r into `dst` (its first element lands row_shift bytes behind dst); returns the bytes that will be
-// counted on the barrier.  Granules that reach over the tensor's first or last byte are left to plain element copies.
+// What row r of an array takes: `*from`, the address from which the bulk copy reads, `*at`, where it lands in the slot, and the
+// bytes that it moves.  The row's first element lands shift(r) bytes into the slot.  A granule that reaches over the tensor's
+// first or last byte is left to plain element copies, made here.
 template <typename T, bool VEC>
-__device__ __forceinline__ uint32_t copy_extent(const void* base, long r, long rows, long stride, int d, const char** from, uint32_t* at,
-                                                uint8_t* dst_generic) {
-    const char* row = static_cast<const char*>(base) + static_cast<size_t>(r) * stride * sizeof(T);
+__device__ __forceinline__ uint32_t copy_extent(const Rows& a, long r, long rows, int d, const char** from, uint32_t* at, uint8_t* slot) {
+    const char* row = a.at(r);
     const size_t bytes = static_cast<size_t>(d) * sizeof(T);
     if (VEC) { *from = row; *at = 0; return static_cast<uint32_t>(bytes); }
     const uintptr_t lo = reinterpret_cast<uintptr_t>(row), hi = lo + bytes;
-    uintptr_t a = lo & ~static_cast<uintptr_t>(15), e = (hi + 15) & ~static_cast<uintptr_t>(15);
-    const uintptr_t origin = a;
-    if (r == 0 && a < lo) a += 16;                      // before the tensor's first element
-    if (r == rows - 1 && e > hi) e -= 16;               // behind its last
-    if (e < a) e = a;
-    if (a > lo || e < hi) {                             // the first or last row's ragged ends, or a row inside one granule
+    uintptr_t b = lo & ~static_cast<uintptr_t>(15), e = (hi + 15) & ~static_cast<uintptr_t>(15);
+    const uintptr_t origin = b;
+    if (r == 0 || r == rows - 1) {
+        if (r == 0 && b < lo) b += 16;
+        if (r == rows - 1 && e > hi) e -= 16;
+        if (e < b) e = b;
         const T* src = reinterpret_cast<const T*>(lo);
-        T* dst = reinterpret_cast<T*>(dst_generic + (lo - origin));
-        for (int c = 0; c < d && lo + c * sizeof(T) < a; ++c) dst[c] = src[c];
+        T* dst = reinterpret_cast<T*>(slot + (lo - origin));
+        for (int c = 0; c < d && lo + c * sizeof(T) < b; ++c) dst[c] = src[c];
         for (int c = d - 1; c >= 0 && lo + c * sizeof(T) >= e; --c) dst[c] = src[c];
     }
-    *from = reinterpret_cast<const char*>(a);
-    *at = static_cast<uint32_t>(a - origin);
-    return static_cast<uint32_t>(e - a);
+    *from = reinterpret_cast<const char*>(b);
+    *at = static_cast<uint32_t>(b - origin);
+    return static_cast<uint32_t>(e - b);
 }
 
-// One thread: row r of the NA arrays into ring slot `slot` (generic address), signalled on `bar`.
+// One thread: row r of the NA arrays into ring slot `slot`, signalled on `bar`.
 template <typename T, bool VEC, int NA>
-__device__ __forceinline__ void fetch_row(const RowArgs& a, long r, uint8_t* slot, uint32_t bar) {
-    const char* from[2];
-    uint32_t at[2], bytes[2] = {0, 0};
-    bytes[0] = copy_extent<T, VEC>(a.x, r, a.rows, a.x_stride, a.d, &from[0], &at[0], slot);
-    if (NA == 2) bytes[1] = copy_extent<T, VEC>(a.dy, r, a.rows, a.dy_stride, a.d, &from[1], &at[1], slot + a.cap);
-    vpce::mbar_arrive_expect_tx(bar, bytes[0] + bytes[1]);
+__device__ __forceinline__ void fetch_row(const RowArgs& a, const Rows* in, long r, uint8_t* slot, uint32_t bar) {
+    const char* from[NA];
+    uint32_t at[NA], bytes[NA], total = 0;
+#pragma unroll
+    for (int i = 0; i < NA; ++i) {
+        bytes[i] = copy_extent<T, VEC>(in[i], r, a.rows, a.d, &from[i], &at[i], slot + i * a.cap);
+        total += bytes[i];
+    }
+    vpce::mbar_arrive_expect_tx(bar, total);
     const uint32_t dst = vpce::smem_u32(slot);
 #pragma unroll
     for (int i = 0; i < NA; ++i)
@@ -148,18 +159,12 @@ __device__ __forceinline__ void group_sync(int group, int warps) {
     else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(warps * 32) : "memory");
 }
 
-// Sums of two values over the group; `part` is that of one pass (the passes of a row take turns).
-__device__ __forceinline__ float2 group_sum2(float a, float b, float2* part, int group, int warps, int warp, int lane) {
-    a = warp_sum(a);
-    b = warp_sum(b);
-    if (warps == 1) return make_float2(a, b);
-    if (lane == 0) part[warp] = make_float2(a, b);
-    group_sync(group, warps);
-    float2 s = part[0];
-    for (int i = 1; i < warps; ++i) { const float2 t = part[i]; s.x += t.x; s.y += t.y; }
-    return s;
+// Sum over 16 neighbouring lanes; after a group's barrier lane l of either half holds what warp l has left.
+__device__ __forceinline__ float half_warp_sum(float v) {
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
 }
-
 // Pairs of fp32 in one 64-bit register.
 using f2 = unsigned long long;
 __device__ __forceinline__ f2 pair(float a, float b) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
@@ -191,6 +196,7 @@ template <typename T, bool VEC, int EPT> struct Columns {
     static constexpr int PIECES = EPT / N, PAIRS = EPT / 2, STEP = 32 * N, PART = 8 / N;
     int first, d;
     __device__ __forceinline__ Columns(int warp, int lane, int d_) : first(warp * 32 * EPT + lane * N), d(d_) {}
+    __device__ __forceinline__ bool whole() const { return first + STEP * (PIECES - 1) + STEP - N < d; }   // no lane of the warp lacks any (N divides d)
     __device__ __forceinline__ bool has(int k) const { return first + STEP * k < d; }    // VEC: d is a multiple of N
 
     // Eight of the thread's elements (part q of EPT / 8) of a row in shared memory (address of its first element); columns beyond
@@ -231,15 +237,18 @@ template <typename T, bool VEC, int EPT> struct Columns {
         }
     }
 
-    // Their weights (W of any alignment), `none` where p is null; columns beyond d as 0.
-    template <typename W> __device__ __forceinline__ void weights(const W* p, float none, f2* v) const {
-        float f[EPT];
+    // Weights as fp32 in shared memory, in the order of the threads' elements: four of a lane's in 16 bytes, lanes side by side.
+    // fill: this warp's (W of any alignment; `none` where p is null; 0 beyond d); weights: part q of this thread's.
+    template <typename W> __device__ __forceinline__ void fill(float* to, int warp, int lane, const W* p, float none) const {
+        for (int e = 0; e < EPT; ++e) {
+            const int k = e / N, c = first + STEP * k + e % N;
+            to[((warp * (EPT / 4) + e / 4) * 32 + lane) * 4 + e % 4] = c < d ? (p ? to_f(p[c]) : none) : 0.f;
+        }
+    }
+    __device__ __forceinline__ void weights(uint32_t at, int q, f2* v) const {
 #pragma unroll
-        for (int k = 0; k < PIECES; ++k)
-#pragma unroll
-            for (int j = 0; j < N; ++j) f[k * N + j] = has(k) ? (p ? to_f(p[first + STEP * k + j]) : none) : 0.f;
-#pragma unroll
-        for (int i = 0; i < PAIRS; ++i) v[i] = pair(f[2 * i], f[2 * i + 1]);
+        for (int i = 0; i < 2; ++i)
+            asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(v[2 * i]), "=l"(v[2 * i + 1]) : "r"(at + (2 * q + i) * 512));
     }
 
     __device__ __forceinline__ void store(T* row, int q, const f2* v) const {
@@ -271,7 +280,7 @@ template <typename T, bool VEC, int EPT> struct Columns {
 // What every row kernel sets up: the group's place and its ring.
 struct Group {
     int id, warp, lane;
-    bool leads;                                         // this thread issues the group's copies
+    Rows in[2];
     long first, step;                                   // rows of this group: first, first + step, ...
     uint8_t* ring;
     uint32_t bars;
@@ -283,75 +292,103 @@ __device__ __forceinline__ Group group_setup(const RowArgs& a, uint8_t* raw) {
     g.id = (threadIdx.x >> 5) / a.warps;
     g.warp = (threadIdx.x >> 5) - g.id * a.warps;
     g.lane = threadIdx.x & 31;
-    g.leads = g.warp == 0 && g.lane == 0;
+    g.in[0] = Rows{static_cast<const char*>(a.x), static_cast<size_t>(a.x_stride) * sizeof(T)};
+    if (NA == 2) g.in[1] = Rows{static_cast<const char*>(a.dy), static_cast<size_t>(a.dy_stride) * sizeof(T)};
     g.first = static_cast<long>(blockIdx.x) * a.groups + g.id;
     g.step = static_cast<long>(gridDim.x) * a.groups;
-    g.ring = raw + RING_OFFSET + static_cast<size_t>(g.id) * a.stages * NA * a.cap;
+    g.ring = raw + a.ring + g.id * a.stages * NA * a.cap;
     g.bars = vpce::smem_u32(&sm->full[g.id][0]);
-    if (g.leads) {
+    if (g.warp == 0 && g.lane == 0) {
         for (int s = 0; s < a.stages; ++s) vpce::mbar_init(g.bars + 8 * s, 1);
         vpce::fence_barrier_init();
         vpce::fence_proxy_async();
     }
     group_sync(g.id, a.warps);
-    if (g.leads)
+    if (g.warp == 0 && g.lane == 0)
         for (int s = 0; s < a.stages; ++s) {
             const long r = g.first + s * g.step;
-            if (r < a.rows) fetch_row<T, VEC, NA>(a, r, g.ring + static_cast<size_t>(s) * NA * a.cap, g.bars + 8 * s);
+            if (r < a.rows) fetch_row<T, VEC, NA>(a, g.in, r, g.ring + s * NA * a.cap, g.bars + 8 * s);
         }
     return g;
 }
 
 template <typename T, typename W, bool VEC, int EPT>
-__global__ void __maxnreg__(FORWARD_REGS<EPT>) ln_forward_rows(const RowArgs a) {
+__global__ void __maxnreg__(FORWARD_REGS) ln_forward_rows(const RowArgs a) {
     extern __shared__ __align__(128) uint8_t raw[];
     const Group g = group_setup<T, VEC, 1>(a, raw);
     const Columns<T, VEC, EPT> cols(g.warp, g.lane, a.d);
     using C = Columns<T, VEC, EPT>;
+    float* const weights = reinterpret_cast<float*>(raw + WEIGHTS_OFFSET);
+    const int n_weights = 32 * EPT * a.warps;
+    if (g.id == 0) cols.fill(weights, g.warp, g.lane, static_cast<const W*>(a.g), 1.f);
+    if (g.id == a.groups - 1) cols.fill(weights + n_weights, g.warp, g.lane, static_cast<const W*>(a.b), 0.f);
+    __syncthreads();
+    const uint32_t gw = vpce::smem_u32(weights) + (g.warp * (EPT / 4) * 32 + g.lane) * 16, bw = gw + 4 * n_weights;
     float2(*part)[MAX_GROUP_WARPS] = reinterpret_cast<Smem*>(raw)->part[g.id];
     const float inv_d = 1.f / static_cast<float>(a.d);
-    f2 gw[C::PAIRS], bw[C::PAIRS];
-    cols.weights(static_cast<const W*>(a.g), 1.f, gw);
-    cols.weights(static_cast<const W*>(a.b), 0.f, bw);
-    int s = 0;
+    const bool whole = cols.whole();
+    auto columns_of = [&](int warp) { return static_cast<float>(min(max(a.d - warp * 32 * EPT, 0), 32 * EPT)); };
+    const float inv_mine = 1.f / columns_of(g.warp);
+    const float n_lane = (g.lane & 15) < a.warps ? columns_of(g.lane & 15) : 0.f;
+    const float inv_lane = n_lane > 0.f ? 1.f / n_lane : 0.f;
+    int s = 0, pass = 0, turn = 0;                                          // the warps take turns at starting copies
     uint32_t parity = 0;
-    for (long r = g.first; r < a.rows; r += g.step) {
-        uint8_t* slot = g.ring + static_cast<size_t>(s) * a.cap;
+    T* out = static_cast<T*>(a.out) + g.first * a.out_stride;
+    const long out_step = g.step * a.out_stride;
+    for (long r = g.first; r < a.rows; r += g.step, out += out_step) {
+        const uint32_t xr = vpce::smem_u32(g.ring + s * a.cap) + (VEC ? 0u : g.in[0].shift(r));
         wait_row(g.bars + 8 * s, parity);
         f2 v[C::PAIRS];
-        const uint32_t xr = vpce::smem_u32(slot) + (VEC ? 0 : row_shift<T>(a.x, r, a.x_stride));
 #pragma unroll
         for (int q = 0; q < EPT / 8; ++q) cols.read(xr, q, v + 4 * q);
+        // A warp's statistics: its columns' sum, and the sum of the squares around their own mean, which needs no other warp.
         f2 s0 = v[0], s1 = v[1];
 #pragma unroll
         for (int i = 2; i < C::PAIRS; i += 2) { s0 = add2(s0, v[i]); s1 = add2(s1, v[i + 1]); }
-        const float2 sum = split(add2(s0, s1));
-        const float mu = group_sum2(sum.x + sum.y, 0.f, part[0], g.id, a.warps, g.warp, g.lane).x * inv_d;
-        // everyone has read the slot
-        if (g.leads && r + a.stages * g.step < a.rows) fetch_row<T, VEC, 1>(a, r + a.stages * g.step, slot, g.bars + 8 * s);
-        if (++s == a.stages) { s = 0; parity ^= 1u; }
-        const f2 minus_mu = pair(-mu, -mu);
+        const float2 t = split(add2(s0, s1));
+        const float sum = warp_sum(t.x + t.y), mine = sum * inv_mine;
+        const f2 minus = pair(-mine, -mine);
+        f2 q0 = 0ull, q1 = 0ull;
+        if (whole) {
 #pragma unroll
-        for (int i = 0; i < C::PAIRS; ++i) {
-            v[i] = add2(v[i], minus_mu);
-            // columns beyond d count nothing
-            if constexpr (VEC) {
-                if (!cols.has(i * 2 / C::N)) v[i] = 0ull;
-            } else {
-                if (!cols.has(2 * i + 1)) { const float2 t = split(v[i]); v[i] = pair(cols.has(2 * i) ? t.x : 0.f, 0.f); }
+            for (int i = 0; i < C::PAIRS; i += 2) {
+                const f2 e = add2(v[i], minus), f = add2(v[i + 1], minus);
+                q0 = fma2(e, e, q0);
+                q1 = fma2(f, f, q1);
+            }
+        } else {                                                            // columns beyond d count nothing
+#pragma unroll
+            for (int i = 0; i < C::PAIRS; ++i) {
+                const float2 e = split(add2(v[i], minus));
+                const f2 f = pair(cols.has(2 * i / C::N) ? e.x : 0.f, cols.has((2 * i + 1) / C::N) ? e.y : 0.f);
+                q0 = fma2(f, f, q0);
             }
         }
-        f2 q0 = mul2(v[0], v[0]), q1 = mul2(v[1], v[1]);
+        const float2 u = split(add2(q0, q1));
+        const float squares = warp_sum(u.x + u.y);
+        if (g.lane == 0) part[pass][g.warp] = make_float2(sum, squares);
+        group_sync(g.id, a.warps);
+        // everyone has read the slot: it takes the next row that is not under way yet
+        if (g.warp == turn && g.lane == 0 && r + a.stages * g.step < a.rows) fetch_row<T, VEC, 1>(a, g.in, r + a.stages * g.step, g.ring + s * a.cap, g.bars + 8 * s);
+        if (++turn == a.warps) turn = 0;
+        if (++s == a.stages) { s = 0; parity ^= 1u; }
+        // The row's statistics from the warps': squares around the row's mean = sum of theirs + n (their mean - the row's)^2.
+        const float2 w = (g.lane & 15) < a.warps ? part[pass][g.lane & 15] : make_float2(0.f, 0.f);
+        pass ^= 1;
+        const float mu = half_warp_sum(w.x) * inv_d;
+        const float off = w.x * inv_lane - mu;
+        const float rs = 1.f / sqrtf(half_warp_sum(fmaf(n_lane * off, off, w.y)) * inv_d + a.eps);
+        const f2 minus_mu = pair(-mu, -mu), rs2 = pair(rs, rs);
 #pragma unroll
-        for (int i = 2; i < C::PAIRS; i += 2) { q0 = fma2(v[i], v[i], q0); q1 = fma2(v[i + 1], v[i + 1], q1); }
-        const float2 sq = split(add2(q0, q1));
-        const float rs = 1.f / sqrtf(group_sum2(sq.x + sq.y, 0.f, part[1], g.id, a.warps, g.warp, g.lane).x * inv_d + a.eps);
-        const f2 rs2 = pair(rs, rs);
+        for (int q = 0; q < EPT / 8; ++q) {
+            f2 gq[4], bq[4];
+            cols.weights(gw, q, gq);
+            cols.weights(bw, q, bq);
 #pragma unroll
-        for (int i = 0; i < C::PAIRS; ++i) v[i] = fma2(mul2(v[i], rs2), gw[i], bw[i]);
-#pragma unroll
-        for (int q = 0; q < EPT / 8; ++q) cols.store(static_cast<T*>(a.out) + r * a.out_stride, q, v + 4 * q);
-        if (g.leads) {
+            for (int i = 0; i < 4; ++i) v[4 * q + i] = fma2(mul2(add2(v[4 * q + i], minus_mu), rs2), gq[i], bq[i]);
+            cols.store(out, q, v + 4 * q);
+        }
+        if (g.warp == 0 && g.lane == 0) {
             if (a.mean) a.mean[r] = mu;
             if (a.rstd) a.rstd[r] = rs;
         }
@@ -359,35 +396,39 @@ __global__ void __maxnreg__(FORWARD_REGS<EPT>) ln_forward_rows(const RowArgs a) 
 }
 
 template <typename T, typename W, bool VEC, int EPT>
-__global__ void __maxnreg__(BACKWARD_REGS<EPT>) ln_backward_rows(const RowArgs a) {
+__global__ void __maxnreg__(BACKWARD_REGS) ln_backward_rows(const RowArgs a) {
     extern __shared__ __align__(128) uint8_t raw[];
     const Group g = group_setup<T, VEC, 2>(a, raw);
     const Columns<T, VEC, EPT> cols(g.warp, g.lane, a.d);
     using C = Columns<T, VEC, EPT>;
     float2(*part)[MAX_GROUP_WARPS] = reinterpret_cast<Smem*>(raw)->part[g.id];
     const float inv_d = 1.f / static_cast<float>(a.d);
-    f2 gw[C::PAIRS], dg[C::PAIRS], db[C::PAIRS];
-    cols.weights(static_cast<const W*>(a.g), 1.f, gw);
+    float* const weights = reinterpret_cast<float*>(raw + WEIGHTS_OFFSET);
+    if (g.id == 0) cols.fill(weights, g.warp, g.lane, static_cast<const W*>(a.g), 1.f);
+    __syncthreads();
+    const uint32_t gw = vpce::smem_u32(weights) + (g.warp * (EPT / 4) * 32 + g.lane) * 16;
+    f2 dg[C::PAIRS], db[C::PAIRS];
 #pragma unroll
     for (int i = 0; i < C::PAIRS; ++i) dg[i] = db[i] = 0ull;
     // The row is read from the ring twice, before and after the group's sums: the registers that would keep it hold the column
     // sums.  Weights of columns beyond d are 0, so those columns add nothing to the sums.  The first reading of a row comes
     // before the second reading of the row before it, so the group's barrier finds everyone with work in between.
-    auto slot_of = [&](int s) { return g.ring + static_cast<size_t>(s) * 2 * a.cap; };
+    auto slot_of = [&](int s) { return g.ring + s * 2 * a.cap; };
     auto first_reading = [&](long r, int s, uint32_t parity, float mu, float rs, float2* to) {
         const uint32_t slot = vpce::smem_u32(slot_of(s));
-        const uint32_t xr = slot + (VEC ? 0 : row_shift<T>(a.x, r, a.x_stride)), dyr = slot + a.cap + (VEC ? 0 : row_shift<T>(a.dy, r, a.dy_stride));
+        const uint32_t xr = slot + (VEC ? 0u : g.in[0].shift(r)), dyr = slot + a.cap + (VEC ? 0u : g.in[1].shift(r));
         const f2 minus_mu = pair(-mu, -mu), rs2 = pair(rs, rs);
         wait_row(g.bars + 8 * s, parity);
         f2 sa = 0ull, sax = 0ull;
 #pragma unroll
         for (int q = 0; q < EPT / 8; ++q) {
-            f2 x[4], u[4];
+            f2 x[4], u[4], gq[4];
             cols.read(xr, q, x);
             cols.read(dyr, q, u);
+            cols.weights(gw, q, gq);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const f2 t = mul2(u[i], gw[4 * q + i]);
+                const f2 t = mul2(u[i], gq[i]);
                 sa = add2(sa, t);
                 sax = fma2(t, mul2(add2(x[i], minus_mu), rs2), sax);
             }
@@ -397,55 +438,59 @@ __global__ void __maxnreg__(BACKWARD_REGS<EPT>) ln_backward_rows(const RowArgs a
         if (g.lane == 0) to[g.warp] = v;
     };
     if (g.first < a.rows) {
-        int s = 0, pass = 0;
+        int s = 0, pass = 0, turn = 0;                                      // the warps take turns at starting copies
         uint32_t parity = 0;
-        float mu = a.mean[g.first], rs = a.rstd[g.first];
+        T* dx = static_cast<T*>(a.out) + g.first * a.out_stride;
+        const long out_step = g.step * a.out_stride;
+        // the statistics of a row are loaded two rows ahead
+        float mu = a.mean[g.first], rs = a.rstd[g.first], mu_next = 0.f, rs_next = 0.f;
+        if (g.first + g.step < a.rows) { mu_next = a.mean[g.first + g.step]; rs_next = a.rstd[g.first + g.step]; }
         first_reading(g.first, 0, 0u, mu, rs, part[0]);
-        for (long r = g.first; r < a.rows; r += g.step) {
+        for (long r = g.first; r < a.rows; r += g.step, dx += out_step) {
             group_sync(g.id, a.warps);
-            float2 t = part[pass][0];
-            for (int i = 1; i < a.warps; ++i) { const float2 o = part[pass][i]; t.x += o.x; t.y += o.y; }
+            float2 t = make_float2(0.f, 0.f);
+            if ((g.lane & 15) < a.warps) t = part[pass][g.lane & 15];
+            t.x = half_warp_sum(t.x);
+            t.y = half_warp_sum(t.y);
             pass ^= 1;
             const int here = s;
             if (++s == a.stages) { s = 0; parity ^= 1u; }
             // the slot of the row before is spent: it takes the next row that is not under way yet
-            if (g.leads && r > g.first && r + (a.stages - 1) * g.step < a.rows) {
+            if (g.warp == turn && g.lane == 0 && r > g.first && r + (a.stages - 1) * g.step < a.rows) {
                 const int before = here == 0 ? a.stages - 1 : here - 1;
-                fetch_row<T, VEC, 2>(a, r + (a.stages - 1) * g.step, slot_of(before), g.bars + 8 * before);
+                fetch_row<T, VEC, 2>(a, g.in, r + (a.stages - 1) * g.step, slot_of(before), g.bars + 8 * before);
             }
-            float mu_next = 0.f, rs_next = 0.f;
-            if (r + g.step < a.rows) {
-                mu_next = a.mean[r + g.step];
-                rs_next = a.rstd[r + g.step];
-                first_reading(r + g.step, s, parity, mu_next, rs_next, part[pass]);
-            }
+            if (++turn == a.warps) turn = 0;
+            float mu_later = 0.f, rs_later = 0.f;
+            if (r + 2 * g.step < a.rows) { mu_later = a.mean[r + 2 * g.step]; rs_later = a.rstd[r + 2 * g.step]; }
+            if (r + g.step < a.rows) first_reading(r + g.step, s, parity, mu_next, rs_next, part[pass]);
             const uint32_t slot = vpce::smem_u32(slot_of(here));
-            const uint32_t xr = slot + (VEC ? 0 : row_shift<T>(a.x, r, a.x_stride)), dyr = slot + a.cap + (VEC ? 0 : row_shift<T>(a.dy, r, a.dy_stride));
+            const uint32_t xr = slot + (VEC ? 0u : g.in[0].shift(r)), dyr = slot + a.cap + (VEC ? 0u : g.in[1].shift(r));
             const float ma = -t.x * inv_d, mx = -t.y * inv_d;
             const f2 minus_mu = pair(-mu, -mu), rs2 = pair(rs, rs), ma2 = pair(ma, ma), mx2 = pair(mx, mx);
-            T* dx = static_cast<T*>(a.out) + r * a.out_stride;
 #pragma unroll
             for (int q = 0; q < EPT / 8; ++q) {
-                f2 x[4], u[4];
+                f2 x[4], u[4], gq[4];
                 cols.read(xr, q, x);
                 cols.read(dyr, q, u);
+                cols.weights(gw, q, gq);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const f2 xh = mul2(add2(x[i], minus_mu), rs2);
                     dg[4 * q + i] = fma2(u[i], xh, dg[4 * q + i]);
                     db[4 * q + i] = add2(u[i], db[4 * q + i]);
-                    x[i] = mul2(rs2, fma2(xh, mx2, add2(mul2(u[i], gw[4 * q + i]), ma2)));
+                    x[i] = mul2(rs2, fma2(xh, mx2, add2(mul2(u[i], gq[i]), ma2)));
                 }
                 if (a.out) cols.store(dx, q, x);
             }
-            mu = mu_next;
-            rs = rs_next;
+            mu = mu_next; rs = rs_next;
+            mu_next = mu_later; rs_next = rs_later;
         }
     }
     if (!a.partial) return;
     // The block's sums: every group leaves its own in the ring (all copies have landed and been read), then all threads add
     // them, the groups in order.
-    float* sums = reinterpret_cast<float*>(raw + RING_OFFSET);
+    float* sums = reinterpret_cast<float*>(raw + a.ring);
     __syncthreads();
     float* mine = sums + static_cast<size_t>(g.id) * 2 * a.d;
 #pragma unroll
@@ -602,26 +647,30 @@ int sm_count() {
     return n;
 }
 
-// Shape of a row kernel's launch: `na` arrays in the ring.
+// Shape of a row kernel's launch: `na` arrays in the ring.  grid 0: the row is too wide for shared memory.
 struct RowShape { int ept, threads, grid, smem; };
 RowShape row_shape(RowArgs* a, size_t elem, int na) {
     RowShape s;
-    // 16 elements a thread: fewer registers each and more warps to hide a row's latencies than 24 or 32, which are for rows that
-    // 16 warps would not reach; 8 do for the narrowest
-    s.ept = a->d <= 256 ? 8 : a->d <= 16 * 32 * MAX_GROUP_WARPS ? 16 : a->d <= 24 * 32 * MAX_GROUP_WARPS ? 24 : 32;
-    a->warps = (a->d + 32 * s.ept - 1) / (32 * s.ept);
-    a->groups = std::max(1, (na == 1 ? 14 : 10) / a->warps);
+    // Elements per thread: a warp costs about 8 instructions for each of its threads' elements and 110 for the rest of a row
+    // (waits, sums over the warp and the group).  At d = 7168 in 16 bits: 7 warps of 32 rather than 14 of 16.
+    s.ept = 8;
+    int best = 1 << 30;
+    for (int ept = 8; ept <= MAX_EPT; ept += 8) {
+        const int warps = (a->d + 32 * ept - 1) / (32 * ept), cost = warps * (8 * ept + 110);
+        if (warps <= MAX_GROUP_WARPS && cost < best) { best = cost; s.ept = ept; a->warps = warps; }
+    }
+    const int most = (na == 1 ? FORWARD_WARPS : BACKWARD_WARPS) / a->warps;
+    a->groups = std::max(1, a->warps > 1 ? std::min(most, 15) : most);          // named barriers 1 to 15
     while (a->groups > 1 && static_cast<int64_t>(a->groups - 1) * sm_count() >= a->rows) --a->groups;   // few rows: spread over the SMs
-    s.threads = 32 * a->warps * a->groups;
     a->cap = static_cast<int>((a->d * elem + 15) / 16 * 16 + 16);
-    const int regs = na == 1 ? (s.ept <= 16 ? FORWARD_REGS<16> : FORWARD_REGS<32>) : (s.ept <= 16 ? BACKWARD_REGS<16> : BACKWARD_REGS<32>);
-    const int per_sm = std::max(1, std::min(3, 65536 / (regs * s.threads)));    // blocks that share an SM
-    const int budget = 220 * 1024 / per_sm - RING_OFFSET;
-    a->stages = std::max(2, std::min(8, budget / (a->groups * na * a->cap)));
-    s.smem = RING_OFFSET + a->groups * a->stages * na * a->cap;
-    if (na == 2) s.smem = std::max<int>(s.smem, RING_OFFSET + 8 * a->d * a->groups);        // the groups' sums take its place
+    a->ring = WEIGHTS_OFFSET + (na == 1 ? 2 : 1) * 4 * 32 * s.ept * a->warps;
+    while (a->groups > 1 && a->ring + a->groups * 2 * na * a->cap > MAX_SMEM) --a->groups;
+    a->stages = std::min(MAX_STAGES, (MAX_SMEM - a->ring) / (a->groups * na * a->cap));
+    s.threads = 32 * a->warps * a->groups;
+    s.smem = a->ring + a->groups * a->stages * na * a->cap;
+    if (na == 2) s.smem = std::max<int>(s.smem, a->ring + 8 * a->d * a->groups);    // the groups' sums take its place
     const int64_t blocks = (a->rows + a->groups - 1) / a->groups;
-    s.grid = static_cast<int>(std::min<int64_t>(blocks, std::min(per_sm * sm_count(), MAX_SLICES)));
+    s.grid = a->stages >= 2 && s.smem <= MAX_SMEM ? static_cast<int>(std::min<int64_t>(blocks, std::min(sm_count(), MAX_SLICES))) : 0;
     return s;
 }
 
@@ -665,9 +714,9 @@ int forward_typed(const void* x, int64_t rows, int64_t d, int64_t xs, const void
         RowArgs a{};
         a.x = x; a.rows = rows; a.x_stride = xs; a.out_stride = ys; a.d = static_cast<int>(d); a.g = g; a.b = b; a.eps = eps; a.out = y;
         a.mean = mean; a.rstd = rstd;
-        const RowShape s = row_shape(&a, sizeof(T), 1);                // two rows of 16384 fp32 fit the ring
+        const RowShape s = row_shape(&a, sizeof(T), 1);
         const bool vec = d * sizeof(T) % 16 == 0 && rows_aligned(x, xs, sizeof(T)) && rows_aligned(y, ys, sizeof(T));
-        return code(vec ? forward_rows<T, W, true>(a, s, st) : forward_rows<T, W, false>(a, s, st));
+        if (s.grid > 0) return code(vec ? forward_rows<T, W, true>(a, s, st) : forward_rows<T, W, false>(a, s, st));
     }
     ln_forward_generic<T, W><<<grid_rows(rows), GEN_THREADS, 0, st>>>(
         static_cast<const T*>(x), rows, d, xs, static_cast<const W*>(g), static_cast<const W*>(b), eps, static_cast<T*>(y), ys, mean, rstd);
@@ -680,7 +729,7 @@ int backward_typed(const void* dy, int64_t dys, const void* x, int64_t xs, int64
     const T *dyt = static_cast<const T*>(dy), *xt = static_cast<const T*>(x);
     const unsigned col_tiles = static_cast<unsigned>((d + COL_TILE - 1) / COL_TILE);
     int slices = slices_for(rows);
-    if (d <= MAX_ROW && rows > 0 && 2 * 2 * (d * sizeof(T) + 32) + RING_OFFSET <= MAX_SMEM) {   // two rows of both arrays fit the ring
+    if (d <= MAX_ROW && rows > 0) {
         RowArgs a{};
         a.x = x; a.dy = dy; a.rows = rows; a.x_stride = xs; a.dy_stride = dys; a.out_stride = dxs; a.d = static_cast<int>(d); a.g = g;
         a.out = dx; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
@@ -688,11 +737,13 @@ int backward_typed(const void* dy, int64_t dys, const void* x, int64_t xs, int64
         const RowShape s = row_shape(&a, sizeof(T), 2);
         const bool vec = d * sizeof(T) % 16 == 0 && rows_aligned(x, xs, sizeof(T)) && rows_aligned(dy, dys, sizeof(T)) &&
                          rows_aligned(dx, dxs, sizeof(T));
-        if (cudaError_t e = vec ? backward_rows<T, W, true>(a, s, st) : backward_rows<T, W, false>(a, s, st); e != cudaSuccess)
-            return VPCE_CUDA_ERROR;
-        if (a.partial)
-            ln_backward_finish<W><<<col_tiles, COL_TILE * FIN_ROWS, 0, st>>>(partial, s.grid, d, static_cast<W*>(dg), static_cast<W*>(db));
-        return code(cudaGetLastError());
+        if (s.grid > 0) {
+            if (cudaError_t e = vec ? backward_rows<T, W, true>(a, s, st) : backward_rows<T, W, false>(a, s, st); e != cudaSuccess)
+                return VPCE_CUDA_ERROR;
+            if (a.partial)
+                ln_backward_finish<W><<<col_tiles, COL_TILE * FIN_ROWS, 0, st>>>(partial, s.grid, d, static_cast<W*>(dg), static_cast<W*>(db));
+            return code(cudaGetLastError());
+        }
     }
     if (dg || db) {
         ln_backward_columns<T><<<dim3(col_tiles, slices), COL_TILE * COL_ROWS, 0, st>>>(dyt, dys, xt, xs, rows, d, mean, rstd, partial);
