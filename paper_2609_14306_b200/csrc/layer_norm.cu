@@ -63,26 +63,14 @@ __device__ __forceinline__ float2 block_sum2(float a, float b, float2* part) {
 // ------------------------------------------------------------------------------------ row kernels
 constexpr int MAX_GROUP_WARPS = 16;
 // One block per SM.  Forward: 28 warps of 72 registers (a row's 32 elements a thread and what is worked on); backward: 16 warps
-// of 128 (the 64 column sums).
+// of 128 (64 column sums).
 constexpr int FORWARD_REGS = 72, FORWARD_WARPS = 28, BACKWARD_REGS = 128, BACKWARD_WARPS = 16;
 constexpr int MAX_GROUPS = FORWARD_WARPS;               // per block; a group of more than one warp has a named barrier
 constexpr int MAX_STAGES = 8;
 constexpr int MAX_EPT = 32;                             // elements per thread
 constexpr int MAX_SMEM = 227 * 1024;
+constexpr int64_t MAX_ROWS = (int64_t{1} << 31) - (1 << 20);   // row numbers and the look-ahead stay below 2^31
 constexpr int64_t MAX_ROW = 32 * MAX_GROUP_WARPS * MAX_EPT;
-
-struct RowArgs {
-    const void *x, *dy;                                 // dy: backward only
-    long rows, x_stride, dy_stride, out_stride;
-    int d, warps;                                       // warps per group
-    int groups, stages, cap;                            // groups per block, ring depth, bytes of a row in the ring
-    int ring;                                           // byte offset of the ring in shared memory
-    const void *g, *b;
-    float eps;
-    void* out;                                          // y or dx (may be null in the backward pass)
-    float *mean, *rstd;                                 // written (forward, may be null) or read (backward)
-    float* partial;                                     // [blocks][2][d] or null
-};
 
 struct Smem {                                           // of a block: barriers, reduction scratch; then weights, ring
     uint64_t full[MAX_GROUPS][MAX_STAGES];              // [group][stage]
@@ -95,22 +83,35 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
-// One array's rows as a group meets them: the address of the row to be fetched next and of the row in work.
+// An array's rows, as the launch gives them (used where needed rather than kept in registers).
 struct Rows {
-    const char* base;
-    size_t pitch;                                       // bytes between rows
-    __device__ __forceinline__ const char* at(long r) const { return base + static_cast<size_t>(r) * pitch; }
+    const void* base;
+    long pitch;                                         // bytes between rows
+    __device__ __forceinline__ const char* at(int r) const { return static_cast<const char*>(base) + r * pitch; }
     // bytes by which row r starts behind a 16-byte boundary
-    __device__ __forceinline__ uint32_t shift(long r) const {
+    __device__ __forceinline__ uint32_t shift(int r) const {
         return (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base)) + static_cast<uint32_t>(r) * static_cast<uint32_t>(pitch)) & 15u;
     }
+};
+
+struct RowArgs {
+    Rows x, dy;                                         // dy: backward only
+    int rows, d, warps;                                 // warps per group
+    int groups, stages, cap, slot;                      // groups per block, ring depth, bytes of a row and of a slot in the ring
+    int ring;                                           // byte offset of the ring in shared memory
+    long out_stride;
+    const void *g, *b;
+    float eps;
+    void* out;                                          // y or dx (may be null in the backward pass)
+    float *mean, *rstd;                                 // written (forward, may be null) or read (backward)
+    float* partial;                                     // [blocks][2][d] or null
 };
 
 // What row r of an array takes: `*from`, the address from which the bulk copy reads, `*at`, where it lands in the slot, and the
 // bytes that it moves.  The row's first element lands shift(r) bytes into the slot.  A granule that reaches over the tensor's
 // first or last byte is left to plain element copies, made here.
 template <typename T, bool VEC>
-__device__ __forceinline__ uint32_t copy_extent(const Rows& a, long r, long rows, int d, const char** from, uint32_t* at, uint8_t* slot) {
+__device__ __forceinline__ uint32_t copy_extent(const Rows& a, int r, int rows, int d, const char** from, uint32_t* at, uint8_t* slot) {
     const char* row = a.at(r);
     const size_t bytes = static_cast<size_t>(d) * sizeof(T);
     if (VEC) { *from = row; *at = 0; return static_cast<uint32_t>(bytes); }
@@ -131,18 +132,24 @@ __device__ __forceinline__ uint32_t copy_extent(const Rows& a, long r, long rows
     return static_cast<uint32_t>(e - b);
 }
 
-// One thread: row r of the NA arrays into ring slot `slot`, signalled on `bar`.
+// One thread: row r of the NA arrays into ring slot `slot`, signalled on `bar`.  With dy the row's mean and rstd come along, to
+// the slot's end (the barrier counts their arrival, too).
 template <typename T, bool VEC, int NA>
-__device__ __forceinline__ void fetch_row(const RowArgs& a, const Rows* in, long r, uint8_t* slot, uint32_t bar) {
+__device__ __forceinline__ void fetch_row(const RowArgs& a, int r, uint8_t* slot, uint32_t bar) {
     const char* from[NA];
     uint32_t at[NA], bytes[NA], total = 0;
 #pragma unroll
     for (int i = 0; i < NA; ++i) {
-        bytes[i] = copy_extent<T, VEC>(in[i], r, a.rows, a.d, &from[i], &at[i], slot + i * a.cap);
+        bytes[i] = copy_extent<T, VEC>(i ? a.dy : a.x, r, a.rows, a.d, &from[i], &at[i], slot + i * a.cap);
         total += bytes[i];
     }
-    vpce::mbar_arrive_expect_tx(bar, total);
     const uint32_t dst = vpce::smem_u32(slot);
+    if (NA == 2) {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + 2 * a.cap), "l"(a.mean + r) : "memory");
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + 2 * a.cap + 4), "l"(a.rstd + r) : "memory");
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
+    }
+    vpce::mbar_arrive_expect_tx(bar, total);
 #pragma unroll
     for (int i = 0; i < NA; ++i)
         if (bytes[i]) bulk_load(dst + i * a.cap + at[i], from[i], bytes[i], bar);
@@ -165,6 +172,12 @@ __device__ __forceinline__ float half_warp_sum(float v) {
     for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
+__device__ __forceinline__ float ld_shared(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
 // Pairs of fp32 in one 64-bit register.
 using f2 = unsigned long long;
 __device__ __forceinline__ f2 pair(float a, float b) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
@@ -280,8 +293,7 @@ template <typename T, bool VEC, int EPT> struct Columns {
 // What every row kernel sets up: the group's place and its ring.
 struct Group {
     int id, warp, lane;
-    Rows in[2];
-    long first, step;                                   // rows of this group: first, first + step, ...
+    int first, step;                                    // rows of this group: first, first + step, ...
     uint8_t* ring;
     uint32_t bars;
 };
@@ -292,22 +304,20 @@ __device__ __forceinline__ Group group_setup(const RowArgs& a, uint8_t* raw) {
     g.id = (threadIdx.x >> 5) / a.warps;
     g.warp = (threadIdx.x >> 5) - g.id * a.warps;
     g.lane = threadIdx.x & 31;
-    g.in[0] = Rows{static_cast<const char*>(a.x), static_cast<size_t>(a.x_stride) * sizeof(T)};
-    if (NA == 2) g.in[1] = Rows{static_cast<const char*>(a.dy), static_cast<size_t>(a.dy_stride) * sizeof(T)};
-    g.first = static_cast<long>(blockIdx.x) * a.groups + g.id;
-    g.step = static_cast<long>(gridDim.x) * a.groups;
-    g.ring = raw + a.ring + g.id * a.stages * NA * a.cap;
+    g.first = blockIdx.x * a.groups + g.id;
+    g.step = gridDim.x * a.groups;
+    g.ring = raw + a.ring + g.id * a.stages * a.slot;
     g.bars = vpce::smem_u32(&sm->full[g.id][0]);
     if (g.warp == 0 && g.lane == 0) {
-        for (int s = 0; s < a.stages; ++s) vpce::mbar_init(g.bars + 8 * s, 1);
+        for (int s = 0; s < a.stages; ++s) vpce::mbar_init(g.bars + 8 * s, NA);
         vpce::fence_barrier_init();
         vpce::fence_proxy_async();
     }
     group_sync(g.id, a.warps);
     if (g.warp == 0 && g.lane == 0)
         for (int s = 0; s < a.stages; ++s) {
-            const long r = g.first + s * g.step;
-            if (r < a.rows) fetch_row<T, VEC, NA>(a, g.in, r, g.ring + s * NA * a.cap, g.bars + 8 * s);
+            const int r = g.first + s * g.step;
+            if (r < a.rows) fetch_row<T, VEC, NA>(a, r, g.ring + s * a.slot, g.bars + 8 * s);
         }
     return g;
 }
@@ -333,10 +343,8 @@ __global__ void __maxnreg__(FORWARD_REGS) ln_forward_rows(const RowArgs a) {
     const float inv_lane = n_lane > 0.f ? 1.f / n_lane : 0.f;
     int s = 0, pass = 0, turn = 0;                                          // the warps take turns at starting copies
     uint32_t parity = 0;
-    T* out = static_cast<T*>(a.out) + g.first * a.out_stride;
-    const long out_step = g.step * a.out_stride;
-    for (long r = g.first; r < a.rows; r += g.step, out += out_step) {
-        const uint32_t xr = vpce::smem_u32(g.ring + s * a.cap) + (VEC ? 0u : g.in[0].shift(r));
+    for (int r = g.first; r < a.rows; r += g.step) {
+        const uint32_t xr = vpce::smem_u32(g.ring + s * a.slot) + (VEC ? 0u : a.x.shift(r));
         wait_row(g.bars + 8 * s, parity);
         f2 v[C::PAIRS];
 #pragma unroll
@@ -369,7 +377,7 @@ __global__ void __maxnreg__(FORWARD_REGS) ln_forward_rows(const RowArgs a) {
         if (g.lane == 0) part[pass][g.warp] = make_float2(sum, squares);
         group_sync(g.id, a.warps);
         // everyone has read the slot: it takes the next row that is not under way yet
-        if (g.warp == turn && g.lane == 0 && r + a.stages * g.step < a.rows) fetch_row<T, VEC, 1>(a, g.in, r + a.stages * g.step, g.ring + s * a.cap, g.bars + 8 * s);
+        if (g.warp == turn && g.lane == 0 && r + a.stages * g.step < a.rows) fetch_row<T, VEC, 1>(a, r + a.stages * g.step, g.ring + s * a.slot, g.bars + 8 * s);
         if (++turn == a.warps) turn = 0;
         if (++s == a.stages) { s = 0; parity ^= 1u; }
         // The row's statistics from the warps': squares around the row's mean = sum of theirs + n (their mean - the row's)^2.
@@ -378,14 +386,16 @@ __global__ void __maxnreg__(FORWARD_REGS) ln_forward_rows(const RowArgs a) {
         const float mu = half_warp_sum(w.x) * inv_d;
         const float off = w.x * inv_lane - mu;
         const float rs = 1.f / sqrtf(half_warp_sum(fmaf(n_lane * off, off, w.y)) * inv_d + a.eps);
-        const f2 minus_mu = pair(-mu, -mu), rs2 = pair(rs, rs);
+        // (x - mu) rs as x rs - mu rs: the rounding of mu rs is that of mu itself
+        const f2 minus_mu = pair(-mu * rs, -mu * rs), rs2 = pair(rs, rs);
+        T* out = static_cast<T*>(a.out) + r * a.out_stride;
 #pragma unroll
         for (int q = 0; q < EPT / 8; ++q) {
             f2 gq[4], bq[4];
             cols.weights(gw, q, gq);
             cols.weights(bw, q, bq);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[4 * q + i] = fma2(mul2(add2(v[4 * q + i], minus_mu), rs2), gq[i], bq[i]);
+            for (int i = 0; i < 4; ++i) v[4 * q + i] = fma2(fma2(v[4 * q + i], rs2, minus_mu), gq[i], bq[i]);
             cols.store(out, q, v + 4 * q);
         }
         if (g.warp == 0 && g.lane == 0) {
@@ -413,12 +423,13 @@ __global__ void __maxnreg__(BACKWARD_REGS) ln_backward_rows(const RowArgs a) {
     // The row is read from the ring twice, before and after the group's sums: the registers that would keep it hold the column
     // sums.  Weights of columns beyond d are 0, so those columns add nothing to the sums.  The first reading of a row comes
     // before the second reading of the row before it, so the group's barrier finds everyone with work in between.
-    auto slot_of = [&](int s) { return g.ring + s * 2 * a.cap; };
-    auto first_reading = [&](long r, int s, uint32_t parity, float mu, float rs, float2* to) {
+    auto slot_of = [&](int s) { return g.ring + s * a.slot; };
+    auto first_reading = [&](int r, int s, uint32_t parity, float2* to) {
         const uint32_t slot = vpce::smem_u32(slot_of(s));
-        const uint32_t xr = slot + (VEC ? 0u : g.in[0].shift(r)), dyr = slot + a.cap + (VEC ? 0u : g.in[1].shift(r));
-        const f2 minus_mu = pair(-mu, -mu), rs2 = pair(rs, rs);
+        const uint32_t xr = slot + (VEC ? 0u : a.x.shift(r)), dyr = slot + a.cap + (VEC ? 0u : a.dy.shift(r));
         wait_row(g.bars + 8 * s, parity);
+        const float mu = ld_shared(slot + 2 * a.cap), rs = ld_shared(slot + 2 * a.cap + 4);
+        const f2 minus_mu = pair(-mu * rs, -mu * rs), rs2 = pair(rs, rs);   // xh = x rs - mu rs
         f2 sa = 0ull, sax = 0ull;
 #pragma unroll
         for (int q = 0; q < EPT / 8; ++q) {
@@ -430,7 +441,7 @@ __global__ void __maxnreg__(BACKWARD_REGS) ln_backward_rows(const RowArgs a) {
             for (int i = 0; i < 4; ++i) {
                 const f2 t = mul2(u[i], gq[i]);
                 sa = add2(sa, t);
-                sax = fma2(t, mul2(add2(x[i], minus_mu), rs2), sax);
+                sax = fma2(t, fma2(x[i], rs2, minus_mu), sax);
             }
         }
         const float2 pa = split(sa), pax = split(sax);
@@ -440,13 +451,8 @@ __global__ void __maxnreg__(BACKWARD_REGS) ln_backward_rows(const RowArgs a) {
     if (g.first < a.rows) {
         int s = 0, pass = 0, turn = 0;                                      // the warps take turns at starting copies
         uint32_t parity = 0;
-        T* dx = static_cast<T*>(a.out) + g.first * a.out_stride;
-        const long out_step = g.step * a.out_stride;
-        // the statistics of a row are loaded two rows ahead
-        float mu = a.mean[g.first], rs = a.rstd[g.first], mu_next = 0.f, rs_next = 0.f;
-        if (g.first + g.step < a.rows) { mu_next = a.mean[g.first + g.step]; rs_next = a.rstd[g.first + g.step]; }
-        first_reading(g.first, 0, 0u, mu, rs, part[0]);
-        for (long r = g.first; r < a.rows; r += g.step, dx += out_step) {
+        first_reading(g.first, 0, 0u, part[0]);
+        for (int r = g.first; r < a.rows; r += g.step) {
             group_sync(g.id, a.warps);
             float2 t = make_float2(0.f, 0.f);
             if ((g.lane & 15) < a.warps) t = part[pass][g.lane & 15];
@@ -458,16 +464,16 @@ __global__ void __maxnreg__(BACKWARD_REGS) ln_backward_rows(const RowArgs a) {
             // the slot of the row before is spent: it takes the next row that is not under way yet
             if (g.warp == turn && g.lane == 0 && r > g.first && r + (a.stages - 1) * g.step < a.rows) {
                 const int before = here == 0 ? a.stages - 1 : here - 1;
-                fetch_row<T, VEC, 2>(a, g.in, r + (a.stages - 1) * g.step, slot_of(before), g.bars + 8 * before);
+                fetch_row<T, VEC, 2>(a, r + (a.stages - 1) * g.step, slot_of(before), g.bars + 8 * before);
             }
             if (++turn == a.warps) turn = 0;
-            float mu_later = 0.f, rs_later = 0.f;
-            if (r + 2 * g.step < a.rows) { mu_later = a.mean[r + 2 * g.step]; rs_later = a.rstd[r + 2 * g.step]; }
-            if (r + g.step < a.rows) first_reading(r + g.step, s, parity, mu_next, rs_next, part[pass]);
+            if (r + g.step < a.rows) first_reading(r + g.step, s, parity, part[pass]);
             const uint32_t slot = vpce::smem_u32(slot_of(here));
-            const uint32_t xr = slot + (VEC ? 0u : g.in[0].shift(r)), dyr = slot + a.cap + (VEC ? 0u : g.in[1].shift(r));
-            const float ma = -t.x * inv_d, mx = -t.y * inv_d;
-            const f2 minus_mu = pair(-mu, -mu), rs2 = pair(rs, rs), ma2 = pair(ma, ma), mx2 = pair(mx, mx);
+            const uint32_t xr = slot + (VEC ? 0u : a.x.shift(r)), dyr = slot + a.cap + (VEC ? 0u : a.dy.shift(r));
+            const float mu = ld_shared(slot + 2 * a.cap), rs = ld_shared(slot + 2 * a.cap + 4);
+            const float ma = -rs * t.x * inv_d, mx = -rs * t.y * inv_d;
+            const f2 minus_mu = pair(-mu * rs, -mu * rs), rs2 = pair(rs, rs), ma2 = pair(ma, ma), mx2 = pair(mx, mx);
+            T* dx = static_cast<T*>(a.out) + r * a.out_stride;
 #pragma unroll
             for (int q = 0; q < EPT / 8; ++q) {
                 f2 x[4], u[4], gq[4];
@@ -476,15 +482,13 @@ __global__ void __maxnreg__(BACKWARD_REGS) ln_backward_rows(const RowArgs a) {
                 cols.weights(gw, q, gq);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const f2 xh = mul2(add2(x[i], minus_mu), rs2);
+                    const f2 xh = fma2(x[i], rs2, minus_mu);
                     dg[4 * q + i] = fma2(u[i], xh, dg[4 * q + i]);
                     db[4 * q + i] = add2(u[i], db[4 * q + i]);
-                    x[i] = mul2(rs2, fma2(xh, mx2, add2(mul2(u[i], gq[i]), ma2)));
+                    x[i] = fma2(mul2(u[i], gq[i]), rs2, fma2(xh, mx2, ma2));
                 }
                 if (a.out) cols.store(dx, q, x);
             }
-            mu = mu_next; rs = rs_next;
-            mu_next = mu_later; rs_next = rs_later;
         }
     }
     if (!a.partial) return;
@@ -664,10 +668,11 @@ RowShape row_shape(RowArgs* a, size_t elem, int na) {
     while (a->groups > 1 && static_cast<int64_t>(a->groups - 1) * sm_count() >= a->rows) --a->groups;   // few rows: spread over the SMs
     a->cap = static_cast<int>((a->d * elem + 15) / 16 * 16 + 16);
     a->ring = WEIGHTS_OFFSET + (na == 1 ? 2 : 1) * 4 * 32 * s.ept * a->warps;
-    while (a->groups > 1 && a->ring + a->groups * 2 * na * a->cap > MAX_SMEM) --a->groups;
-    a->stages = std::min(MAX_STAGES, (MAX_SMEM - a->ring) / (a->groups * na * a->cap));
+    a->slot = na * a->cap + (na == 2 ? 16 : 0);
+    while (a->groups > 1 && a->ring + a->groups * 2 * a->slot > MAX_SMEM) --a->groups;
+    a->stages = std::min(MAX_STAGES, (MAX_SMEM - a->ring) / (a->groups * a->slot));
     s.threads = 32 * a->warps * a->groups;
-    s.smem = a->ring + a->groups * a->stages * na * a->cap;
+    s.smem = a->ring + a->groups * a->stages * a->slot;
     if (na == 2) s.smem = std::max<int>(s.smem, a->ring + 8 * a->d * a->groups);    // the groups' sums take its place
     const int64_t blocks = (a->rows + a->groups - 1) / a->groups;
     s.grid = a->stages >= 2 && s.smem <= MAX_SMEM ? static_cast<int>(std::min<int64_t>(blocks, std::min(sm_count(), MAX_SLICES))) : 0;
@@ -710,9 +715,9 @@ int code(cudaError_t e) { return e == cudaSuccess ? VPCE_OK : VPCE_CUDA_ERROR; }
 template <typename T, typename W>
 int forward_typed(const void* x, int64_t rows, int64_t d, int64_t xs, const void* g, const void* b, float eps, void* y, int64_t ys,
                   float* mean, float* rstd, cudaStream_t st) {
-    if (d <= MAX_ROW) {
+    if (d <= MAX_ROW && rows <= MAX_ROWS) {
         RowArgs a{};
-        a.x = x; a.rows = rows; a.x_stride = xs; a.out_stride = ys; a.d = static_cast<int>(d); a.g = g; a.b = b; a.eps = eps; a.out = y;
+        a.x = Rows{x, static_cast<long>(xs * sizeof(T))}; a.rows = static_cast<int>(rows); a.out_stride = ys; a.d = static_cast<int>(d); a.g = g; a.b = b; a.eps = eps; a.out = y;
         a.mean = mean; a.rstd = rstd;
         const RowShape s = row_shape(&a, sizeof(T), 1);
         const bool vec = d * sizeof(T) % 16 == 0 && rows_aligned(x, xs, sizeof(T)) && rows_aligned(y, ys, sizeof(T));
@@ -729,9 +734,10 @@ int backward_typed(const void* dy, int64_t dys, const void* x, int64_t xs, int64
     const T *dyt = static_cast<const T*>(dy), *xt = static_cast<const T*>(x);
     const unsigned col_tiles = static_cast<unsigned>((d + COL_TILE - 1) / COL_TILE);
     int slices = slices_for(rows);
-    if (d <= MAX_ROW && rows > 0) {
+    if (d <= MAX_ROW && rows > 0 && rows <= MAX_ROWS) {
         RowArgs a{};
-        a.x = x; a.dy = dy; a.rows = rows; a.x_stride = xs; a.dy_stride = dys; a.out_stride = dxs; a.d = static_cast<int>(d); a.g = g;
+        a.x = Rows{x, static_cast<long>(xs * sizeof(T))}; a.dy = Rows{dy, static_cast<long>(dys * sizeof(T))};
+        a.rows = static_cast<int>(rows); a.out_stride = dxs; a.d = static_cast<int>(d); a.g = g;
         a.out = dx; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
         a.partial = dg || db ? partial : nullptr;
         const RowShape s = row_shape(&a, sizeof(T), 2);
