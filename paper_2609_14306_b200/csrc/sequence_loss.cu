@@ -6,9 +6,15 @@
 // its piece (`first`: the piece of the sequence that reaches into the tile from before, `last`: of the one that leaves it at
 // the end).  One block then joins the pieces in the order of the tiles, forms the loss and a weight per sequence; a third
 // pass over the tokens writes the gradient.
+//
+// These are latencies, not bandwidth (22 MB at 2^20 tokens: 3.4 us).  Up to SMALL_T tokens in SMALL_SEQS sequences one block
+// does it all in one launch: its warps keep their tokens in registers and everything between the passes in shared memory.
+// Beyond, each pass is a launch that starts while the one before drains (programmatic launch) and first reads what does not
+// depend on it.
 
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "sequence_loss.h"
@@ -18,9 +24,11 @@ namespace {
 
 constexpr int THREADS = 128;                    // four warps, each with a tile of its own
 constexpr int WARPS = THREADS / 32;
-constexpr int PER_LANE = 8;                     // tokens of one lane in a step: a step covers 256 tokens
+constexpr int64_t SMALL_T = 8192, SMALL_SEQS = 1024;   // of the one-block kernel: 32 warps with 256 tokens each
+constexpr int PER_LANE = 4;                     // tokens of one lane in a step: a step covers 128 tokens
 constexpr int STEP = 32 * PER_LANE;
-constexpr int64_t MAX_TILES = 2048;             // the tile grows with T beyond 512 Ki tokens: bounds what one block joins
+constexpr int SMALL_PER_LANE = 8, SMALL_TILE = 32 * SMALL_PER_LANE;   // of the one-block kernel
+constexpr int64_t MAX_TILES = 4096;             // the tile grows with T beyond 2^19 tokens: bounds what one block joins
 constexpr int FIN_THREADS = 1024;
 constexpr unsigned ALL = 0xffffffffu;
 
@@ -30,13 +38,14 @@ struct SeqArgs {
     const uint8_t* mask;
     const int64_t* offsets;
     long T, n_seqs;
-    int steps;                                  // steps of 256 tokens per tile
+    long span;                                  // tokens per tile
     long n_tiles;
     int adv_per_token, by_seq;                  // by_seq: the loss needs sums per sequence
     float lo, hi, kl_coef;
     float2 *first, *last;                       // [n_tiles] pieces: (sum, count)
     float2* seq_sum;                            // [n_seqs] (sum, count)
-    float* tile_stats;                          // [5][n_tiles] count, sum of l, KL, clipped, r
+    float* tile_stats;                          // [5][n_stats] count, sum of l, KL, clipped, r of a block's (or warp's) tiles
+    long n_stats;
     float* weight;                              // [n_seqs + 1] weight of a sequence's tokens; the last: of every token
     // preference
     double beta, margin, smoothing;
@@ -56,19 +65,29 @@ __device__ __forceinline__ long seq_begin(const SeqArgs& a, long s) {
     return v < 0 ? 0 : v > a.T ? a.T : v;
 }
 
-// The first sequence that ends behind token t (n_seqs if none does): 32 probes a round.
+// The first sequence that ends behind token t (n_seqs if none does): 256 probes a round, so one round of loads for up to 256
+// sequences and two for 65536.
 __device__ __forceinline__ long first_seq(const SeqArgs& a, long t, int lane) {
+    constexpr int PROBES = 8;
     long lo = 0, hi = a.n_seqs;                 // the answer is in [lo, hi]
     while (hi > lo) {
-        const long step = (hi - lo + 31) / 32;
-        const long probe = lo + step * (lane + 1) - 1;
-        const bool beyond = probe >= hi || seq_begin(a, probe + 1) > t;   // the answer is <= probe
-        const unsigned ball = __ballot_sync(ALL, beyond);
-        const int k = ball ? __ffs(ball) - 1 : 32;
-        const long nlo = lo + step * k;
-        const long nhi = k == 32 ? hi : lo + step * (k + 1) - 1;
+        const long step = (hi - lo + 32 * PROBES - 1) / (32 * PROBES);
+        // this lane's probes: the ends of its PROBES pieces of `step` sequences; how many of them does t lie behind?
+        long begin[PROBES];
+#pragma unroll
+        for (int k = 0; k < PROBES; ++k) {
+            const long probe = lo + step * (lane * PROBES + k + 1) - 1;
+            begin[k] = probe < hi ? seq_begin(a, probe + 1) : a.T + 1;
+        }
+        int behind = 0;
+#pragma unroll
+        for (int k = 0; k < PROBES; ++k) behind += begin[k] <= t ? 1 : 0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) behind += __shfl_xor_sync(ALL, behind, o);
+        const long nlo = lo + step * behind, nhi = nlo + step - 1;
         lo = nlo < hi ? nlo : hi;
         hi = nhi < hi ? nhi : hi;
+        if (step == 1) hi = lo;                 // every sequence was probed
     }
     return lo;
 }
@@ -92,6 +111,34 @@ __device__ __forceinline__ Policy policy_token(const SeqArgs& a, float logp, flo
     return p;
 }
 
+// Waits for the kernel before this one in the stream (a no-op where the launch did not ask for an early start).
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Lets the kernel behind this one start.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// N tokens of a lane, read whether their mask says so or not (one memory latency instead of two; what lies under the mask
+// is not used): those at base + i + 32 j + lane that lie before base + e.  i, e: offsets inside a tile, in 32 bits.
+template <bool POLICY, bool VALUES, int N> struct Tokens {
+    bool on[N];
+    float logp[N], old_logp[N], ref[N], adv[N];
+    __device__ __forceinline__ void load(const SeqArgs& a, long base, int i, int e, int lane, float adv_s) {
+        const int at = i + lane;
+        const uint8_t* mask = a.mask ? a.mask + base + at : nullptr;
+        const float *lp = a.logp + base + at, *op = a.old_logp + base + at, *rp = a.ref_logp + base + at, *ap = a.adv + base + at;
+        const bool has_ref = VALUES && a.ref_logp, has_adv = VALUES && POLICY && a.adv_per_token;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const bool in = at + j * 32 < e;
+            on[j] = in;
+            if (mask && in) on[j] = mask[j * 32] != 0;
+            logp[j] = VALUES && in ? lp[j * 32] : 0.f;
+            old_logp[j] = VALUES && POLICY && in ? op[j * 32] : 0.f;
+            ref[j] = has_ref && in ? rp[j * 32] : 0.f;
+            adv[j] = has_adv && in ? ap[j * 32] : adv_s;
+        }
+    }
+};
+
 // Calls f(s, begin, end) for every sequence s that meets the tokens [t0, t1), with its range cut to them.
 template <typename F>
 __device__ __forceinline__ void for_sequences(const SeqArgs& a, long t0, long t1, int lane, F f) {
@@ -102,34 +149,30 @@ __device__ __forceinline__ void for_sequences(const SeqArgs& a, long t0, long t1
     }
 }
 
-// Pass 1: sums of each tile.  POLICY: value = l and the four statistics; else value = logp - ref_logp.
+// Pass 1: sums of one tile, by one warp.  POLICY: value = l and the four statistics; else value = logp - ref_logp.
 template <bool POLICY>
-__global__ void __launch_bounds__(THREADS) seq_sums_kernel(const SeqArgs a) {
-    const int lane = threadIdx.x & 31;
-    const long tile = static_cast<long>(blockIdx.x) * WARPS + (threadIdx.x >> 5);
-    if (tile >= a.n_tiles) return;                                          // the whole warp
-    const long span = static_cast<long>(a.steps) * STEP;
-    const long t0 = tile * span, t1 = t0 + span < a.T ? t0 + span : a.T;
+__device__ __forceinline__ void sum_tile(const SeqArgs& a, long tile, int lane, float (&stats)[5]) {
+    const long t0 = tile * a.span, t1 = t0 + a.span < a.T ? t0 + a.span : a.T;
     float2 first = make_float2(0.f, 0.f), last = first;
     float cnt = 0.f, sl = 0.f, skl = 0.f, sclip = 0.f, sr = 0.f;
     for_sequences(a, t0, t1, lane, [&](long s, long sb, long se) {
         const long b = sb > t0 ? sb : t0, e = se < t1 ? se : t1;
         const float adv_s = POLICY && !a.adv_per_token ? a.adv[s] : 0.f;
         float sum = 0.f, n = 0.f;
-        for (long c = b; c < e; c += STEP) {
+        const int end = static_cast<int>(e - t0);
+        for (int c = static_cast<int>(b - t0); c < end; c += STEP) {
+            Tokens<POLICY, true, PER_LANE> k;
+            k.load(a, t0, c, end, lane, adv_s);
 #pragma unroll
             for (int j = 0; j < PER_LANE; ++j) {
-                const long t = c + j * 32 + lane;
-                if (t < e && (!a.mask || a.mask[t])) {
-                    n += 1.f;
-                    if (POLICY) {
-                        const Policy p = policy_token(a, a.logp[t], a.old_logp[t], a.ref_logp ? a.ref_logp[t] : 0.f,
-                                                      a.adv_per_token ? a.adv[t] : adv_s);
-                        sum += p.l;
-                        skl += p.kl; sclip += p.clipped; sr += p.r;
-                    } else {
-                        sum += a.logp[t] - (a.ref_logp ? a.ref_logp[t] : 0.f);
-                    }
+                if (!k.on[j]) continue;
+                n += 1.f;
+                if (POLICY) {
+                    const Policy p = policy_token(a, k.logp[j], k.old_logp[j], k.ref[j], k.adv[j]);
+                    sum += p.l;
+                    skl += p.kl; sclip += p.clipped; sr += p.r;
+                } else {
+                    sum += k.logp[j] - k.ref[j];
                 }
             }
         }
@@ -142,31 +185,25 @@ __global__ void __launch_bounds__(THREADS) seq_sums_kernel(const SeqArgs a) {
         cnt += n; sl += sum;
     });
     if (a.by_seq && lane == 0) { a.first[tile] = first; a.last[tile] = last; }
-    if (POLICY) {
-        cnt = wsum(cnt); sl = wsum(sl); skl = wsum(skl); sclip = wsum(sclip); sr = wsum(sr);
-        if (lane == 0) {
-            float* o = a.tile_stats + tile;
-            o[0] = cnt; o[a.n_tiles] = sl; o[2 * a.n_tiles] = skl; o[3 * a.n_tiles] = sclip; o[4 * a.n_tiles] = sr;
-        }
-    }
+    if (POLICY) { stats[0] = wsum(cnt); stats[1] = wsum(sl); stats[2] = wsum(skl); stats[3] = wsum(sclip); stats[4] = wsum(sr); }
 }
 
+__device__ __forceinline__ double wsum(double v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(ALL, v, o);
+    return v;
+}
 // Sums of K doubles over the block (fixed order); every thread receives them.
 template <int K>
 __device__ __forceinline__ void block_sum(double (&v)[K], double (*part)[K]) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(ALL, v[k], o);
+    for (int k = 0; k < K; ++k) v[k] = wsum(v[k]);
+    if (lane == 0)
+        for (int k = 0; k < K; ++k) part[warp][k] = v[k];
     __syncthreads();
-    if ((threadIdx.x & 31) == 0)
-        for (int k = 0; k < K; ++k) part[threadIdx.x >> 5][k] = v[k];
-    __syncthreads();
-    for (int k = 0; k < K; ++k) {
-        v[k] = part[threadIdx.x & 31][k];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(ALL, v[k], o);
-    }
+    for (int k = 0; k < K; ++k) v[k] = wsum(lane < warps ? part[lane][k] : 0.0);
 }
 
 // (sum, count) of sequence s by the lanes of a group of `width` lanes (a power of two up to 32), pieces in a fixed order.
@@ -175,13 +212,13 @@ __device__ __forceinline__ double2 join_pieces(const SeqArgs& a, long s, int sub
     if (s < a.n_seqs) {
         const long b = seq_begin(a, s), e = seq_begin(a, s + 1);
         if (e > b) {
-            const long span = static_cast<long>(a.steps) * STEP;
-            const long ta = b / span, tb = (e - 1) / span;
+            const long ta = b / a.span, tb = (e - 1) / a.span;
             if (ta == tb) {
                 // inside one tile: finished there
                 if (sub == 0) { const float2 f = a.seq_sum[s]; v.x = f.x; v.y = f.y; }
             } else {
                 if (sub == 0) { const float2 f = a.last[ta]; v.x = f.x; v.y = f.y; }
+#pragma unroll 4
                 for (long t = ta + 1 + sub; t <= tb; t += width) { const float2 f = a.first[t]; v.x += f.x; v.y += f.y; }
             }
         }
@@ -196,22 +233,25 @@ __device__ __forceinline__ double2 join_pieces(const SeqArgs& a, long s, int sub
 // Lanes that join one sequence's pieces: enough that all sequences are in flight at once, 32 at most.
 __device__ __forceinline__ int join_width(long n_seqs) {
     int w = 32;
-    while (w > 1 && static_cast<long>(FIN_THREADS / w) < n_seqs) w >>= 1;
+    while (w > 1 && static_cast<long>(blockDim.x / w) < n_seqs) w >>= 1;
     return w;
 }
 
-__global__ void __launch_bounds__(FIN_THREADS) policy_finish_kernel(const SeqArgs a) {
-    __shared__ double part[32][5];
-    __shared__ double part2[32][2];
-    double v[5] = {0, 0, 0, 0, 0};
-    for (long t = threadIdx.x; t < a.n_tiles; t += FIN_THREADS)
-#pragma unroll
-        for (int k = 0; k < 5; ++k) v[k] += a.tile_stats[k * a.n_tiles + t];
-    block_sum<5>(v, part);
-    const double inv = v[0] > 0 ? 1.0 / v[0] : 0.0;
-    double loss = v[1] * inv;
+// Pass 2, by one block of FIN_THREADS.
+__device__ __forceinline__ void policy_finish(const SeqArgs& a) {
+    __shared__ double total[5];
+    __shared__ double part[32][2];
+    // one warp (or, in a block of fewer than five, a few turns) for each of the five sums
+    for (int k = threadIdx.x >> 5; k < 5; k += blockDim.x >> 5) {
+        double t = 0.0;
+#pragma unroll 8
+        for (long i = threadIdx.x & 31; i < a.n_stats; i += 32) t += a.tile_stats[k * a.n_stats + i];
+        t = wsum(t);
+        if ((threadIdx.x & 31) == 0) total[k] = t;
+    }
+    double loss = 0.0;
     if (a.by_seq) {
-        const int width = join_width(a.n_seqs), per_round = FIN_THREADS / width;
+        const int width = join_width(a.n_seqs), per_round = blockDim.x / width;
         double u[2] = {0, 0};                                               // sum of the sequences' means, sequences that have one
         for (long s0 = 0; s0 < a.n_seqs; s0 += per_round) {
             const long s = s0 + threadIdx.x / width;
@@ -221,7 +261,7 @@ __global__ void __launch_bounds__(FIN_THREADS) policy_finish_kernel(const SeqArg
                 if (w.y > 0) { u[0] += w.x / w.y; u[1] += 1.0; }
             }
         }
-        block_sum<2>(u, part2);
+        block_sum<2>(u, part);
         loss = u[1] > 0 ? u[0] / u[1] : 0.0;
         for (long s0 = 0; s0 < a.n_seqs; s0 += per_round) {                 // each thread meets the entries that it wrote
             const long s = s0 + threadIdx.x / width;
@@ -231,19 +271,22 @@ __global__ void __launch_bounds__(FIN_THREADS) policy_finish_kernel(const SeqArg
             }
         }
     }
+    __syncthreads();
     if (threadIdx.x == 0) {
+        const double inv = total[0] > 0 ? 1.0 / total[0] : 0.0;
+        if (!a.by_seq) loss = total[1] * inv;
         a.weight[a.n_seqs] = static_cast<float>(inv);
         a.stats[0] = static_cast<float>(loss);
-        a.stats[1] = static_cast<float>(v[2] * inv);
-        a.stats[2] = static_cast<float>(v[3] * inv);
-        a.stats[3] = static_cast<float>(v[4] * inv);
+        a.stats[1] = static_cast<float>(total[2] * inv);
+        a.stats[2] = static_cast<float>(total[3] * inv);
+        a.stats[3] = static_cast<float>(total[4] * inv);
     }
 }
 
-__global__ void __launch_bounds__(FIN_THREADS) preference_finish_kernel(const SeqArgs a) {
+__device__ __forceinline__ void preference_finish(const SeqArgs& a) {
     __shared__ double part[32][3];
     const long pairs = a.n_seqs / 2;
-    const int width = join_width(a.n_seqs), per_round = FIN_THREADS / width;
+    const int width = join_width(a.n_seqs), per_round = blockDim.x / width;
     for (long s0 = 0; s0 < a.n_seqs; s0 += per_round) {
         const long s = s0 + threadIdx.x / width;
         const double2 w = join_pieces(a, s, threadIdx.x % width, width);
@@ -255,72 +298,168 @@ __global__ void __launch_bounds__(FIN_THREADS) preference_finish_kernel(const Se
     }
     __syncthreads();
     double v[3] = {0, 0, 0};
-    for (long i = threadIdx.x; i < pairs; i += FIN_THREADS) {
+    for (long i = threadIdx.x; i < pairs; i += blockDim.x) {
         const float2 c = a.seq_sum[i], r = a.seq_sum[pairs + i];
-        const double diff = static_cast<double>(c.x) - static_cast<double>(r.x);
-        double l, slope;
+        const float diff = c.x - r.x;
+        float l, slope;
         if (a.kind == VPCE_PREF_SIGMOID) {
-            const double z = a.beta * diff - a.margin;
-            const double tail = log1p(exp(-fabs(z)));                       // log(1 + e^-|z|)
-            const double neg = (z < 0 ? -z : 0.0) + tail;                   // -log sigmoid(z)
-            const double pos = (z > 0 ? z : 0.0) + tail;                    // -log sigmoid(-z)
-            l = (1.0 - a.smoothing) * neg + a.smoothing * pos;
-            slope = a.beta * (a.smoothing - 1.0 / (1.0 + exp(z)));
+            const float z = static_cast<float>(a.beta) * diff - static_cast<float>(a.margin), eps = static_cast<float>(a.smoothing);
+            const float tail = log1pf(expf(-fabsf(z)));                     // log(1 + e^-|z|)
+            const float neg = (z < 0.f ? -z : 0.f) + tail;                  // -log sigmoid(z)
+            const float pos = (z > 0.f ? z : 0.f) + tail;                   // -log sigmoid(-z)
+            l = (1.f - eps) * neg + eps * pos;
+            slope = static_cast<float>(a.beta) * (eps - 1.f / (1.f + expf(z)));
         } else {
-            const double g = diff - 1.0 / (2.0 * a.beta);
+            const float g = diff - static_cast<float>(1.0 / (2.0 * a.beta));
             l = g * g;
-            slope = 2.0 * g;
+            slope = 2.f * g;
         }
         v[0] += l;
-        v[1] += diff > 0 ? 1.0 : 0.0;
+        v[1] += diff > 0.f ? 1.0 : 0.0;
         v[2] += a.beta * diff;
-        slope /= static_cast<double>(pairs);
-        a.weight[i] = static_cast<float>(slope / c.y);
-        a.weight[pairs + i] = static_cast<float>(-slope / r.y);
+        slope /= static_cast<float>(pairs);
+        a.weight[i] = slope / c.y;
+        a.weight[pairs + i] = -slope / r.y;
     }
     block_sum<3>(v, part);
     if (threadIdx.x == 0)
         for (int k = 0; k < 3; ++k) a.stats[k] = pairs > 0 ? static_cast<float>(v[k] / static_cast<double>(pairs)) : 0.f;
 }
 
-// Pass 3: the gradient of every token.
+// Pass 3: the gradient of one tile's tokens, by one warp.
 template <bool POLICY>
-__global__ void __launch_bounds__(THREADS) seq_grad_kernel(const SeqArgs a) {
-    const int lane = threadIdx.x & 31;
-    const long tile = static_cast<long>(blockIdx.x) * WARPS + (threadIdx.x >> 5);
-    if (tile >= a.n_tiles) return;
-    const long span = static_cast<long>(a.steps) * STEP;
-    const long t0 = tile * span, t1 = t0 + span < a.T ? t0 + span : a.T;
-    const float up = a.upstream ? *a.upstream : 1.f;
-    const float w_all = POLICY && !a.by_seq ? a.weight[a.n_seqs] * up : 0.f;
+__device__ __forceinline__ void grad_tile(const SeqArgs& a, long tile, int lane) {
+    const long t0 = tile * a.span, t1 = t0 + a.span < a.T ? t0 + a.span : a.T;
     long done = t0;                                                         // everything before is written
     auto zeros = [&](long to) { for (long t = done + lane; t < to; t += 32) a.dlogp[t] = 0.f; };
     for_sequences(a, t0, t1, lane, [&](long s, long sb, long se) {
         const long b = sb > t0 ? sb : t0, e = se < t1 ? se : t1;
         if (b < done) return;                                               // offsets that do not rise: every token is written once
         zeros(b);
-        const float w = POLICY && !a.by_seq ? w_all : a.weight[s] * up;
         const float adv_s = POLICY && !a.adv_per_token ? a.adv[s] : 0.f;
-        for (long c = b; c < e; c += STEP) {
+        const int end = static_cast<int>(e - t0);
+        float* out = a.dlogp + t0 + lane;
+        for (int c = static_cast<int>(b - t0); c < end; c += STEP) {
+            Tokens<POLICY, POLICY, PER_LANE> k;
+            k.load(a, t0, c, end, lane, adv_s);
+            wait_for_previous();                                            // the weights come from pass 2
+            const float w = a.weight[POLICY && !a.by_seq ? a.n_seqs : s] * (a.upstream ? *a.upstream : 1.f);
 #pragma unroll
             for (int j = 0; j < PER_LANE; ++j) {
-                const long t = c + j * 32 + lane;
-                if (t < e) {
-                    float g = 0.f;
-                    if (!a.mask || a.mask[t]) {
-                        if (POLICY)
-                            g = w * policy_token(a, a.logp[t], a.old_logp[t], a.ref_logp ? a.ref_logp[t] : 0.f,
-                                                 a.adv_per_token ? a.adv[t] : adv_s).grad;
-                        else
-                            g = w;
-                    }
-                    a.dlogp[t] = g;
-                }
+                if (c + j * 32 + lane < end)
+                    out[c + j * 32] = !k.on[j] ? 0.f : POLICY ? w * policy_token(a, k.logp[j], k.old_logp[j], k.ref[j], k.adv[j]).grad : w;
             }
         }
         done = e;
     });
     zeros(t1);
+}
+
+// Eight blocks an SM: all tiles run at once.
+template <bool POLICY> __global__ void __launch_bounds__(THREADS, 8) seq_sums_kernel(const SeqArgs a) {
+    __shared__ float part[WARPS][5];
+    let_next_start();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long tile = static_cast<long>(blockIdx.x) * WARPS + warp;
+    float stats[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
+    if (tile < a.n_tiles) sum_tile<POLICY>(a, tile, lane, stats);
+    if (!POLICY) return;
+    if (lane == 0)
+        for (int k = 0; k < 5; ++k) part[warp][k] = stats[k];
+    __syncthreads();
+    if (threadIdx.x < 5) {
+        float v = 0.f;
+        for (int w = 0; w < WARPS; ++w) v += part[w][threadIdx.x];
+        a.tile_stats[threadIdx.x * a.n_stats + blockIdx.x] = v;
+    }
+}
+template <bool POLICY> __global__ void __launch_bounds__(FIN_THREADS) seq_finish_kernel(const SeqArgs a) {
+    let_next_start();
+    wait_for_previous();
+    if (POLICY) policy_finish(a); else preference_finish(a);
+}
+template <bool POLICY> __global__ void __launch_bounds__(THREADS, 8) seq_grad_kernel(const SeqArgs a) {
+    const long tile = static_cast<long>(blockIdx.x) * WARPS + (threadIdx.x >> 5);
+    if (tile < a.n_tiles) grad_tile<POLICY>(a, tile, threadIdx.x & 31);
+    wait_for_previous();                                                    // what follows this kernel follows pass 2 as well
+}
+// All passes of a small call: a warp's 256 tokens stay in registers, the sequences and what joins the passes in shared memory.
+template <bool POLICY> __global__ void __launch_bounds__(FIN_THREADS) seq_small_kernel(const SeqArgs a) {
+    __shared__ int64_t offsets[SMALL_SEQS + 1];
+    __shared__ float2 seq_sum[SMALL_SEQS], first[32], last[32];
+    __shared__ float weight[SMALL_SEQS + 1], adv[SMALL_SEQS], tile_stats[5 * 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = static_cast<int>(a.n_seqs);
+    const int t0 = warp * SMALL_TILE, t1 = min(t0 + SMALL_TILE, static_cast<int>(a.T));
+    Tokens<POLICY, true, SMALL_PER_LANE> k;
+    k.load(a, 0, t0, t1, lane, 0.f);                                        // nothing where t0 >= T
+    const float up = a.upstream ? *a.upstream : 1.f;
+    for (int i = threadIdx.x; i <= n; i += blockDim.x) offsets[i] = seq_begin(a, i);
+    for (int i = threadIdx.x; i < n; i += blockDim.x) seq_sum[i] = make_float2(0.f, 0.f);   // of offsets that do not rise nobody may write it
+    if (POLICY && !a.adv_per_token)
+        for (int i = threadIdx.x; i < n; i += blockDim.x) adv[i] = a.adv[i];
+    __syncthreads();
+    // the sequence of each token: the last that begins at or before it, if it also ends behind it
+    int seq[SMALL_PER_LANE];
+#pragma unroll
+    for (int j = 0; j < SMALL_PER_LANE; ++j) {
+        const int t = t0 + j * 32 + lane;
+        int lo = 0, hi = n;                                                 // first sequence that ends behind t
+        while (lo < hi) { const int mid = (lo + hi) >> 1; if (offsets[mid + 1] > t) hi = mid; else lo = mid + 1; }
+        seq[j] = lo < n && offsets[lo] <= t && t < t1 ? lo : -1;
+        k.on[j] = k.on[j] && seq[j] >= 0;
+    }
+    float value[SMALL_PER_LANE], grad[SMALL_PER_LANE], st[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < SMALL_PER_LANE; ++j) {
+        value[j] = grad[j] = 0.f;
+        if (!k.on[j]) continue;
+        if (POLICY) {
+            const Policy p = policy_token(a, k.logp[j], k.old_logp[j], k.ref[j], a.adv_per_token ? k.adv[j] : adv[seq[j]]);
+            value[j] = p.l; grad[j] = p.grad;
+            st[0] += 1.f; st[1] += p.l; st[2] += p.kl; st[3] += p.clipped; st[4] += p.r;
+        } else {
+            value[j] = k.logp[j] - k.ref[j];
+        }
+    }
+    SeqArgs b = a;                                                          // the same, with what lies in shared memory here
+    b.offsets = offsets; b.seq_sum = seq_sum; b.first = first; b.last = last; b.weight = weight; b.tile_stats = tile_stats;
+    b.span = SMALL_TILE; b.n_stats = blockDim.x >> 5;
+    if (POLICY) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+            st[i] = wsum(st[i]);
+            if (lane == 0) tile_stats[i * b.n_stats + warp] = st[i];
+        }
+    }
+    if (a.by_seq && t0 < t1) {
+        float2 head = make_float2(0.f, 0.f), tail = head;
+        int s = 1 << 30, s_end = -1;                                        // sequences of this tile
+#pragma unroll
+        for (int j = 0; j < SMALL_PER_LANE; ++j) { if (seq[j] >= 0) { s = min(s, seq[j]); s_end = max(s_end, seq[j]); } }
+        s = __reduce_min_sync(ALL, s);
+        s_end = __reduce_max_sync(ALL, s_end);
+        for (; s <= s_end; ++s) {
+            float sum = 0.f, cnt = 0.f;
+#pragma unroll
+            for (int j = 0; j < SMALL_PER_LANE; ++j) if (seq[j] == s && k.on[j]) { sum += value[j]; cnt += 1.f; }
+            const float2 v = make_float2(wsum(sum), wsum(cnt));
+            const bool begins = offsets[s] >= t0, ends = offsets[s + 1] <= t1;
+            if (!begins) head = v;
+            else if (!ends) tail = v;
+            else if (lane == 0) seq_sum[s] = v;
+        }
+        if (lane == 0) { first[warp] = head; last[warp] = tail; }
+    }
+    __syncthreads();
+    if (POLICY) policy_finish(b); else preference_finish(b);
+    __syncthreads();
+    for (int i = threadIdx.x; i <= n; i += blockDim.x) a.weight[i] = weight[i];    // for a later gradient call
+    if (!a.dlogp) return;
+#pragma unroll
+    for (int j = 0; j < SMALL_PER_LANE; ++j) {
+        const int t = t0 + j * 32 + lane;
+        if (t < t1) a.dlogp[t] = !k.on[j] ? 0.f : (POLICY ? grad[j] : 1.f) * (weight[POLICY && !a.by_seq ? n : seq[j]] * up);
+    }
 }
 
 // ------------------------------------------------------------------------------------ host side
@@ -364,20 +503,39 @@ int common(SeqArgs* a, const float* logp, const float* ref_logp, const uint8_t* 
     if (ws_bytes < workspace_for(T, n_seqs, a, ws)) return VPCE_WORKSPACE_TOO_SMALL;
     a->logp = logp; a->ref_logp = ref_logp; a->mask = mask; a->offsets = offsets;
     a->T = static_cast<long>(T); a->n_seqs = static_cast<long>(n_seqs);
-    a->steps = static_cast<int>(steps_for(T)); a->n_tiles = static_cast<long>(tiles_for(T));
+    a->span = static_cast<long>(steps_for(T) * STEP); a->n_tiles = static_cast<long>(tiles_for(T));
+    a->n_stats = (a->n_tiles + WARPS - 1) / WARPS;
     a->dlogp = dlogp; a->upstream = upstream;
     return VPCE_OK;
 }
 
 unsigned blocks_for(const SeqArgs& a) { return static_cast<unsigned>((a.n_tiles + WARPS - 1) / WARPS); }
 
-template <bool POLICY> void launch_sums(const SeqArgs& a, cudaStream_t st) {
-    if (a.n_tiles > 0) seq_sums_kernel<POLICY><<<blocks_for(a), THREADS, 0, st>>>(a);
+// `early`: may start before the kernel in front of it has ended (it waits for it where it needs its results).
+template <typename K> cudaError_t launch(K kern, unsigned blocks, int threads, const SeqArgs& a, bool early, cudaStream_t st) {
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(threads); cfg.stream = st;
+    cfg.attrs = &attr; cfg.numAttrs = early ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, a);
 }
-template <bool POLICY> void launch_grad(const SeqArgs& a, cudaStream_t st) {
-    if (a.n_tiles > 0 && a.dlogp) seq_grad_kernel<POLICY><<<blocks_for(a), THREADS, 0, st>>>(a);
+
+// `backward`: the gradient alone (the call that filled the workspace is an ordinary predecessor in the stream).
+template <bool POLICY> int launch_all(const SeqArgs& a, bool backward, cudaStream_t st) {
+    cudaError_t e = cudaSuccess;
+    const bool grad = a.dlogp && a.n_tiles > 0;
+    if (!backward) {
+        if (a.T <= SMALL_T && a.n_seqs <= SMALL_SEQS)
+            // as many warps as there are tiles; the join of many sequences takes a few more
+            return launch(seq_small_kernel<POLICY>, 1, static_cast<int>(32 * std::max<int64_t>((a.T + SMALL_TILE - 1) / SMALL_TILE, a.n_seqs > 64 ? 16 : 4)), a, false, st) == cudaSuccess ? VPCE_OK : VPCE_CUDA_ERROR;
+        e = launch(seq_sums_kernel<POLICY>, blocks_for(a), THREADS, a, false, st);
+        if (e == cudaSuccess) e = launch(seq_finish_kernel<POLICY>, 1, FIN_THREADS, a, true, st);
+    }
+    if (e == cudaSuccess && grad) e = launch(seq_grad_kernel<POLICY>, blocks_for(a), THREADS, a, !backward, st);
+    return e == cudaSuccess ? VPCE_OK : VPCE_CUDA_ERROR;
 }
-int done() { return cudaGetLastError() == cudaSuccess ? VPCE_OK : VPCE_CUDA_ERROR; }
 
 int policy_args(SeqArgs* a, const float* logp, const float* old_logp, const float* ref_logp, const float* adv, int adv_per_token,
                 const uint8_t* mask, const int64_t* offsets, int64_t T, int64_t n_seqs, double clip_low, double clip_high,
@@ -415,11 +573,7 @@ int vp_policy_loss(const float* logp, const float* old_logp, const float* ref_lo
                                    clip_high, kl_coef, aggregate, dlogp, upstream, workspace, workspace_bytes))
         return rc;
     a.stats = stats;
-    const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    launch_sums<true>(a, st);
-    policy_finish_kernel<<<1, FIN_THREADS, 0, st>>>(a);
-    launch_grad<true>(a, st);
-    return done();
+    return launch_all<true>(a, false, static_cast<cudaStream_t>(stream));
 }
 
 int vp_policy_loss_backward(const float* logp, const float* old_logp, const float* ref_logp, const float* advantages,
@@ -431,8 +585,7 @@ int vp_policy_loss_backward(const float* logp, const float* old_logp, const floa
     if (const int rc = policy_args(&a, logp, old_logp, ref_logp, advantages, adv_per_token, mask, seq_offsets, T, n_seqs, clip_low,
                                    clip_high, kl_coef, aggregate, dlogp, upstream, const_cast<void*>(workspace), workspace_bytes))
         return rc;
-    launch_grad<true>(a, static_cast<cudaStream_t>(stream));
-    return done();
+    return launch_all<true>(a, true, static_cast<cudaStream_t>(stream));
 }
 
 size_t vp_preference_loss_workspace_bytes(int64_t T, int64_t n_pairs) {
@@ -453,11 +606,7 @@ int vp_preference_loss(const float* logp, const float* ref_logp, const uint8_t* 
     a.by_seq = 1;
     a.beta = beta; a.margin = margin; a.smoothing = label_smoothing; a.kind = kind; a.average = average != 0;
     a.stats = stats; a.rewards = rewards;
-    const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    launch_sums<false>(a, st);
-    preference_finish_kernel<<<1, FIN_THREADS, 0, st>>>(a);
-    launch_grad<false>(a, st);
-    return done();
+    return launch_all<false>(a, false, static_cast<cudaStream_t>(stream));
 }
 
 int vp_preference_loss_backward(const uint8_t* mask, const int64_t* seq_offsets, int64_t T, int64_t n_pairs, float* dlogp,
@@ -468,8 +617,7 @@ int vp_preference_loss_backward(const uint8_t* mask, const int64_t* seq_offsets,
                               workspace_bytes))
         return rc;
     a.by_seq = 1;
-    launch_grad<false>(a, static_cast<cudaStream_t>(stream));
-    return done();
+    return launch_all<false>(a, true, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -59,25 +59,29 @@ def _stream(stream, index: int) -> int:
     return int(stream.cuda_stream) if stream is not None else torch._C._cuda_getCurrentRawStream(index)
 
 
-def _call(fn, device: torch.device, *args) -> None:
+def _call(fn, index: int, *args) -> None:
     """Calls the C entry point with the operands' device current (the library launches on the current device)."""
-    if torch.cuda.current_device() == device.index:
+    if torch._C._cuda_getDevice() == index:
         code = fn(*args)
     else:
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             code = fn(*args)
     if code:
         _fail(code)
 
 
-def _device(t, name: str) -> torch.device:
+def _device(t, name: str) -> int:
+    """Index of the device that holds t."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
-    return t.device
+    return t.get_device()
 
 
-def _ptr(t, dtype, name: str, numel: int, device) -> int:
-    """Pointer of a contiguous tensor of `numel` elements on `device`."""
+def _ptr(t, dtype, name: str, numel: int, dev: int) -> int:
+    """Pointer of a contiguous tensor of `numel` elements on device `dev`."""
+    # what is right is found out with as few calls as possible; what is wrong, and why, below
+    if type(t) is torch.Tensor and t.dtype is dtype and t.numel() == numel and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dtype is not dtype:
@@ -86,31 +90,33 @@ def _ptr(t, dtype, name: str, numel: int, device) -> int:
         raise ValueError(f"{name} has {t.numel()} elements, expected {numel}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{dev}")
     return t.data_ptr()
 
 
-def _opt(t, dtype, name: str, numel: int, device) -> Optional[int]:
-    return None if t is None else _ptr(t, dtype, name, numel, device)
+def _opt(t, dtype, name: str, numel: int, dev: int) -> Optional[int]:
+    return None if t is None else _ptr(t, dtype, name, numel, dev)
 
 
-def _workspace(t, device) -> Tuple[int, int]:
+def _workspace(t, dev: int) -> Tuple[int, int]:
     n = t.numel() if isinstance(t, torch.Tensor) else 0
-    return _ptr(t, torch.uint8, "workspace", n, device), n
+    return _ptr(t, torch.uint8, "workspace", n, dev), n
 
 
 # --------------------------------------------------------------------------- layer norm (layer_norm.h)
-def _rows(t, dtype, name: str, rows: int, d: int, device) -> Tuple[int, int]:
+def _rows(t, dtype, name: str, rows: int, d: int, dev: int) -> Tuple[int, int]:
     """Pointer and row stride of a [rows, d] tensor whose rows are contiguous."""
+    if type(t) is torch.Tensor and t.dtype is dtype and t.shape == (rows, d) and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr(), d
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
     if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != d:
         raise ValueError(f"{name} must be [{rows}, {d}], got {list(t.shape)}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{dev}")
     s0, s1 = t.stride()
     if d > 1 and rows > 0 and s1 != 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
@@ -147,7 +153,7 @@ def vp_ln_forward(x, weight, bias, eps: float, y, mean, rstd, stream=None) -> No
     yp, ys = _rows(y, dt, "y", rows, d, dev)
     _call(_lib().vp_ln_forward, dev, xp, _DTYPE_CODE[dt], rows, d, xs, _opt(weight, wdt, "weight", d, dev),
           _opt(bias, wdt, "bias", d, dev), _DTYPE_CODE[wdt], eps, yp, ys, _opt(mean, _F32, "mean", rows, dev),
-          _opt(rstd, _F32, "rstd", rows, dev), _stream(stream, dev.index))
+          _opt(rstd, _F32, "rstd", rows, dev), _stream(stream, dev))
 
 
 def vp_ln_workspace_bytes(rows: int, d: int) -> int:
@@ -169,7 +175,7 @@ def vp_ln_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace, str
     wsp, wsn = (None, 0) if workspace is None else _workspace(workspace, dev)
     _call(_lib().vp_ln_backward, dev, dyp, dys, xp, xs, _DTYPE_CODE[dt], rows, d, _opt(weight, wdt, "weight", d, dev),
           _DTYPE_CODE[wdt], _ptr(mean, _F32, "mean", rows, dev), _ptr(rstd, _F32, "rstd", rows, dev), dxp, dxs,
-          _opt(dweight, wdt, "dweight", d, dev), _opt(dbias, wdt, "dbias", d, dev), wsp, wsn, _stream(stream, dev.index))
+          _opt(dweight, wdt, "dweight", d, dev), _opt(dbias, wdt, "dbias", d, dev), wsp, wsn, _stream(stream, dev))
 
 
 class _LayerNorm(torch.autograd.Function):
@@ -268,7 +274,7 @@ def vp_policy_loss(logp, old_logp, ref_logp, advantages, mask, seq_offsets, clip
                                 adv_per_token)
     wsp, wsn = _workspace(workspace, dev)
     _call(_lib().vp_policy_loss, dev, *args, _ptr(stats, _F32, "stats", 4, dev), _opt(dlogp, _F32, "dlogp", T, dev),
-          _opt(upstream, _F32, "upstream", 1, dev), wsp, wsn, _stream(stream, dev.index))
+          _opt(upstream, _F32, "upstream", 1, dev), wsp, wsn, _stream(stream, dev))
 
 
 def vp_policy_loss_backward(logp, old_logp, ref_logp, advantages, mask, seq_offsets, clip_low: float, clip_high: float,
@@ -279,7 +285,7 @@ def vp_policy_loss_backward(logp, old_logp, ref_logp, advantages, mask, seq_offs
                                 adv_per_token)
     wsp, wsn = _workspace(workspace, dev)
     _call(_lib().vp_policy_loss_backward, dev, *args, _ptr(dlogp, _F32, "dlogp", T, dev),
-          _opt(upstream, _F32, "upstream", 1, dev), wsp, wsn, _stream(stream, dev.index))
+          _opt(upstream, _F32, "upstream", 1, dev), wsp, wsn, _stream(stream, dev))
 
 
 class _PolicyLoss(torch.autograd.Function):
@@ -335,7 +341,7 @@ def vp_preference_loss(logp, ref_logp, mask, seq_offsets, beta: float, margin: f
     _call(_lib().vp_preference_loss, dev, lp, _opt(ref_logp, _F32, "ref_logp", T, dev), mp, op, T, pairs, beta, margin,
           label_smoothing, _choice(_KIND, kind, "kind"), 1 if average else 0, _ptr(stats, _F32, "stats", 3, dev),
           _opt(rewards, _F32, "rewards", n, dev), _opt(dlogp, _F32, "dlogp", T, dev), _opt(upstream, _F32, "upstream", 1, dev),
-          wsp, wsn, _stream(stream, dev.index))
+          wsp, wsn, _stream(stream, dev))
 
 
 def vp_preference_loss_backward(mask, seq_offsets, dlogp, workspace, upstream=None, stream=None) -> None:
@@ -343,7 +349,7 @@ def vp_preference_loss_backward(mask, seq_offsets, dlogp, workspace, upstream=No
     dev, T, n, dp, mp, op = _packed(dlogp, mask, seq_offsets)
     wsp, wsn = _workspace(workspace, dev)
     _call(_lib().vp_preference_loss_backward, dev, mp, op, T, _pairs(n), dp, _opt(upstream, _F32, "upstream", 1, dev), wsp, wsn,
-          _stream(stream, dev.index))
+          _stream(stream, dev))
 
 
 class _PreferenceLoss(torch.autograd.Function):
@@ -424,7 +430,7 @@ def muon_orthogonalize(G, O, workspace, coeffs=None, steps: int = 5, eps: float 
         raise ValueError(f"O must have G's shape {list(G.shape)}, got {list(O.shape)}")
     wsp, wsn = _workspace(workspace, dev)
     _call(_lib().muon_orthogonalize, dev, _ptr(G, G.dtype, "G", n, dev), gc, _ptr(O, O.dtype, "O", n, dev), oc, batch, rows, cols,
-          _coeffs(coeffs, steps), steps, eps, wsp, wsn, _stream(stream, dev.index))
+          _coeffs(coeffs, steps), steps, eps, wsp, wsn, _stream(stream, dev))
 
 
 def muon_step(p, m, grad, w_bf16, lr: float, mu: float, weight_decay: float, scale: float, workspace, nesterov: bool = True,
@@ -442,12 +448,12 @@ def muon_step(p, m, grad, w_bf16, lr: float, mu: float, weight_decay: float, sca
     wsp, wsn = _workspace(workspace, dev)
     _call(_lib().muon_step, dev, _ptr(p, _F32, "p", n, dev), _ptr(m, _F32, "m", n, dev),
           _ptr(grad, getattr(grad, "dtype", None), "grad", n, dev), gc, _opt(w_bf16, _BF16, "w_bf16", n, dev), batch, rows, cols, lr, mu,
-          1 if nesterov else 0, weight_decay, scale, _coeffs(coeffs, steps), steps, eps, wsp, wsn, _stream(stream, dev.index))
+          1 if nesterov else 0, weight_decay, scale, _coeffs(coeffs, steps), steps, eps, wsp, wsn, _stream(stream, dev))
 
 
 def muon_device_status(workspace, stream=None) -> int:
     """The status word of the last call that used this workspace (synchronises): 0, or 2 when a wait ran out."""
     dev = _device(workspace, "workspace")
     out = ctypes.c_int32(-1)
-    _call(_lib().muon_device_status, dev, _workspace(workspace, dev)[0], ctypes.byref(out), _stream(stream, dev.index))
+    _call(_lib().muon_device_status, dev, _workspace(workspace, dev)[0], ctypes.byref(out), _stream(stream, dev))
     return int(out.value)

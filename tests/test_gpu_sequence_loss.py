@@ -381,3 +381,30 @@ def test_refusals():
         with pytest.raises(vp.VpceError) as ei:
             pref(**bad)
         assert ei.value.code == code
+
+
+@pytest.mark.parametrize("lens", [[700, 0, 41], [30000, 1, 9000]])
+def test_graph_and_other_stream(lens):
+    off, T, logp, old, ref, mask, adv, adv_seq = make(lens, seed=8)
+    t = [cuda(x) for x in (logp, old, ref, adv)]
+    m, o = cuda(mask, torch.bool), cuda(off, torch.int64)
+    stats, d = torch.empty(4, device="cuda"), torch.empty(T, device="cuda")
+    ws = torch.empty(vp.vp_policy_loss_workspace_bytes(T, len(lens)), dtype=torch.uint8, device="cuda")
+    call = lambda **kw: vp.vp_policy_loss(*t, m, o, LO, HI, 0.1, "seq_mean", stats, d, ws, **kw)
+    call()
+    want = stats.clone(), d.clone()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for _ in range(5):                                    # back to back: a call may not start before the one before it is done
+        call(stream=s)
+    s.synchronize()
+    assert torch.equal(stats, want[0]) and torch.equal(d, want[1])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+        twice = d * 2                                     # enqueued right behind: sees the finished gradient
+    for _ in range(3):
+        stats.zero_(), d.zero_(), twice.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(stats, want[0]) and torch.equal(d, want[1]) and torch.equal(twice, 2 * want[1])
