@@ -185,9 +185,36 @@ template <typename G, int V> void launch_prep_v(const PrepParams& p, cudaStream_
         muon_start_kernel<G, V><<<dim3(static_cast<unsigned>(std::min(blocks, most)), nb), PREP_THREADS, 0, st>>>(p);
     }
 }
-template <typename G> void launch_prep(const PrepParams& p, bool four, cudaStream_t st) {
-    if (four) launch_prep_v<G, 4>(p, st);
+template <typename G> void launch_prep(const PrepParams& p, cudaStream_t st) {
+    if (p.four) launch_prep_v<G, 4>(p, st);
     else launch_prep_v<G, 1>(p, st);
+}
+
+// CTAs that hold a matrix in the one-launch kernel, 0: it does not fit.
+int small_cg(int64_t R, int64_t C) {
+    if (R <= 128 && C <= SmallShape<1>::MAX_C) return 1;
+    return R <= SmallShape<2>::ROWS && C <= SmallShape<2>::MAX_C ? 2 : 0;
+}
+
+template <int CG, typename G> cudaError_t launch_small_cg(const GemmParams& q, const PrepParams& pp, cudaStream_t st) {
+    static std::atomic<bool> raised[64];
+    int dev = 0;
+    if (cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess) return e;
+    auto kern = muon_small_kernel<CG, G>;
+    if (dev < 0 || dev >= 64 || !raised[dev].load(std::memory_order_acquire)) {
+        if (cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SmallShape<CG>::SMEM); e != cudaSuccess) return e;
+        if (dev >= 0 && dev < 64) raised[dev].store(true, std::memory_order_release);
+    }
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = CG; attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(CG * q.batch)); cfg.blockDim = dim3(SMALL_THREADS);
+    cfg.dynamicSmemBytes = SmallShape<CG>::SMEM; cfg.stream = st; cfg.attrs = &attr; cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, q, pp);
+}
+template <typename G> cudaError_t launch_small(const GemmParams& q, const PrepParams& pp, int cg, cudaStream_t st) {
+    return cg == 1 ? launch_small_cg<1, G>(q, pp, st) : launch_small_cg<2, G>(q, pp, st);
 }
 
 struct Target {                                 // what the last product writes
@@ -216,6 +243,24 @@ int run(const void* g, int g_dtype, float* m, float mu, int nesterov, int64_t ba
     q.status = reinterpret_cast<int*>(base); q.next = q.status + 16; q.done = reinterpret_cast<int*>(base + L.done);
     q.wait_limit_ns = static_cast<unsigned long long>(vp_ce_set_wait_limit_ns(0));
     Maps maps;
+    PrepParams pp{};
+    pp.g = g; pp.m = m; pp.mu = mu; pp.nesterov = nesterov;
+    pp.batch = q.batch; pp.rows = rows; pp.cols = cols; pp.parts = static_cast<int>(L.parts);
+    pp.sumsq = reinterpret_cast<double*>(base + L.sumsq);
+    pp.eps = static_cast<float>(eps); pp.scale = static_cast<float>(plan.scale0);
+    pp.X = q.X[0]; pp.R = q.R; pp.C = q.C; pp.ldx = q.ldx; pp.status = q.status; pp.next = q.next; pp.done = q.done;
+    // four elements per access where every matrix (and every row, for the start) begins on a boundary of four elements
+    pp.four = cols % 4 == 0 && aligned(g, g_dtype == VPCE_F32 ? 16 : 8) && aligned(m, 16);
+    q.steps = steps;
+    std::copy(plan.alpha, plan.alpha + 3 * steps, q.alpha);
+    std::copy(plan.beta, plan.beta + 3 * steps, q.beta);
+    if (const int cg = small_cg(L.R, L.C)) {
+        if (batch > 1 && cudaMemsetAsync(q.status, 0, sizeof(int), st) != cudaSuccess) return VPCE_CUDA_ERROR;
+        if (cg == 2) q.ldx = static_cast<int>((L.C + 127) / 128 * 128);     // two halves of whole chunks
+        const cudaError_t e = g_dtype == VPCE_F32 ? launch_small<float>(q, pp, cg, st)
+                              : g_dtype == VPCE_F16 ? launch_small<__half>(q, pp, cg, st) : launch_small<__nv_bfloat16>(q, pp, cg, st);
+        return e == cudaSuccess ? VPCE_OK : VPCE_CUDA_ERROR;
+    }
     const int pairs = sm_count() / 2;
     int64_t most = 0;
     for (int mode = 0; mode < 3; ++mode) {
@@ -233,21 +278,10 @@ int run(const void* g, int g_dtype, float* m, float mu, int nesterov, int64_t ba
              map(&maps.x_mn[i], q.X[i], L.ldx, 64, q.bn[APPLY] / 128) && map(&maps.x_blk[i], q.X[i], L.ldx, 32, 1, 32);
     if (!ok || ensure_smem() != cudaSuccess) return VPCE_CUDA_ERROR;
 
-    PrepParams pp{};
-    pp.g = g; pp.m = m; pp.mu = mu; pp.nesterov = nesterov;
-    pp.batch = q.batch; pp.rows = rows; pp.cols = cols; pp.parts = static_cast<int>(L.parts);
-    pp.sumsq = reinterpret_cast<double*>(base + L.sumsq);
-    pp.eps = static_cast<float>(eps); pp.scale = static_cast<float>(plan.scale0);
-    pp.X = q.X[0]; pp.R = q.R; pp.C = q.C; pp.ldx = q.ldx; pp.status = q.status; pp.next = q.next; pp.done = q.done;
-    // four elements per access where every matrix (and every row, for the start) begins on a boundary of four elements
-    const bool four = cols % 4 == 0 && aligned(g, g_dtype == VPCE_F32 ? 16 : 8) && aligned(m, 16);
-    if (g_dtype == VPCE_F32) launch_prep<float>(pp, four, st);
-    else if (g_dtype == VPCE_F16) launch_prep<__half>(pp, four, st);
-    else launch_prep<__nv_bfloat16>(pp, four, st);
+    if (g_dtype == VPCE_F32) launch_prep<float>(pp, st);
+    else if (g_dtype == VPCE_F16) launch_prep<__half>(pp, st);
+    else launch_prep<__nv_bfloat16>(pp, st);
 
-    q.steps = steps;
-    std::copy(plan.alpha, plan.alpha + 3 * steps, q.alpha);
-    std::copy(plan.beta, plan.beta + 3 * steps, q.beta);
     muon_products_kernel<<<2 * static_cast<unsigned>(most), GEMM_THREADS, GEMM_SMEM, st>>>(maps, q);
     return cudaGetLastError() == cudaSuccess ? VPCE_OK : VPCE_CUDA_ERROR;
 }

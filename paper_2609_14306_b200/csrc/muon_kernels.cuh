@@ -113,6 +113,7 @@ struct PrepParams {
     int batch; long rows, cols;
     int parts; double* sumsq;               // [batch][parts]
     float eps, scale;                       // X_0 is stored times `scale`
+    int four;                               // four elements per access: see the host
     __half* X; int R, C, ldx;
     int *status, *next, *done;
 };
@@ -350,14 +351,16 @@ __device__ __forceinline__ void epilogue_block(const GemmParams& p, const Maps& 
 }
 
 // One warp's block of the last product, to the caller's arrays: coalesced along their rows.  Where those are X's columns
-// (TRANSPOSED) a lane keeps its row of X and element i is column col0 + i; else 16 columns at a time pass through shared memory
-// (`blk`, whose addend is read first) and element i is row row0 + 2 (i % 16) + lane / 16, column col0 + 16 (i / 16) + lane % 16.
+// (TRANSPOSED) a lane keeps its row of X and element i is column col0 + i; else 16 columns at a time pass through 2 KB of shared
+// memory (`scratch`) and element i is row row0 + 2 (i % 16) + lane / 16, column col0 + 16 (i / 16) + lane % 16.  addend(q, f):
+// eight elements of this lane's row of X, from column col0 + 8 q (read before `scratch`, which may be their place, is written).
 // All loads of a block are issued before its stores (p could alias itself for all the compiler knows): one memory latency a
 // block, not 32.  Nothing here is used again soon: evict-first, so that the operands stay in the L2.
-template <bool TRANSPOSED>
-__device__ __forceinline__ void epilogue_last(const GemmParams& p, const Tile& w, int row0, int col0, int lane, uint32_t tmem, uint32_t blk) {
+template <bool TRANSPOSED, typename Addend>
+__device__ __forceinline__ void epilogue_last(const GemmParams& p, int k, int b, int row0, int col0, int lane, uint32_t tmem, uint32_t scratch,
+                                              Addend addend) {
     const int r = row0 + (TRANSPOSED ? lane : lane >> 4), c = col0 + (TRANSPOSED ? 0 : lane & 15);
-    const long at = static_cast<long>(w.b) * p.R * p.C + (TRANSPOSED ? static_cast<long>(c) * p.R + r : static_cast<long>(r) * p.C + c);
+    const long at = static_cast<long>(b) * p.R * p.C + (TRANSPOSED ? static_cast<long>(c) * p.R + r : static_cast<long>(r) * p.C + c);
     const int pitch = TRANSPOSED ? p.R : 2 * p.C;
     auto offset = [&](int i) { return TRANSPOSED ? i * pitch : (i & 15) * pitch + (i & 16); };
     auto inside = [&](int i) { return TRANSPOSED ? r < p.R && c + i < p.C : r + 2 * (i & 15) < p.R && c + (i & 16) < p.C; };
@@ -370,11 +373,11 @@ __device__ __forceinline__ void epilogue_last(const GemmParams& p, const Tile& w
     __syncwarp();
     tmem_ld32(tmem, v);
     tmem_ld_wait();
-    const float alpha = p.alpha[w.k], beta = p.beta[w.k];
+    const float alpha = p.alpha[k], beta = p.beta[k];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         float f[8];
-        unpack8(ld_shared_v4(blk + block_at(lane, q)), f);
+        addend(q, f);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[8 * q + j] = alpha * v[8 * q + j] + beta * f[j];
     }
@@ -384,12 +387,12 @@ __device__ __forceinline__ void epilogue_last(const GemmParams& p, const Tile& w
         for (int h = 0; h < 2; ++h) {
             __syncwarp();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) st_shared_f32(blk + 4 * (16 * lane + (j ^ (lane & 15))), v[16 * h + j]);
+            for (int j = 0; j < 16; ++j) st_shared_f32(scratch + 4 * (16 * lane + (j ^ (lane & 15))), v[16 * h + j]);
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int row = 2 * i + (lane >> 4);
-                v[16 * h + i] = ld_shared_f32(blk + 4 * (16 * row + ((lane & 15) ^ (row & 15))));
+                v[16 * h + i] = ld_shared_f32(scratch + 4 * (16 * row + ((lane & 15) ^ (row & 15))));
             }
         }
     }
@@ -638,8 +641,10 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
             for (int n = 0; n < blocks_here; ++n) {
                 const int col0 = col_first + 64 * n;
                 if (w.last) {
-                    if (p.transposed) epilogue_last<true>(p, w, row0, col0, lane, tmem_row + 64 * n, place(n));
-                    else epilogue_last<false>(p, w, row0, col0, lane, tmem_row + 64 * n, place(n));
+                    const uint32_t blk = place(n);
+                    auto from_block = [&](int q, float* f) { unpack8(ld_shared_v4(blk + block_at(lane, q)), f); };
+                    if (p.transposed) epilogue_last<true>(p, w.k, w.b, row0, col0, lane, tmem_row + 64 * n, blk, from_block);
+                    else epilogue_last<false>(p, w.k, w.b, row0, col0, lane, tmem_row + 64 * n, blk, from_block);
                 } else {
                     float v[32];
                     __syncwarp();
@@ -678,6 +683,254 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
         __syncwarp();
         tc_fence_after();
         tmem2_dealloc(tmem_base, 512);
+    }
+}
+
+// ------------------------------------------------------------------------------------ small matrices
+// The whole update of a matrix that fits the shared memory of one CTA (CG = 1: R <= 128, C <= 512) or a CTA pair (CG = 2: R and
+// C <= 256, 128 rows in each), one launch for a batch: momentum, norm, all products, write-back.  X and A (later B) stay in
+// shared memory as fp16 in the operands' layout: 64-column chunks of rows of 128 bytes, 128-byte swizzle.  A row of X is K-major
+// for X X^T, and the same bytes are the MN-major right operand of B X, whose K are the rows.  In a pair the right operand's
+// columns are split, not its rows, so B X reads a second copy, XN: all 256 rows of this CTA's half of the columns, to which the
+// other CTA's epilogue writes its rows.
+// Each product is issued by one thread, waited for by all 16 warps (four per quarter of the tensor memory's lanes), and turned
+// into the next operand in place.
+constexpr int SMALL_WARPS = 16, SMALL_THREADS = 32 * SMALL_WARPS;
+constexpr int SMALL_KEPT = 8;                           // pieces of 8 elements of U that a thread keeps while the norm is formed
+template <int CG> struct SmallShape {
+    static constexpr int ROWS = 128 * CG;               // of the padded X
+    static constexpr int MAX_C = CG == 1 ? 512 : 256;
+    static constexpr int A_CHUNKS = 2 * CG;             // 64-column chunks of A
+    static constexpr int X_CHUNK = 128 * 128;           // bytes: this CTA's 128 rows
+    static constexpr int XN_CHUNK = 256 * 128;
+    static constexpr int X_BYTES = MAX_C / 64 * X_CHUNK, A_OFFSET = X_BYTES, XN_OFFSET = A_OFFSET + A_CHUNKS * X_CHUNK;
+    static constexpr int SCRATCH = XN_OFFSET + (CG == 2 ? MAX_C / 128 * XN_CHUNK : 0);
+    static constexpr int SMEM = SCRATCH + 1024;   // the scratch (2 KB a warp, in A) and alignment slack
+};
+static_assert(SmallShape<1>::SMEM <= 227 * 1024 && SmallShape<2>::SMEM <= 227 * 1024, "shared memory per CTA");
+
+template <int CG> __device__ __forceinline__ void small_sync() {
+    if (CG == 2) cluster_sync_all();
+    else __syncthreads();
+}
+__device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint4 v) {
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+// Byte offset of 16-byte piece q (8 halves) of row r inside a chunk.
+__device__ __forceinline__ uint32_t chunk_at(int r, int q) { return static_cast<uint32_t>(r * 128 + ((q ^ (r & 7)) << 4)); }
+
+template <int CG, typename G>
+__global__ void __launch_bounds__(SMALL_THREADS, 1) muon_small_kernel(const __grid_constant__ GemmParams p, const __grid_constant__ PrepParams pp) {
+    using S = SmallShape<CG>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ double part[SMALL_WARPS];
+    __shared__ uint64_t bar_slot;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_word;
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    const uint32_t bar = smem_u32(&bar_slot);
+    volatile int* abort_flag = &abort_word;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = CG == 2 ? static_cast<int>(cluster_ctarank()) : 0;
+    const int b = blockIdx.x / CG;
+    const int chunks = p.ldx / 64;                                          // CG = 2: an even number (ldx a multiple of 128)
+
+    if (threadIdx.x == 0) {
+        abort_word = 0;
+        mbar_init(bar, 1);
+        fence_barrier_init();
+        if (gridDim.x == CG && rank == 0) *p.status = 0;                    // of several matrices the host clears it
+    }
+    if (warp == 0) {
+        if (CG == 2) { tmem2_alloc(smem_u32(&tmem_slot), 512); tmem2_relinquish(); }
+        else { tmem_alloc(smem_u32(&tmem_slot), 512); tmem_relinquish(); }
+    }
+
+    // ---- momentum and sum of squares over this CTA's rows of X, in pieces of 8 neighbouring columns of a row of X.  Neighbouring
+    // threads take neighbouring elements of the caller's array: along X's rows, or down them where it holds X^T.
+    const size_t mat = static_cast<size_t>(b) * p.R * p.C;
+    const G* g = static_cast<const G*>(pp.g) + mat;
+    float* m = pp.m ? pp.m + mat : nullptr;
+    const int rows_here = min(128, p.R - rank * 128);                       // 0 or less: this CTA holds zeros only
+    const int pieces = 128 * chunks * 8;
+    auto row_of = [&](int k) { return p.transposed ? k & 127 : k / (chunks * 8); };
+    auto col_of = [&](int k) { return (p.transposed ? k >> 7 : k % (chunks * 8)) * 8; };
+    const size_t along = p.transposed ? p.R : 1, down = p.transposed ? 1 : p.C, origin = static_cast<size_t>(rank) * 128 * down;
+    // U of a piece (0 beyond the matrix); UPDATE: with the momentum brought up to date
+    auto load_piece = [&](int k, float* u, bool update) {
+        const int r = row_of(k), c = col_of(k);
+        const int n = r < rows_here ? min(8, p.C - c) : 0;
+        const size_t at = origin + r * down + c * along;
+        const bool four = pp.four && !p.transposed;                         // n is then 0, 4 or 8
+        float mv[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = 0.f;
+        if (four) {
+#pragma unroll
+            for (int j = 0; j < 8; j += 4) {
+                if (j < n) load_v<G, 4>(g + at + j, u + j);
+                if (m && j < n) load_v<float, 4>(m + at + j, mv + j);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (j < n) u[j] = to_float(g[at + j * along]);
+                if (m && j < n) mv[j] = m[at + j * along];
+            }
+        }
+        if (m) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (update) mv[j] = pp.mu * mv[j] + u[j];
+                u[j] = pp.nesterov ? u[j] + pp.mu * mv[j] : mv[j];
+            }
+            if (update) {
+                if (four) {
+#pragma unroll
+                    for (int j = 0; j < 8; j += 4) if (j < n) store_v<4>(m + at + j, mv + j);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) if (j < n) m[at + j * along] = mv[j];
+                }
+            }
+        }
+    };
+    double sq = 0.0;
+    float kept[SMALL_KEPT][8];
+    auto squares = [&](const float* u) {
+        float q = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q += u[j] * u[j];
+        sq += q;
+    };
+#pragma unroll
+    for (int i = 0; i < SMALL_KEPT; ++i) {
+        const int k = i * SMALL_THREADS + threadIdx.x;
+        if (k < pieces) { load_piece(k, kept[i], true); squares(kept[i]); }
+    }
+    for (int k = SMALL_KEPT * SMALL_THREADS + threadIdx.x; k < pieces; k += SMALL_THREADS) {
+        float u[8];
+        load_piece(k, u, true);
+        squares(u);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+    if (lane == 0) part[warp] = sq;
+    tc_fence_before();
+    small_sync<CG>();
+    tc_fence_after();
+    double total = 0.0;
+    for (int r = 0; r < CG; ++r)
+        for (int i = 0; i < SMALL_WARPS; ++i) {
+            double v;
+            if (CG == 2) asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(mapa_shared(smem_u32(part + i), r)) : "memory");
+            else v = part[i];
+            total += v;
+        }
+    const float norm = static_cast<float>(sqrt(total));
+    const float inv = pp.scale / (norm < pp.eps ? pp.eps : norm);           // NaN stays NaN
+    const uint32_t tmem = tmem_slot;
+
+    // Eight neighbouring elements of this CTA's row r of X from column c on: into X, and into XN where that lies.
+    auto put_x = [&](int r, int c, uint4 v) {
+        const uint32_t at = base + (c >> 6) * S::X_CHUNK + chunk_at(r, (c >> 3) & 7);
+        st_shared_v4(at, v);
+        if (CG == 2) {
+            const int half = p.ldx / 2, to = c >= half ? 1 : 0, cc = c - to * half;
+            st_cluster_v4(mapa_shared(base + S::XN_OFFSET + (cc >> 6) * S::XN_CHUNK + chunk_at(rank * 128 + r, (cc >> 3) & 7), to), v);
+        }
+    };
+    // ---- X_0; rows and columns beyond the matrix hold zeros.  A piece that was not kept is formed again.
+    auto start_piece = [&](int k, float* u) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] *= inv;
+        put_x(row_of(k), col_of(k), pack8(u));
+    };
+#pragma unroll
+    for (int i = 0; i < SMALL_KEPT; ++i) {
+        const int k = i * SMALL_THREADS + threadIdx.x;
+        if (k < pieces) start_piece(k, kept[i]);
+    }
+    for (int k = SMALL_KEPT * SMALL_THREADS + threadIdx.x; k < pieces; k += SMALL_THREADS) {
+        float u[8];
+        load_piece(k, u, false);
+        start_piece(k, u);
+    }
+
+    const int quad = warp & 3, first = warp >> 2, row = quad * 32 + lane;
+    const uint32_t tmem_row = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+    uint32_t parity = 0;
+    for (int k = 0; k < 3 * p.steps; ++k) {
+        const int mode = k % 3;
+        // what was written to either CTA's shared memory is read by the tensor cores next
+        asm volatile("fence.proxy.async;" ::: "memory");
+        tc_fence_before();
+        small_sync<CG>();
+        tc_fence_after();
+        if (threadIdx.x == 0 && rank == 0) {
+            asm volatile("fence.proxy.async;" ::: "memory");
+            const int k_steps = mode == GRAM ? p.ldx / 16 : S::ROWS / 16;
+            const int groups = mode == APPLY ? (p.ldx + 255) / 256 : 1;     // of up to 256 result columns
+            for (int n = 0; n < groups; ++n) {
+                const int width = mode == APPLY ? min(256, p.ldx - 256 * n) : S::ROWS;
+                const uint32_t idesc = make_idesc(width, false, mode == APPLY, 128 * CG, 0u);
+                for (int q = 0; q < k_steps; ++q) {
+                    const uint32_t along = (q >> 2) * S::X_CHUNK + (q & 3) * 32;            // K-major: 32 bytes of a chunk's rows
+                    const uint64_t ad = make_smem_desc(base + (mode == GRAM ? 0 : S::A_OFFSET) + along, 16, 1024);
+                    uint64_t bd;
+                    if (mode != APPLY) bd = ad;                                             // the same rows
+                    else if (CG == 1) bd = make_smem_desc(base + 4 * n * S::X_CHUNK + q * 2048, S::X_CHUNK, 1024);
+                    else bd = make_smem_desc(base + S::XN_OFFSET + q * 2048, S::XN_CHUNK, 1024);
+                    if (CG == 2) umma2_f16(tmem + 256 * n, ad, bd, idesc, q != 0 ? 1u : 0u);
+                    else umma_f16(tmem + 256 * n, ad, bd, idesc, q != 0 ? 1u : 0u);
+                }
+            }
+            if (CG == 2) umma2_commit_both(bar);
+            else umma_commit(bar);
+        }
+        mbar_wait(bar, parity, abort_flag, p.wait_limit_ns);                // on expiry: the status word is set below, nobody leaves early
+        parity ^= 1u;
+        tc_fence_after();
+        if (k + 1 == 3 * p.steps) break;
+        const float alpha = p.alpha[k], beta = p.beta[k];
+        const int blocks = (mode == APPLY ? p.ldx : S::ROWS) / 32;
+        for (int n = first; n < blocks; n += SMALL_WARPS / 4) {
+            float v[32];
+            __syncwarp();
+            tmem_ld32(tmem_row + 32 * n, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = 32 * n + 8 * q;
+                const uint32_t at = base + (mode == APPLY ? 0 : S::A_OFFSET) + (c >> 6) * S::X_CHUNK + chunk_at(row, (c >> 3) & 7);
+                float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                if (mode != GRAM) unpack8(ld_shared_v4(at), f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = alpha * v[8 * q + j] + beta * f[j];
+                if (mode == APPLY) put_x(row, c, pack8(f));
+                else st_shared_v4(at, pack8(f));
+            }
+        }
+    }
+    // ---- the last X, to the caller's arrays
+    for (int n = first; n < p.ldx / 32; n += SMALL_WARPS / 4) {
+        if (32 * n >= p.C || quad * 32 >= rows_here) break;                 // uniform in the warp
+        auto from_x = [&](int q, float* f) {
+            const int c = 32 * n + 8 * q;
+            unpack8(ld_shared_v4(base + (c >> 6) * S::X_CHUNK + chunk_at(row, (c >> 3) & 7)), f);
+        };
+        const uint32_t scratch = base + S::A_OFFSET + warp * 2048;          // B is spent
+        if (p.transposed) epilogue_last<true>(p, 3 * p.steps - 1, b, rank * 128 + quad * 32, 32 * n, lane, tmem_row + 32 * n, scratch, from_x);
+        else epilogue_last<false>(p, 3 * p.steps - 1, b, rank * 128 + quad * 32, 32 * n, lane, tmem_row + 32 * n, scratch, from_x);
+    }
+    tc_fence_before();
+    small_sync<CG>();                                                       // no CTA leaves while its pair may still write to it
+    if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, VPCE_DEV_WAIT_EXPIRED);
+    if (warp == 0) {
+        __syncwarp();
+        tc_fence_after();
+        if (CG == 2) tmem2_dealloc(tmem, 512);
+        else tmem_dealloc(tmem, 512);
     }
 }
 

@@ -53,7 +53,7 @@ def oracle(g, **kw):
 
 SHAPES = [(1, 1, 1), (1, 1, 7), (2, 9, 1), (1, 2, 3), (1, 64, 64), (1, 63, 65), (2, 128, 256), (1, 256, 128), (1, 256, 256), (1, 257, 300),
           (3, 300, 257), (1, 500, 1203), (1, 1203, 500), (1, 512, 512), (1, 640, 640), (1, 1030, 130), (40, 48, 60), (2, 385, 769),
-          (1, 129, 2100), (9, 200, 450)]
+          (1, 129, 2100), (9, 200, 450), (5, 100, 500), (2, 512, 90), (3, 200, 250), (2, 250, 140), (170, 30, 20), (1, 128, 513), (1, 257, 257)]
 
 
 @pytest.mark.parametrize("batch,rows,cols", SHAPES)
