@@ -70,6 +70,15 @@ __device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, uint32_t sr
     asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
                  ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
+// 32 lanes x 16 consecutive fp32 columns of tensor memory.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+}
 __device__ __forceinline__ void bulk_wait_read_all() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
     uint4 v;
@@ -350,13 +359,13 @@ __device__ __forceinline__ void epilogue_block(const GemmParams& p, const Maps& 
     }
 }
 
-// One warp's block of the last product, to the caller's arrays: coalesced along their rows.  Where those are X's columns
-// (TRANSPOSED) a lane keeps its row of X and element i is column col0 + i; else 16 columns at a time pass through 2 KB of shared
-// memory (`scratch`) and element i is row row0 + 2 (i % 16) + lane / 16, column col0 + 16 (i / 16) + lane % 16.  addend(q, f):
-// eight elements of this lane's row of X, from column col0 + 8 q (read before `scratch`, which may be their place, is written).
-// All loads of a block are issued before its stores (p could alias itself for all the compiler knows): one memory latency a
-// block, not 32.  Nothing here is used again soon: evict-first, so that the operands stay in the L2.
-template <bool TRANSPOSED, typename Addend>
+// N columns (16 or 32) of one warp's rows of the last product, to the caller's arrays: coalesced along their rows.  Where those
+// are X's columns (TRANSPOSED) a lane keeps its row of X and element i is column col0 + i; else 16 columns at a time pass through
+// 2 KB of shared memory (`scratch`) and element i is row row0 + 2 (i % 16) + lane / 16, column col0 + 16 (i / 16) + lane % 16.
+// addend(q, f): eight elements of this lane's row of X, from column col0 + 8 q (read before `scratch`, which may be their place,
+// is written).  All loads are issued before the stores (p could alias itself for all the compiler knows): one memory latency for
+// N elements.  Nothing here is used again soon: evict-first, so that the operands stay in the L2.
+template <int N, bool TRANSPOSED, typename Addend>
 __device__ __forceinline__ void epilogue_last(const GemmParams& p, int k, int b, int row0, int col0, int lane, uint32_t tmem, uint32_t scratch,
                                               Addend addend) {
     const int r = row0 + (TRANSPOSED ? lane : lane >> 4), c = col0 + (TRANSPOSED ? 0 : lane & 15);
@@ -364,18 +373,19 @@ __device__ __forceinline__ void epilogue_last(const GemmParams& p, int k, int b,
     const int pitch = TRANSPOSED ? p.R : 2 * p.C;
     auto offset = [&](int i) { return TRANSPOSED ? i * pitch : (i & 15) * pitch + (i & 16); };
     auto inside = [&](int i) { return TRANSPOSED ? r < p.R && c + i < p.C : r + 2 * (i & 15) < p.R && c + (i & 16) < p.C; };
-    float old[32];
+    float old[N];
     if (p.p) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) old[i] = inside(i) ? __ldcs(p.p + at + offset(i)) : 0.f;
+        for (int i = 0; i < N; ++i) old[i] = inside(i) ? __ldcs(p.p + at + offset(i)) : 0.f;
     }
-    float v[32];
+    float v[N];
     __syncwarp();
-    tmem_ld32(tmem, v);
+    if constexpr (N == 32) tmem_ld32(tmem, v);
+    else tmem_ld16(tmem, v);
     tmem_ld_wait();
     const float alpha = p.alpha[k], beta = p.beta[k];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < N / 8; ++q) {
         float f[8];
         addend(q, f);
 #pragma unroll
@@ -384,7 +394,7 @@ __device__ __forceinline__ void epilogue_last(const GemmParams& p, int k, int b,
     if (!TRANSPOSED) {
         // element (row, j) of 16 columns at word 16 row + (j ^ row % 16): no bank is hit more than twice
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < N / 16; ++h) {
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < 16; ++j) st_shared_f32(scratch + 4 * (16 * lane + (j ^ (lane & 15))), v[16 * h + j]);
@@ -398,23 +408,23 @@ __device__ __forceinline__ void epilogue_last(const GemmParams& p, int k, int b,
     }
     if (p.p) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
+        for (int i = 0; i < N; ++i) {
             v[i] = old[i] * p.decay - p.step * v[i];
             if (inside(i)) __stcs(p.p + at + offset(i), v[i]);
         }
         if (p.w) {
             unsigned short* wp = reinterpret_cast<unsigned short*>(p.w) + at;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) if (inside(i)) __stcs(wp + offset(i), __bfloat16_as_ushort(__float2bfloat16_rn(v[i])));
+            for (int i = 0; i < N; ++i) if (inside(i)) __stcs(wp + offset(i), __bfloat16_as_ushort(__float2bfloat16_rn(v[i])));
         }
     } else if (p.out_dtype == VPCE_F32) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) if (inside(i)) __stcs(static_cast<float*>(p.out) + at + offset(i), v[i]);
+        for (int i = 0; i < N; ++i) if (inside(i)) __stcs(static_cast<float*>(p.out) + at + offset(i), v[i]);
     } else {
         unsigned short* o = static_cast<unsigned short*>(p.out) + at;
         const bool f16 = p.out_dtype == VPCE_F16;
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
+        for (int i = 0; i < N; ++i)
             if (inside(i)) __stcs(o + offset(i), f16 ? __half_as_ushort(__float2half_rn(v[i])) : __bfloat16_as_ushort(__float2bfloat16_rn(v[i])));
     }
 }
@@ -643,8 +653,8 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
                 if (w.last) {
                     const uint32_t blk = place(n);
                     auto from_block = [&](int q, float* f) { unpack8(ld_shared_v4(blk + block_at(lane, q)), f); };
-                    if (p.transposed) epilogue_last<true>(p, w.k, w.b, row0, col0, lane, tmem_row + 64 * n, blk, from_block);
-                    else epilogue_last<false>(p, w.k, w.b, row0, col0, lane, tmem_row + 64 * n, blk, from_block);
+                    if (p.transposed) epilogue_last<32, true>(p, w.k, w.b, row0, col0, lane, tmem_row + 64 * n, blk, from_block);
+                    else epilogue_last<32, false>(p, w.k, w.b, row0, col0, lane, tmem_row + 64 * n, blk, from_block);
                 } else {
                     float v[32];
                     __syncwarp();
@@ -795,6 +805,8 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) muon_small_kernel(const __gr
             }
         }
     };
+    // What bounds this part is one SM's share of the L2's bandwidth (256 x 256 in fp32: 384 KB in and out per CTA), so U is kept
+    // rather than read again, as far as registers go.
     double sq = 0.0;
     float kept[SMALL_KEPT][8];
     auto squares = [&](const float* u) {
@@ -808,6 +820,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) muon_small_kernel(const __gr
         const int k = i * SMALL_THREADS + threadIdx.x;
         if (k < pieces) { load_piece(k, kept[i], true); squares(kept[i]); }
     }
+#pragma unroll 1
     for (int k = SMALL_KEPT * SMALL_THREADS + threadIdx.x; k < pieces; k += SMALL_THREADS) {
         float u[8];
         load_piece(k, u, true);
@@ -851,6 +864,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) muon_small_kernel(const __gr
         const int k = i * SMALL_THREADS + threadIdx.x;
         if (k < pieces) start_piece(k, kept[i]);
     }
+#pragma unroll 1
     for (int k = SMALL_KEPT * SMALL_THREADS + threadIdx.x; k < pieces; k += SMALL_THREADS) {
         float u[8];
         load_piece(k, u, false);
@@ -912,16 +926,18 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) muon_small_kernel(const __gr
             }
         }
     }
-    // ---- the last X, to the caller's arrays
-    for (int n = first; n < p.ldx / 32; n += SMALL_WARPS / 4) {
-        if (32 * n >= p.C || quad * 32 >= rows_here) break;                 // uniform in the warp
+    // ---- the last X, to the caller's arrays, 16 columns at a time
+#pragma unroll 1
+    for (int n = first; n < p.ldx / 16; n += SMALL_WARPS / 4) {
+        if (16 * n >= p.C || quad * 32 >= rows_here) break;                 // uniform in the warp
         auto from_x = [&](int q, float* f) {
-            const int c = 32 * n + 8 * q;
+            const int c = 16 * n + 8 * q;
             unpack8(ld_shared_v4(base + (c >> 6) * S::X_CHUNK + chunk_at(row, (c >> 3) & 7)), f);
         };
         const uint32_t scratch = base + S::A_OFFSET + warp * 2048;          // B is spent
-        if (p.transposed) epilogue_last<true>(p, 3 * p.steps - 1, b, rank * 128 + quad * 32, 32 * n, lane, tmem_row + 32 * n, scratch, from_x);
-        else epilogue_last<false>(p, 3 * p.steps - 1, b, rank * 128 + quad * 32, 32 * n, lane, tmem_row + 32 * n, scratch, from_x);
+        const int last = 3 * p.steps - 1, row0 = rank * 128 + quad * 32;
+        if (p.transposed) epilogue_last<16, true>(p, last, b, row0, 16 * n, lane, tmem_row + 16 * n, scratch, from_x);
+        else epilogue_last<16, false>(p, last, b, row0, 16 * n, lane, tmem_row + 16 * n, scratch, from_x);
     }
     tc_fence_before();
     small_sync<CG>();                                                       // no CTA leaves while its pair may still write to it
