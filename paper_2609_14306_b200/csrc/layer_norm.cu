@@ -253,10 +253,12 @@ template <typename T, bool VEC, int EPT> struct Columns {
     // Weights as fp32 in shared memory, in the order of the threads' elements: four of a lane's in 16 bytes, lanes side by side.
     // fill: this warp's (W of any alignment; `none` where p is null; 0 beyond d); weights: part q of this thread's.
     template <typename W> __device__ __forceinline__ void fill(float* to, int warp, int lane, const W* p, float none) const {
-        for (int e = 0; e < EPT; ++e) {
-            const int k = e / N, c = first + STEP * k + e % N;
-            to[((warp * (EPT / 4) + e / 4) * 32 + lane) * 4 + e % 4] = c < d ? (p ? to_f(p[c]) : none) : 0.f;
-        }
+        float f[EPT];
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) f[e] = has(e / N) ? (p ? to_f(p[first + STEP * (e / N) + e % N]) : none) : 0.f;
+#pragma unroll
+        for (int e = 0; e < EPT; e += 4)
+            *reinterpret_cast<float4*>(to + ((warp * (EPT / 4) + e / 4) * 32 + lane) * 4) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
     }
     __device__ __forceinline__ void weights(uint32_t at, int q, f2* v) const {
 #pragma unroll
