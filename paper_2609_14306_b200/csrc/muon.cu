@@ -46,7 +46,7 @@ bool layout(int64_t batch, int64_t rows, int64_t cols, Layout* L) {
     L->parts = std::max<int64_t>(1, std::min<int64_t>(MAX_PARTS, (rows * cols + 16 * PREP_THREADS - 1) / (16 * PREP_THREADS)));
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     size_t off = 256;                                                      // the status word, the work list's counter
-    L->done = off;  off = up(off + sizeof(int) * batch);
+    L->done = off;  off = up(off + sizeof(int) * DONE_PITCH * batch);
     L->sumsq = off; off = up(off + sizeof(double) * batch * L->parts);
     L->X0 = off;    off = up(off + 2 * static_cast<size_t>(batch) * L->R * L->ldx);
     L->X1 = off;    off = up(off + 2 * static_cast<size_t>(batch) * L->R * L->ldx);

@@ -26,6 +26,7 @@ constexpr int EPI_BYTES = EPI_WARPS * EPI_WARP_BYTES;
 constexpr int GEMM_SMEM = STAGES * STAGE_BYTES + EPI_BYTES + 2048;   // barriers (1024) and alignment slack
 static_assert(GEMM_SMEM <= 227 * 1024, "shared memory per CTA");
 constexpr int MAX_STEPS = 32;
+constexpr int DONE_PITCH = 32;              // a counter has a line of its own: its matrix's CTAs poll it
 constexpr int PREP_THREADS = 256;
 constexpr int MAX_PARTS = 512;              // partial sums of squares per matrix
 
@@ -52,7 +53,7 @@ struct GemmParams {
     void* out; int out_dtype;               // muon_orthogonalize
     float* p; __nv_bfloat16* w; float decay, step; // muon_step: p <- p decay - step X
     int *status, *next;                     // next: work-list position to be taken, zero before the launch
-    int* done;                              // [batch] epilogue warps that have finished a tile of this matrix, zero before the launch
+    int* done;                              // [batch][DONE_PITCH] epilogue warps that have finished a tile of this matrix, zero before the launch
     unsigned long long wait_limit_ns;
 };
 
@@ -154,7 +155,7 @@ __global__ void __launch_bounds__(PREP_THREADS) muon_momentum_kernel(const PrepP
     constexpr int UNROLL = V == 4 ? 4 : 8;
     __shared__ double part[PREP_THREADS / 32];
     if (blockIdx.x == 0 && threadIdx.x == 0) {                              // the products' bookkeeping starts at zero
-        p.done[blockIdx.y] = 0;
+        p.done[blockIdx.y * DONE_PITCH] = 0;
         if (blockIdx.y == 0) { *p.status = 0; *p.next = 0; }
     }
     const long n = p.rows * p.cols / V;                                     // accesses of a matrix
@@ -323,6 +324,27 @@ __device__ __forceinline__ void signal_stored(int* counter) {
     asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(counter) : "memory");
 }
 
+// A CTA's producer polls `done` in global memory for all of its CTA; the epilogue warps learn of it here (list positions rise).
+__device__ __forceinline__ void store_ready(uint32_t addr, int t) { asm volatile("st.release.cta.shared::cta.s32 [%0], %1;" ::"r"(addr), "r"(t) : "memory"); }
+__device__ __forceinline__ bool wait_ready(uint32_t addr, int t, volatile int* abort_flag, unsigned long long limit_ns) {
+    unsigned long long t0 = 0;
+    for (uint32_t it = 0;; ++it) {
+        int v;
+        asm volatile("ld.acquire.cta.shared::cta.s32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+        if (v >= t) {
+            asm volatile("fence.proxy.async;" ::: "memory");
+            return true;
+        }
+        if ((it & 63u) == 63u) {
+            if (*abort_flag) return false;
+            const unsigned long long now = globaltimer_ns();
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > limit_ns) { *abort_flag = 1; return false; }
+        }
+        __nanosleep(32);
+    }
+}
+
 __device__ __forceinline__ int steps_of_k(const GemmParams& p, const Tile& w) { return ((w.mode == GRAM ? p.ldx : p.lda) + KB - 1) / KB; }
 
 // Byte offset of 16-byte chunk c (8 halves) of row r in a 64-byte-swizzled block.
@@ -457,8 +479,9 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     volatile int* sched_slot = reinterpret_cast<volatile int*>(tmem_slot + 2);   // [SCHED_DEPTH] list positions
     const uint32_t sched_slot_addr = bars + 8u * NUM_BARS + 8u;
+    const uint32_t ready_addr = sched_slot_addr + 4u * SCHED_DEPTH;          // the last list position whose inputs the producer found complete
     const uint32_t epi = bars + 1024u;                                       // 1024-byte aligned
-    static_assert(8 * NUM_BARS + 8 + 4 * SCHED_DEPTH <= 1024, "barriers before the epilogue's staging");
+    static_assert(8 * NUM_BARS + 12 + 4 * SCHED_DEPTH <= 1024, "barriers before the epilogue's staging");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
@@ -467,6 +490,7 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
 
     if (threadIdx.x == 0) {
         *abort_flag = 0;
+        store_ready(ready_addr, -1);
         for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 2 * EPI_WARPS); }
         mbar_init(drain_bar, 1);
@@ -519,7 +543,8 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
                 }
                 if (t < 0) break;
                 const Tile w = decode(p, t);
-                if (w.k > 0 && !flag_wait_ge(p.done + w.b, w.need, abort_flag, p.wait_limit_ns)) { ok = false; break; }
+                if (w.k > 0 && !flag_wait_ge(p.done + w.b * DONE_PITCH, w.need, abort_flag, p.wait_limit_ns)) { ok = false; break; }
+                store_ready(ready_addr, t);
                 const int xb = (w.k / 3) & 1;
                 const CUtensorMap* ma = w.mode == GRAM ? &maps.x_l[xb] : w.mode == POLY ? &maps.a_l : &maps.b_l;
                 const CUtensorMap* mb = w.mode == GRAM ? &maps.x_r[xb] : w.mode == POLY ? &maps.a_r : &maps.x_mn[xb];
@@ -633,7 +658,7 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
             };
             int ok = 1;
             if (lane == 0) {
-                if (addend) ok = flag_wait_ge(p.done + w.b, w.need, abort_flag, p.wait_limit_ns);
+                if (addend) ok = wait_ready(ready_addr, t, abort_flag, p.wait_limit_ns);
                 bulk_wait_read_all();                                        // the stores of the tile before have left the blocks
                 if (addend && ok) {
                     const int now = w.mode == POLY ? min(blocks_here, 2) : blocks_here;
@@ -680,7 +705,7 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(mapa_shared(tempty_bar(ab), 0));
-            if (!w.last && lane == 0) signal_stored(p.done + w.b);
+            if (!w.last && lane == 0) signal_stored(p.done + w.b * DONE_PITCH);
         }
         if (lane == 0) bulk_wait_all();                                      // nothing reads this CTA's shared memory any more
     }
