@@ -38,7 +38,7 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float
 constexpr int GEN_THREADS = 256;
 constexpr int COL_TILE = 32;            // columns per block of the column sums
 constexpr int COL_ROWS = 8;             // rows that a block of the column sums takes at a time
-constexpr int MAX_SLICES = 256;         // partial sums over rows: at least one block per SM
+constexpr int MAX_SLICES = 296;         // partial sums over rows: two blocks per SM of a 148-SM device
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -204,12 +204,13 @@ template <> __device__ __forceinline__ uint32_t narrow<__half>(float a, float b)
 
 // A thread's EPT columns: a warp owns 32 EPT neighbouring columns, in pieces of 32 N: lane l has N neighbours of each (N = 16 /
 // sizeof(T) where VEC, else 1).  Piece k begins at column first + 32 N k; pairs are neighbours in the thread's order.
-template <typename T, bool VEC, int EPT> struct Columns {
+// SPLIT: code of its own for warps that have all their columns (it pays in the forward pass, not in the longer backward one).
+template <typename T, bool VEC, int EPT, bool SPLIT> struct Columns {
     static constexpr int N = VEC ? 16 / static_cast<int>(sizeof(T)) : 1;
-    static constexpr int PIECES = EPT / N, PAIRS = EPT / 2, STEP = 32 * N, PART = 8 / N;
+    static constexpr int PAIRS = EPT / 2, STEP = 32 * N, PART = 8 / N;
     int first, d;
-    __device__ __forceinline__ Columns(int warp, int lane, int d_) : first(warp * 32 * EPT + lane * N), d(d_) {}
-    __device__ __forceinline__ bool whole() const { return first + STEP * (PIECES - 1) + STEP - N < d; }   // no lane of the warp lacks any (N divides d)
+    bool all;                                           // no lane of the warp lacks a column
+    __device__ __forceinline__ Columns(int warp, int lane, int d_) : first(warp * 32 * EPT + lane * N), d(d_), all((warp + 1) * 32 * EPT <= d_) {}
     __device__ __forceinline__ bool has(int k) const { return first + STEP * k < d; }    // VEC: d is a multiple of N
 
     // Eight of the thread's elements (part q of EPT / 8) of a row in shared memory (address of its first element); columns beyond
@@ -229,12 +230,18 @@ template <typename T, bool VEC, int EPT> struct Columns {
                     for (int i = 0; i < 4; ++i) v[4 * k + i] = widen<T>(w[i]);
                 }
             }
-        } else if constexpr (sizeof(T) == 4) {
+        } else {
+            if (SPLIT && all) read_single<true>(at, q, v);
+            else read_single<false>(at, q, v);
+        }
+    }
+    template <bool ALL> __device__ __forceinline__ void read_single(uint32_t at, int q, f2* v) const {
+        if constexpr (sizeof(T) == 4) {
             float f[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 f[k] = 0.f;
-                if (has(q * PART + k)) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f[k]) : "r"(at + k * 128));
+                if (ALL || has(q * PART + k)) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f[k]) : "r"(at + k * 128));
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = pair(f[2 * i], f[2 * i + 1]);
@@ -243,7 +250,7 @@ template <typename T, bool VEC, int EPT> struct Columns {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 h[k] = 0;
-                if (has(q * PART + k)) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h[k]) : "r"(at + k * 64));
+                if (ALL || has(q * PART + k)) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h[k]) : "r"(at + k * 64));
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = widen<T>(static_cast<uint32_t>(h[2 * i]) | static_cast<uint32_t>(h[2 * i + 1]) << 16);
@@ -282,12 +289,16 @@ template <typename T, bool VEC, int EPT> struct Columns {
                 if (has(q * PART + k)) *reinterpret_cast<uint4*>(at + STEP * k) = make_uint4(w[0], w[1], w[2], w[3]);
             }
         } else {
+            if (SPLIT && all) store_single<true>(at, q, v);
+            else store_single<false>(at, q, v);
+        }
+    }
+    template <bool ALL> __device__ __forceinline__ void store_single(T* at, int q, const f2* v) const {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 a = split(v[i]);
-                if (has(q * PART + 2 * i)) at[STEP * (2 * i)] = from_f<T>(a.x);
-                if (has(q * PART + 2 * i + 1)) at[STEP * (2 * i + 1)] = from_f<T>(a.y);
-            }
+        for (int i = 0; i < 4; ++i) {
+            const float2 a = split(v[i]);
+            if (ALL || has(q * PART + 2 * i)) at[STEP * (2 * i)] = from_f<T>(a.x);
+            if (ALL || has(q * PART + 2 * i + 1)) at[STEP * (2 * i + 1)] = from_f<T>(a.y);
         }
     }
 };
@@ -328,8 +339,8 @@ template <typename T, typename W, bool VEC, int EPT>
 __global__ void __maxnreg__(FORWARD_REGS) ln_forward_rows(const RowArgs a) {
     extern __shared__ __align__(128) uint8_t raw[];
     const Group g = group_setup<T, VEC, 1>(a, raw);
-    const Columns<T, VEC, EPT> cols(g.warp, g.lane, a.d);
-    using C = Columns<T, VEC, EPT>;
+    const Columns<T, VEC, EPT, true> cols(g.warp, g.lane, a.d);
+    using C = Columns<T, VEC, EPT, true>;
     float* const weights = reinterpret_cast<float*>(raw + WEIGHTS_OFFSET);
     const int n_weights = 32 * EPT * a.warps;
     if (g.id == 0) cols.fill(weights, g.warp, g.lane, static_cast<const W*>(a.g), 1.f);
@@ -338,7 +349,6 @@ __global__ void __maxnreg__(FORWARD_REGS) ln_forward_rows(const RowArgs a) {
     const uint32_t gw = vpce::smem_u32(weights) + (g.warp * (EPT / 4) * 32 + g.lane) * 16, bw = gw + 4 * n_weights;
     float2(*part)[MAX_GROUP_WARPS] = reinterpret_cast<Smem*>(raw)->part[g.id];
     const float inv_d = 1.f / static_cast<float>(a.d);
-    const bool whole = cols.whole();
     auto columns_of = [&](int warp) { return static_cast<float>(min(max(a.d - warp * 32 * EPT, 0), 32 * EPT)); };
     const float inv_mine = 1.f / columns_of(g.warp);
     const float n_lane = (g.lane & 15) < a.warps ? columns_of(g.lane & 15) : 0.f;
@@ -359,7 +369,7 @@ __global__ void __maxnreg__(FORWARD_REGS) ln_forward_rows(const RowArgs a) {
         const float sum = warp_sum(t.x + t.y), mine = sum * inv_mine;
         const f2 minus = pair(-mine, -mine);
         f2 q0 = 0ull, q1 = 0ull;
-        if (whole) {
+        if (cols.all) {
 #pragma unroll
             for (int i = 0; i < C::PAIRS; i += 2) {
                 const f2 e = add2(v[i], minus), f = add2(v[i + 1], minus);
@@ -411,8 +421,8 @@ template <typename T, typename W, bool VEC, int EPT>
 __global__ void __maxnreg__(BACKWARD_REGS) ln_backward_rows(const RowArgs a) {
     extern __shared__ __align__(128) uint8_t raw[];
     const Group g = group_setup<T, VEC, 2>(a, raw);
-    const Columns<T, VEC, EPT> cols(g.warp, g.lane, a.d);
-    using C = Columns<T, VEC, EPT>;
+    const Columns<T, VEC, EPT, false> cols(g.warp, g.lane, a.d);
+    using C = Columns<T, VEC, EPT, false>;
     float2(*part)[MAX_GROUP_WARPS] = reinterpret_cast<Smem*>(raw)->part[g.id];
     const float inv_d = 1.f / static_cast<float>(a.d);
     float* const weights = reinterpret_cast<float*>(raw + WEIGHTS_OFFSET);
@@ -512,6 +522,175 @@ __global__ void __maxnreg__(BACKWARD_REGS) ln_backward_rows(const RowArgs a) {
         float v = sums[c];
         for (int q = 1; q < a.groups; ++q) v += sums[static_cast<size_t>(q) * 2 * a.d + c];
         out[c] = v;
+    }
+}
+
+// ------------------------------------------------------------------------------------ narrow rows
+// Rows of up to 512 bytes on 16-byte boundaries (a norm over one head's 64 to 256 elements): L lanes hold a row, 16 bytes each,
+// so a warp has 32 / L rows at once, and UNROLL times as many under way.  A ring would be all barriers here: 2^20 rows of 64 bf16
+// took 285 us forward in it.
+constexpr int NARROW_BYTES = 512, NARROW_THREADS = 512, NARROW_WARPS = NARROW_THREADS / 32, UNROLL = 4;
+
+template <int L> __device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// 16 bytes as pairs, and back.
+template <typename T> struct Piece {
+    static constexpr int N = 16 / static_cast<int>(sizeof(T)), PAIRS = N / 2;
+    __device__ static __forceinline__ void unpack(uint4 q, f2* v) {
+        if constexpr (sizeof(T) == 4) {
+            v[0] = pair(__uint_as_float(q.x), __uint_as_float(q.y));
+            v[1] = pair(__uint_as_float(q.z), __uint_as_float(q.w));
+        } else {
+            v[0] = widen<T>(q.x); v[1] = widen<T>(q.y); v[2] = widen<T>(q.z); v[3] = widen<T>(q.w);
+        }
+    }
+    __device__ static __forceinline__ uint4 pack(const f2* v) {
+        uint32_t w[4];
+        if constexpr (sizeof(T) == 4) {
+            const float2 a = split(v[0]), b = split(v[1]);
+            w[0] = __float_as_uint(a.x); w[1] = __float_as_uint(a.y); w[2] = __float_as_uint(b.x); w[3] = __float_as_uint(b.y);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { const float2 a = split(v[i]); w[i] = narrow<T>(a.x, a.y); }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    template <typename W> __device__ static __forceinline__ void weights(const W* p, int c, bool has, float none, f2* v) {
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            const float a = has ? (p ? to_f(p[c + 2 * i]) : none) : 0.f, b = has ? (p ? to_f(p[c + 2 * i + 1]) : none) : 0.f;
+            v[i] = pair(a, b);
+        }
+    }
+};
+
+template <typename T, typename W, int L>
+__global__ void __launch_bounds__(NARROW_THREADS) ln_forward_narrow(const RowArgs a) {
+    using P = Piece<T>;
+    constexpr int PER = 32 / L;                         // rows of a warp at once
+    const int lane = threadIdx.x & 31, c = (lane & (L - 1)) * P::N;
+    const bool has = c < a.d;
+    const float inv_d = 1.f / static_cast<float>(a.d);
+    f2 gw[P::PAIRS], bw[P::PAIRS];
+    P::weights(static_cast<const W*>(a.g), c, has, 1.f, gw);
+    P::weights(static_cast<const W*>(a.b), c, has, 0.f, bw);
+    const int step = gridDim.x * NARROW_WARPS * PER * UNROLL;
+    for (int r0 = (blockIdx.x * NARROW_WARPS + (threadIdx.x >> 5)) * PER * UNROLL; r0 < a.rows; r0 += step) {
+        uint4 q[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int r = r0 + u * PER + lane / L;
+            q[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (has && r < a.rows) q[u] = *reinterpret_cast<const uint4*>(a.x.at(r) + c * sizeof(T));
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int r = r0 + u * PER + lane / L;
+            f2 v[P::PAIRS];
+            P::unpack(q[u], v);
+            f2 sum = v[0];
+#pragma unroll
+            for (int i = 1; i < P::PAIRS; ++i) sum = add2(sum, v[i]);
+            const float2 t = split(sum);
+            const float mu = lanes_sum<L>(t.x + t.y) * inv_d;
+            const f2 minus = has ? pair(-mu, -mu) : 0ull;                   // lanes beyond d hold 0 and stay 0
+            f2 sq = 0ull;
+#pragma unroll
+            for (int i = 0; i < P::PAIRS; ++i) { v[i] = add2(v[i], minus); sq = fma2(v[i], v[i], sq); }
+            const float2 w = split(sq);
+            const float rs = 1.f / sqrtf(lanes_sum<L>(w.x + w.y) * inv_d + a.eps);
+            const f2 rs2 = pair(rs, rs);
+#pragma unroll
+            for (int i = 0; i < P::PAIRS; ++i) v[i] = fma2(mul2(v[i], rs2), gw[i], bw[i]);
+            if (r < a.rows) {
+                if (has) *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + r * a.out_stride + c) = P::pack(v);
+                if (c == 0) {
+                    if (a.mean) a.mean[r] = mu;
+                    if (a.rstd) a.rstd[r] = rs;
+                }
+            }
+        }
+    }
+}
+
+template <typename T, typename W, int L>
+__global__ void __launch_bounds__(NARROW_THREADS, 2) ln_backward_narrow(const RowArgs a) {
+    using P = Piece<T>;
+    constexpr int PER = 32 / L, ROWS = UNROLL / 2;
+    __shared__ float sums[NARROW_WARPS][2][NARROW_BYTES / 2];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = (lane & (L - 1)) * P::N;
+    const bool has = c < a.d;
+    const float inv_d = 1.f / static_cast<float>(a.d);
+    f2 gw[P::PAIRS], dg[P::PAIRS], db[P::PAIRS];
+    P::weights(static_cast<const W*>(a.g), c, has, 1.f, gw);
+#pragma unroll
+    for (int i = 0; i < P::PAIRS; ++i) dg[i] = db[i] = 0ull;
+    const int step = gridDim.x * NARROW_WARPS * PER * ROWS;
+    for (int r0 = (blockIdx.x * NARROW_WARPS + warp) * PER * ROWS; r0 < a.rows; r0 += step) {
+        uint4 qx[ROWS], qu[ROWS];
+        float mu[ROWS], rs[ROWS];
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
+            const int r = r0 + u * PER + lane / L;
+            qx[u] = qu[u] = make_uint4(0u, 0u, 0u, 0u);
+            mu[u] = rs[u] = 0.f;
+            if (has && r < a.rows) {
+                qx[u] = *reinterpret_cast<const uint4*>(a.x.at(r) + c * sizeof(T));
+                qu[u] = *reinterpret_cast<const uint4*>(a.dy.at(r) + c * sizeof(T));
+                mu[u] = a.mean[r];
+                rs[u] = a.rstd[r];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
+            const int r = r0 + u * PER + lane / L;
+            f2 x[P::PAIRS], w[P::PAIRS], t[P::PAIRS];
+            P::unpack(qx[u], x);
+            P::unpack(qu[u], w);
+            const f2 minus_mu = pair(-mu[u] * rs[u], -mu[u] * rs[u]), rs2 = pair(rs[u], rs[u]);
+            f2 sa = 0ull, sax = 0ull;
+#pragma unroll
+            for (int i = 0; i < P::PAIRS; ++i) {
+                x[i] = fma2(x[i], rs2, minus_mu);                           // xh; 0 in lanes and rows that do not exist
+                dg[i] = fma2(w[i], x[i], dg[i]);
+                db[i] = add2(w[i], db[i]);
+                t[i] = mul2(w[i], gw[i]);
+                sa = add2(sa, t[i]);
+                sax = fma2(t[i], x[i], sax);
+            }
+            const float2 pa = split(sa), pax = split(sax);
+            const float ma = -rs[u] * lanes_sum<L>(pa.x + pa.y) * inv_d, mx = -rs[u] * lanes_sum<L>(pax.x + pax.y) * inv_d;
+            const f2 ma2 = pair(ma, ma), mx2 = pair(mx, mx);
+#pragma unroll
+            for (int i = 0; i < P::PAIRS; ++i) x[i] = fma2(t[i], rs2, fma2(x[i], mx2, ma2));
+            if (a.out && has && r < a.rows) *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + r * a.out_stride + c) = P::pack(x);
+        }
+    }
+    if (!a.partial) return;
+    // the warp's rows at once, then the block's warps in order
+#pragma unroll
+    for (int i = 0; i < P::PAIRS; ++i) {
+        float2 p = split(dg[i]), q = split(db[i]);
+#pragma unroll
+        for (int o = L; o < 32; o <<= 1) {
+            p.x += __shfl_xor_sync(0xffffffffu, p.x, o); p.y += __shfl_xor_sync(0xffffffffu, p.y, o);
+            q.x += __shfl_xor_sync(0xffffffffu, q.x, o); q.y += __shfl_xor_sync(0xffffffffu, q.y, o);
+        }
+        if (lane < L && has) {
+            sums[warp][0][c + 2 * i] = p.x; sums[warp][0][c + 2 * i + 1] = p.y;
+            sums[warp][1][c + 2 * i] = q.x; sums[warp][1][c + 2 * i + 1] = q.y;
+        }
+    }
+    __syncthreads();
+    float* out = a.partial + static_cast<size_t>(blockIdx.x) * 2 * a.d;
+    for (int k = threadIdx.x; k < 2 * a.d; k += NARROW_THREADS) {
+        const int which = k >= a.d ? 1 : 0, col = k - which * a.d;
+        float v = 0.f;
+        for (int w = 0; w < NARROW_WARPS; ++w) v += sums[w][which][col];
+        out[k] = v;
     }
 }
 
@@ -712,6 +891,13 @@ template <typename T, typename W, bool VEC> cudaError_t backward_rows(const RowA
     }
 }
 
+// Blocks of a narrow launch: `per_sm` an SM at most, none without rows.
+int narrow_grid(int64_t rows, int lanes, int unroll, int per_sm) {
+    const int64_t per = static_cast<int64_t>(NARROW_WARPS) * (32 / lanes) * unroll;
+    return static_cast<int>(std::min<int64_t>((rows + per - 1) / per, static_cast<int64_t>(per_sm) * sm_count()));
+}
+int narrow_lanes(int64_t bytes) { return bytes <= 128 ? 8 : bytes <= 256 ? 16 : 32; }
+
 int code(cudaError_t e) { return e == cudaSuccess ? VPCE_OK : VPCE_CUDA_ERROR; }
 
 template <typename T, typename W>
@@ -721,8 +907,15 @@ int forward_typed(const void* x, int64_t rows, int64_t d, int64_t xs, const void
         RowArgs a{};
         a.x = Rows{x, static_cast<long>(xs * sizeof(T))}; a.rows = static_cast<int>(rows); a.out_stride = ys; a.d = static_cast<int>(d); a.g = g; a.b = b; a.eps = eps; a.out = y;
         a.mean = mean; a.rstd = rstd;
-        const RowShape s = row_shape(&a, sizeof(T), 1);
         const bool vec = d * sizeof(T) % 16 == 0 && rows_aligned(x, xs, sizeof(T)) && rows_aligned(y, ys, sizeof(T));
+        if (vec && d * sizeof(T) <= NARROW_BYTES) {
+            const int lanes = narrow_lanes(d * sizeof(T)), grid = narrow_grid(rows, lanes, UNROLL, 4);
+            if (lanes == 8) ln_forward_narrow<T, W, 8><<<grid, NARROW_THREADS, 0, st>>>(a);
+            else if (lanes == 16) ln_forward_narrow<T, W, 16><<<grid, NARROW_THREADS, 0, st>>>(a);
+            else ln_forward_narrow<T, W, 32><<<grid, NARROW_THREADS, 0, st>>>(a);
+            return code(cudaGetLastError());
+        }
+        const RowShape s = row_shape(&a, sizeof(T), 1);
         if (s.grid > 0) return code(vec ? forward_rows<T, W, true>(a, s, st) : forward_rows<T, W, false>(a, s, st));
     }
     ln_forward_generic<T, W><<<grid_rows(rows), GEN_THREADS, 0, st>>>(
@@ -742,9 +935,18 @@ int backward_typed(const void* dy, int64_t dys, const void* x, int64_t xs, int64
         a.rows = static_cast<int>(rows); a.out_stride = dxs; a.d = static_cast<int>(d); a.g = g;
         a.out = dx; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
         a.partial = dg || db ? partial : nullptr;
-        const RowShape s = row_shape(&a, sizeof(T), 2);
         const bool vec = d * sizeof(T) % 16 == 0 && rows_aligned(x, xs, sizeof(T)) && rows_aligned(dy, dys, sizeof(T)) &&
                          rows_aligned(dx, dxs, sizeof(T));
+        if (vec && d * sizeof(T) <= NARROW_BYTES) {
+            const int lanes = narrow_lanes(d * sizeof(T)), grid = std::min(narrow_grid(rows, lanes, UNROLL / 2, 2), slices);
+            if (lanes == 8) ln_backward_narrow<T, W, 8><<<grid, NARROW_THREADS, 0, st>>>(a);
+            else if (lanes == 16) ln_backward_narrow<T, W, 16><<<grid, NARROW_THREADS, 0, st>>>(a);
+            else ln_backward_narrow<T, W, 32><<<grid, NARROW_THREADS, 0, st>>>(a);
+            if (a.partial)
+                ln_backward_finish<W><<<col_tiles, COL_TILE * FIN_ROWS, 0, st>>>(partial, grid, d, static_cast<W*>(dg), static_cast<W*>(db));
+            return code(cudaGetLastError());
+        }
+        const RowShape s = row_shape(&a, sizeof(T), 2);
         if (s.grid > 0) {
             if (cudaError_t e = vec ? backward_rows<T, W, true>(a, s, st) : backward_rows<T, W, false>(a, s, st); e != cudaSuccess)
                 return VPCE_CUDA_ERROR;

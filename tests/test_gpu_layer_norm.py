@@ -111,7 +111,7 @@ TYPES = [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (tor
 @pytest.mark.parametrize("dtype,wdtype", TYPES)
 @pytest.mark.parametrize("rows,d", [(1, 1), (3, 2), (1, 2880), (5, 7), (64, 64), (33, 255), (300, 256), (17, 257), (700, 1000),
                                     (149, 1111), (37, 2880), (20, 4096), (9, 7168), (6, 8192), (5, 8200), (3, 12288), (2, 20001), (4, 16384), (3, 16383),
-                                    (1500, 96)])
+                                    (1500, 96), (4001, 64), (777, 128), (2049, 200), (1003, 8), (5, 256)])
 def test_matches_oracle(rows, d, dtype, wdtype):
     check(*make(rows, d, dtype, wdtype, seed=rows * 7 + d))
 
