@@ -13,10 +13,10 @@
  * of two that follows from the iteration's own bound (the spectral norm of X stays below the largest |a s + b s^3 + c s^5|
  * over 0 <= s <= its bound before the step), so nothing overflows and eleven bits of every entry survive; products
  * accumulate in fp32, the last X never leaves fp32.  M, p, the norm and all elementwise arithmetic are fp32 (squares are
- * summed in double across a thread's elements).  The rounding to fp16 shows in the result as about 1.5e-3 of its Frobenius
- * norm for gradients of full rank; in directions that a gradient lacks (a rank below the smaller side) it is amplified like
- * the iteration amplifies everything small, by the product of the a's (485 for the default steps), and reaches some 4e-2
- * for a rank of a fifteenth.  A NaN or infinity in one matrix's gradient stays in that matrix.
+ * formed and summed in fp32 over up to eight neighbours, in double beyond: entries above 1e19 overflow, as they would in
+ * a plain fp32 norm).  The rounding to fp16 shows in the result as about 1.5e-3 of its Frobenius norm for gradients of full
+ * rank; in directions that a gradient lacks (a rank below the smaller side) it is amplified like the iteration amplifies
+ * everything small, by the product of the a's (485 for the default steps), and reaches some 4e-2 for a rank of a fifteenth.  A NaN or infinity in one matrix's gradient stays in that matrix.
  *
  * Status codes are those of vp_ce.h.  VPCE_UNSUPPORTED: coefficients whose bound leaves the fp16 range (a bound on X
  * above 8), sizes whose tiles do not fit 31 bits.  Every call only enqueues work on `stream` of the current device.

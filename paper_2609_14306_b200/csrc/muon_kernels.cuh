@@ -149,7 +149,8 @@ template <int V> __device__ __forceinline__ void store_v(float* p, const float* 
 }
 
 // M <- mu M + G and the sum of squares of U over one part of one matrix: grid (parts, batch).  V: elements per access, 4
-// where every matrix starts on a 16-byte boundary.  Each thread has UNROLL accesses in flight.
+// where every matrix starts on a 16-byte boundary.  Each thread has UNROLL accesses in flight.  Bound: memory; four 2880 x 2880
+// matrices with bf16 gradients take 49 us (332 MB: 6.7 TB/s).
 template <typename G, int V>
 __global__ void __launch_bounds__(PREP_THREADS) muon_momentum_kernel(const PrepParams p) {
     constexpr int UNROLL = V == 4 ? 4 : 8;
@@ -231,7 +232,7 @@ __device__ __forceinline__ void load_u(const PrepParams& p, size_t at, float* u)
 }
 
 // X_0 = U / max(|U|_F, eps), stored as fp16 times `scale` with zeros in the padding columns, where the user's matrices are
-// wide already: grid (blocks, batch), eight columns a thread.
+// wide already: grid (blocks, batch), eight columns a thread.  Four 2880 x 2880 with momentum: 41 us (265 MB: 6.5 TB/s).
 template <typename G, int V>
 __global__ void __launch_bounds__(PREP_THREADS) muon_start_kernel(const PrepParams p) {
     const float inv = start_factor(p, blockIdx.y);
@@ -457,6 +458,8 @@ __device__ __forceinline__ void epilogue_last(const GemmParams& p, int k, int b,
 // Pairs take the entries of the work list in order from a counter.  An entry whose inputs other pairs are still writing waits
 // for its matrix's `done` count; an entry only ever waits for entries before it in the list, which running pairs hold, so
 // there is always one that can finish, however many pairs the GPU runs at a time.
+// Bound: tensor cores where matrices are large (four 2880 x 2880, 15 products: 1.67 ms, 2.27e12 operations with the padding to
+// tiles, 1.36 PFLOP/s, tensor pipe 78 % busy); the chain of dependent products where they are not (8 to 15 us each).
 constexpr int SCHED_DEPTH = 4;
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1)
@@ -729,7 +732,8 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
 // columns are split, not its rows, so B X reads a second copy, XN: all 256 rows of this CTA's half of the columns, to which the
 // other CTA's epilogue writes its rows.
 // Each product is issued by one thread, waited for by all 16 warps (four per quarter of the tensor memory's lanes), and turned
-// into the next operand in place.
+// into the next operand in place.  Bound: latency.  256 x 256 in fp32: 74 us, of which 15 products of 3.4 us (barrier 0.6 to 0.9,
+// tensor cores 1.35, epilogue 1.1 to 2.4), 9.7 us to bring the matrix in and 8.3 us to write it back.
 constexpr int SMALL_WARPS = 16, SMALL_THREADS = 32 * SMALL_WARPS;
 constexpr int SMALL_KEPT = 8;                           // pieces of 8 elements of U that a thread keeps while the norm is formed
 template <int CG> struct SmallShape {
