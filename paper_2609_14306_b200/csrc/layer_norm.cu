@@ -12,7 +12,7 @@
 //   VEC      every row starts on a 16-byte boundary: 16-byte accesses
 //   !VEC     any alignment: the copies take the 16-byte granules that a row touches (cut at the tensor's ends, whose few
 //            elements are copied one by one), threads read single elements at the row's offset, neighbours side by side:
-//            2.6 to 3.8 TB/s forward and 1.9 to 3.2 backward in 16 bits, where VEC has 4.6 to 5.3 and 4.4 to 5.1 (2^26 elements)
+//            2.8 to 3.8 TB/s forward and 2.6 to 3.6 backward in 16 bits, where VEC has 4.8 to 5.3 and 4.4 to 5.1 (2^26 elements)
 //
 // Generic kernels (wider rows): one block per row, elements read one at a time in the order of the threads, three passes over
 // a row that the caches hold after the first.
@@ -79,11 +79,11 @@ constexpr int MAX_SMEM = 227 * 1024;
 constexpr int64_t MAX_ROWS = (int64_t{1} << 31) - (1 << 20);   // row numbers and the look-ahead stay below 2^31
 constexpr int64_t MAX_ROW = 32 * MAX_GROUP_WARPS * MAX_EPT;
 
-struct Smem {                                           // of a block: barriers, reduction scratch; then weights, ring
-    uint64_t full[MAX_GROUPS][MAX_STAGES];              // [group][stage]
-    float2 part[MAX_GROUPS][2][MAX_GROUP_WARPS];        // [group][turn][warp]
-};
-constexpr int WEIGHTS_OFFSET = (sizeof(Smem) + 127) / 128 * 128;
+// Shared memory of a block: barriers [MAX_GROUPS][MAX_STAGES], weights, reduction scratch (`part`, float2 [group][turn][warp]), ring.
+// The scratch is for the groups that the launch has: at 8192 columns of 16 bits that is what lets the backward pass's two groups
+// have three stages each (two: 108 us for 8192 rows, three: 82).
+constexpr int FULL_BYTES = MAX_GROUPS * MAX_STAGES * 8, PART_BYTES = 2 * MAX_GROUP_WARPS * 8;
+static_assert(FULL_BYTES % 128 == 0 && PART_BYTES % 128 == 0, "what follows begins on a 128-byte boundary");
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -113,6 +113,17 @@ struct RowArgs {
     float *mean, *rstd;                                 // written (forward, may be null) or read (backward)
     float* partial;                                     // [blocks][2][d] or null
 };
+// The same, longer.  With more than 112 bytes of arguments the compiler keeps them in registers instead of reading them where they
+// are used.  That serves the forward kernels (2^26 bf16 elements: 54 us instead of 58 at 10000 columns, 52 instead of 56 at 64)
+// and the backward pass on unaligned rows (120 instead of 170 at 2881); on aligned rows that spills and
+// takes 91 instead of 78.
+struct LongRowArgs : RowArgs { int64_t none; };
+template <typename Args> Args args_of(const RowArgs& a) {
+    Args r{};
+    static_cast<RowArgs&>(r) = a;
+    return r;
+}
+template <bool VEC> using BackwardArgs = std::conditional_t<VEC, RowArgs, LongRowArgs>;
 
 // What row r of an array takes: `*from`, the address from which the bulk copy reads, `*at`, where it lands in the slot, and the
 // bytes that it moves.  The row's first element lands shift(r) bytes into the slot.  A granule that reaches over the tensor's
@@ -321,7 +332,6 @@ struct Group {
 };
 template <typename T, bool VEC, int NA>
 __device__ __forceinline__ Group group_setup(const RowArgs& a, uint8_t* raw) {
-    Smem* sm = reinterpret_cast<Smem*>(raw);
     Group g;
     g.id = (threadIdx.x >> 5) / a.warps;
     g.warp = (threadIdx.x >> 5) - g.id * a.warps;
@@ -329,7 +339,7 @@ __device__ __forceinline__ Group group_setup(const RowArgs& a, uint8_t* raw) {
     g.first = blockIdx.x * a.groups + g.id;
     g.step = gridDim.x * a.groups;
     g.ring = raw + a.ring + g.id * a.stages * a.slot;
-    g.bars = vpce::smem_u32(&sm->full[g.id][0]);
+    g.bars = vpce::smem_u32(raw) + g.id * MAX_STAGES * 8;
     if (g.warp == 0 && g.lane == 0) {
         for (int s = 0; s < a.stages; ++s) vpce::mbar_init(g.bars + 8 * s, NA);
         vpce::fence_barrier_init();
@@ -345,18 +355,18 @@ __device__ __forceinline__ Group group_setup(const RowArgs& a, uint8_t* raw) {
 }
 
 template <typename T, typename W, bool VEC, int EPT>
-__global__ void __maxnreg__(FORWARD_REGS) ln_forward_rows(const RowArgs a) {
+__global__ void __maxnreg__(FORWARD_REGS) ln_forward_rows(const LongRowArgs a) {
     extern __shared__ __align__(128) uint8_t raw[];
     const Group g = group_setup<T, VEC, 1>(a, raw);
     const Columns<T, VEC, EPT, true> cols(g.warp, g.lane, a.d);
     using C = Columns<T, VEC, EPT, true>;
-    float* const weights = reinterpret_cast<float*>(raw + WEIGHTS_OFFSET);
+    float* const weights = reinterpret_cast<float*>(raw + FULL_BYTES);
     const int n_weights = 32 * EPT * a.warps;
     if (g.id == 0) cols.fill(weights, g.warp, g.lane, static_cast<const W*>(a.g), 1.f);
     if (g.id == a.groups - 1) cols.fill(weights + n_weights, g.warp, g.lane, static_cast<const W*>(a.b), 0.f);
     __syncthreads();
     const uint32_t gw = vpce::smem_u32(weights) + (g.warp * (EPT / 4) * 32 + g.lane) * 16, bw = gw + 4 * n_weights;
-    float2(*part)[MAX_GROUP_WARPS] = reinterpret_cast<Smem*>(raw)->part[g.id];
+    float2(*part)[MAX_GROUP_WARPS] = reinterpret_cast<float2(*)[MAX_GROUP_WARPS]>(raw + a.ring - (a.groups - g.id) * PART_BYTES);
     const float inv_d = 1.f / static_cast<float>(a.d);
     auto columns_of = [&](int warp) { return static_cast<float>(min(max(a.d - warp * 32 * EPT, 0), 32 * EPT)); };
     const float inv_mine = 1.f / columns_of(g.warp);
@@ -427,14 +437,14 @@ __global__ void __maxnreg__(FORWARD_REGS) ln_forward_rows(const RowArgs a) {
 }
 
 template <typename T, typename W, bool VEC, int EPT>
-__global__ void __maxnreg__(BACKWARD_REGS) ln_backward_rows(const RowArgs a) {
+__global__ void __maxnreg__(BACKWARD_REGS) ln_backward_rows(const BackwardArgs<VEC> a) {
     extern __shared__ __align__(128) uint8_t raw[];
     const Group g = group_setup<T, VEC, 2>(a, raw);
     const Columns<T, VEC, EPT, false> cols(g.warp, g.lane, a.d);
     using C = Columns<T, VEC, EPT, false>;
-    float2(*part)[MAX_GROUP_WARPS] = reinterpret_cast<Smem*>(raw)->part[g.id];
+    float2(*part)[MAX_GROUP_WARPS] = reinterpret_cast<float2(*)[MAX_GROUP_WARPS]>(raw + a.ring - (a.groups - g.id) * PART_BYTES);
     const float inv_d = 1.f / static_cast<float>(a.d);
-    float* const weights = reinterpret_cast<float*>(raw + WEIGHTS_OFFSET);
+    float* const weights = reinterpret_cast<float*>(raw + FULL_BYTES);
     if (g.id == 0) cols.fill(weights, g.warp, g.lane, static_cast<const W*>(a.g), 1.f);
     __syncthreads();
     const uint32_t gw = vpce::smem_u32(weights) + (g.warp * (EPT / 4) * 32 + g.lane) * 16;
@@ -537,7 +547,7 @@ __global__ void __maxnreg__(BACKWARD_REGS) ln_backward_rows(const RowArgs a) {
 // ------------------------------------------------------------------------------------ narrow rows
 // Rows of up to 512 bytes on 16-byte boundaries (a norm over one head's 64 to 256 elements): L lanes hold a row, 16 bytes each,
 // so a warp has 32 / L rows at once, and UNROLL times as many under way.  A ring would be all barriers here: 2^26 bf16
-// elements take 56 us forward and 75 backward here at any of these widths; in the ring 285 and 408 at 64 columns, 147 and 211 at
+// elements take 52 us forward and 75 backward here at any of these widths; in the ring 285 and 408 at 64 columns, 147 and 211 at
 // 128, 78 and 115 at 256.
 constexpr int NARROW_BYTES = 512, NARROW_THREADS = 512, NARROW_WARPS = NARROW_THREADS / 32, UNROLL = 4;
 
@@ -578,7 +588,7 @@ template <typename T> struct Piece {
 };
 
 template <typename T, typename W, int L>
-__global__ void __launch_bounds__(NARROW_THREADS) ln_forward_narrow(const RowArgs a) {
+__global__ void __launch_bounds__(NARROW_THREADS) ln_forward_narrow(const LongRowArgs a) {
     using P = Piece<T>;
     constexpr int PER = 32 / L;                         // rows of a warp at once
     const int lane = threadIdx.x & 31, c = (lane & (L - 1)) * P::N;
@@ -858,9 +868,10 @@ RowShape row_shape(RowArgs* a, size_t elem, int na) {
     a->groups = std::max(1, a->warps > 1 ? std::min(most, 15) : most);          // named barriers 1 to 15
     while (a->groups > 1 && static_cast<int64_t>(a->groups - 1) * sm_count() >= a->rows) --a->groups;   // few rows: spread over the SMs
     a->cap = static_cast<int>((a->d * elem + 15) / 16 * 16 + 16);
-    a->ring = WEIGHTS_OFFSET + (na == 1 ? 2 : 1) * 4 * 32 * s.ept * a->warps;
     a->slot = na * a->cap + (na == 2 ? 16 : 0);
-    while (a->groups > 1 && a->ring + a->groups * 2 * a->slot > MAX_SMEM) --a->groups;
+    auto ring = [&] { return FULL_BYTES + a->groups * PART_BYTES + (na == 1 ? 2 : 1) * 4 * 32 * s.ept * a->warps; };
+    while (a->groups > 1 && ring() + a->groups * 2 * a->slot > MAX_SMEM) --a->groups;
+    a->ring = ring();
     a->stages = std::min(MAX_STAGES, (MAX_SMEM - a->ring) / (a->groups * a->slot));
     s.threads = 32 * a->warps * a->groups;
     s.smem = a->ring + a->groups * a->stages * a->slot;
@@ -870,7 +881,7 @@ RowShape row_shape(RowArgs* a, size_t elem, int na) {
     return s;
 }
 
-template <void (*kern)(const RowArgs)> cudaError_t launch_rows(const RowArgs& a, const RowShape& s, cudaStream_t st) {
+template <typename Args, void (*kern)(const Args)> cudaError_t launch_rows(const RowArgs& a, const RowShape& s, cudaStream_t st) {
     static std::atomic<int> raised[64];                                         // of this kernel, per device
     int dev = 0;
     if (cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess) return e;
@@ -878,7 +889,7 @@ template <void (*kern)(const RowArgs)> cudaError_t launch_rows(const RowArgs& a,
         if (cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM); e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) raised[dev].store(1, std::memory_order_release);
     }
-    kern<<<s.grid, s.threads, s.smem, st>>>(a);
+    kern<<<s.grid, s.threads, s.smem, st>>>(args_of<Args>(a));
     return cudaGetLastError();
 }
 
@@ -886,18 +897,18 @@ bool rows_aligned(const void* p, int64_t stride, size_t e) { return aligned_to(p
 
 template <typename T, typename W, bool VEC> cudaError_t forward_rows(const RowArgs& a, const RowShape& s, cudaStream_t st) {
     switch (s.ept) {
-        case 8: return launch_rows<ln_forward_rows<T, W, VEC, 8>>(a, s, st);
-        case 16: return launch_rows<ln_forward_rows<T, W, VEC, 16>>(a, s, st);
-        case 24: return launch_rows<ln_forward_rows<T, W, VEC, 24>>(a, s, st);
-        default: return launch_rows<ln_forward_rows<T, W, VEC, 32>>(a, s, st);
+        case 8: return launch_rows<LongRowArgs, ln_forward_rows<T, W, VEC, 8>>(a, s, st);
+        case 16: return launch_rows<LongRowArgs, ln_forward_rows<T, W, VEC, 16>>(a, s, st);
+        case 24: return launch_rows<LongRowArgs, ln_forward_rows<T, W, VEC, 24>>(a, s, st);
+        default: return launch_rows<LongRowArgs, ln_forward_rows<T, W, VEC, 32>>(a, s, st);
     }
 }
 template <typename T, typename W, bool VEC> cudaError_t backward_rows(const RowArgs& a, const RowShape& s, cudaStream_t st) {
     switch (s.ept) {
-        case 8: return launch_rows<ln_backward_rows<T, W, VEC, 8>>(a, s, st);
-        case 16: return launch_rows<ln_backward_rows<T, W, VEC, 16>>(a, s, st);
-        case 24: return launch_rows<ln_backward_rows<T, W, VEC, 24>>(a, s, st);
-        default: return launch_rows<ln_backward_rows<T, W, VEC, 32>>(a, s, st);
+        case 8: return launch_rows<BackwardArgs<VEC>, ln_backward_rows<T, W, VEC, 8>>(a, s, st);
+        case 16: return launch_rows<BackwardArgs<VEC>, ln_backward_rows<T, W, VEC, 16>>(a, s, st);
+        case 24: return launch_rows<BackwardArgs<VEC>, ln_backward_rows<T, W, VEC, 24>>(a, s, st);
+        default: return launch_rows<BackwardArgs<VEC>, ln_backward_rows<T, W, VEC, 32>>(a, s, st);
     }
 }
 
@@ -920,9 +931,9 @@ int forward_typed(const void* x, int64_t rows, int64_t d, int64_t xs, const void
         const bool vec = d * sizeof(T) % 16 == 0 && rows_aligned(x, xs, sizeof(T)) && rows_aligned(y, ys, sizeof(T));
         if (vec && d * sizeof(T) <= NARROW_BYTES) {
             const int lanes = narrow_lanes(d * sizeof(T)), grid = narrow_grid(rows, lanes, UNROLL, 4);
-            if (lanes == 8) ln_forward_narrow<T, W, 8><<<grid, NARROW_THREADS, 0, st>>>(a);
-            else if (lanes == 16) ln_forward_narrow<T, W, 16><<<grid, NARROW_THREADS, 0, st>>>(a);
-            else ln_forward_narrow<T, W, 32><<<grid, NARROW_THREADS, 0, st>>>(a);
+            if (lanes == 8) ln_forward_narrow<T, W, 8><<<grid, NARROW_THREADS, 0, st>>>(args_of<LongRowArgs>(a));
+            else if (lanes == 16) ln_forward_narrow<T, W, 16><<<grid, NARROW_THREADS, 0, st>>>(args_of<LongRowArgs>(a));
+            else ln_forward_narrow<T, W, 32><<<grid, NARROW_THREADS, 0, st>>>(args_of<LongRowArgs>(a));
             return code(cudaGetLastError());
         }
         const RowShape s = row_shape(&a, sizeof(T), 1);
