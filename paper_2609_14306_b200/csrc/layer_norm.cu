@@ -6,8 +6,8 @@
 // in registers over all rows of its group, so the weight's gradient costs no second pass over the data, only one partial sum
 // per block.  The variance is taken from the centred values in registers.  Bound: memory, two passes over the rows forward,
 // three backward; at 16-bit types the arithmetic is nearly as scarce, so it runs on pairs (fp32x2 instructions).  Measured on
-// 65536 x 7168 bf16, fp32 weights: 299 us forward, 426 us backward (6.3 and 6.6 TB/s, the rate of a plain copy), 845 us for
-// both in sustained repetition, where the lowered clock shows the arithmetic; 16384 x 2880: 103 us for both.  Registers without
+// 65536 x 7168 bf16, fp32 weights: 299 us forward, 426 us backward (6.3 and 6.6 TB/s, the rate of a plain copy), 796 us for
+// both in sustained repetition, where the lowered clock shows the arithmetic; 16384 x 2880: 102 us for both.  Registers without
 // a spill matter most: 24 to 60 bytes of spill in the row loop cost 10 to 25 %.
 //   VEC      every row starts on a 16-byte boundary: 16-byte accesses
 //   !VEC     any alignment: the copies take the 16-byte granules that a row touches (cut at the tensor's ends, whose few
