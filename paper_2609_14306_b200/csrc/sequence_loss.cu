@@ -396,7 +396,8 @@ template <bool POLICY> __global__ void __launch_bounds__(FIN_THREADS) seq_small_
     Tokens<POLICY, true, SMALL_PER_LANE> k;
     k.load(a, 0, t0, t1, lane, 0.f);                                        // nothing where t0 >= T
     const float up = a.upstream ? *a.upstream : 1.f;
-    for (int i = threadIdx.x; i <= n; i += blockDim.x) offsets[i] = seq_begin(a, i);
+    if (n > 0)                                                              // without sequences a.offsets may be null
+        for (int i = threadIdx.x; i <= n; i += blockDim.x) offsets[i] = seq_begin(a, i);
     for (int i = threadIdx.x; i < n; i += blockDim.x) seq_sum[i] = make_float2(0.f, 0.f);   // of offsets that do not rise nobody may write it
     if (POLICY && !a.adv_per_token)
         for (int i = threadIdx.x; i < n; i += blockDim.x) adv[i] = a.adv[i];

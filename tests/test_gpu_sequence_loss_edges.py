@@ -1,0 +1,47 @@
+"""Policy and preference loss at the edges of what the C entries accept, where the paths of small and large calls meet, and
+where the terms are small differences of large numbers.  Oracle and helpers are those of test_gpu_sequence_loss."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_14306_b200 as vp
+
+pytestmark = pytest.mark.gpu
+
+
+def library():
+    vp.vp_policy_loss_workspace_bytes(0, 0)                              # binds the signatures
+    return vp.load_library()
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+# ------------------------------------------------------------------------------------------------ calls without sequences
+@pytest.mark.parametrize("T", [0, 1, 300, 8192, 8193])
+def test_no_sequences_and_null_offsets(T):
+    """n_seqs == 0 needs no offsets: statistics and gradients are 0 in the one-launch and the three-launch path."""
+    lib = library()
+    x = torch.randn(max(T, 1), device="cuda")
+    d = torch.full((T + 8,), 9.0, device="cuda")
+    s4, s3 = torch.full((4,), 9.0, device="cuda"), torch.full((3,), 9.0, device="cuda")
+    ws = torch.full((vp.vp_policy_loss_workspace_bytes(T, 0),), 255, dtype=torch.uint8, device="cuda")
+    for per_token in (0, 1):
+        for aggregate in (0, 1):
+            d.fill_(9.0), s4.fill_(9.0)
+            args = (x.data_ptr(), x.data_ptr(), x.data_ptr(), x.data_ptr() if per_token else None, per_token, None, None, T, 0, 0.2,
+                    0.2, 0.1, aggregate)
+            assert lib.vp_policy_loss(*args, s4.data_ptr(), d.data_ptr(), None, ws.data_ptr(), ws.numel(), stream()) == 0
+            torch.cuda.synchronize()
+            assert not s4.any() and not d[:T].any() and (d[T:] == 9).all()
+            d.fill_(9.0)
+            assert lib.vp_policy_loss_backward(*args, d.data_ptr(), None, ws.data_ptr(), ws.numel(), stream()) == 0
+            torch.cuda.synchronize()
+            assert not d[:T].any() and (d[T:] == 9).all()
+    for kind in (0, 1):
+        d.fill_(9.0), s3.fill_(9.0)
+        assert lib.vp_preference_loss(x.data_ptr(), None, None, None, T, 0, 0.1, 0.0, 0.0, kind, 0, s3.data_ptr(), None, d.data_ptr(), None,
+                                      ws.data_ptr(), ws.numel(), stream()) == 0
+        torch.cuda.synchronize()
+        assert not s3.any() and not d[:T].any() and (d[T:] == 9).all()
