@@ -534,8 +534,8 @@ template <bool POLICY> int launch_all(const SeqArgs& a, bool backward, cudaStrea
         if (a.T <= SMALL_T && a.n_seqs <= SMALL_SEQS)
             // as many warps as there are tiles; the join of many sequences takes a few more
             return launch(seq_small_kernel<POLICY>, 1, static_cast<int>(32 * std::max<int64_t>((a.T + SMALL_TILE - 1) / SMALL_TILE, a.n_seqs > 64 ? 16 : 4)), a, false, st) == cudaSuccess ? VPCE_OK : VPCE_CUDA_ERROR;
-        e = launch(seq_sums_kernel<POLICY>, blocks_for(a), THREADS, a, false, st);
-        if (e == cudaSuccess) e = launch(seq_finish_kernel<POLICY>, 1, FIN_THREADS, a, true, st);
+        if (a.n_tiles > 0) e = launch(seq_sums_kernel<POLICY>, blocks_for(a), THREADS, a, false, st);   // many sequences may share no token at all
+        if (e == cudaSuccess) e = launch(seq_finish_kernel<POLICY>, 1, FIN_THREADS, a, a.n_tiles > 0, st);
     }
     if (e == cudaSuccess && grad) e = launch(seq_grad_kernel<POLICY>, blocks_for(a), THREADS, a, !backward, st);
     return e == cudaSuccess ? VPCE_OK : VPCE_CUDA_ERROR;

@@ -45,3 +45,27 @@ def test_no_sequences_and_null_offsets(T):
                                       ws.data_ptr(), ws.numel(), stream()) == 0
         torch.cuda.synchronize()
         assert not s3.any() and not d[:T].any() and (d[T:] == 9).all()
+
+
+# ------------------------------------------------------------------------------------------------ sequences without tokens
+@pytest.mark.parametrize("n", [2, 1024, 1026, 5000])
+def test_sequences_but_no_tokens(n):
+    """T == 0 with few and with many sequences: every sequence is empty.  The policy loss is 0; the preference loss is the loss
+    of D = 0, exactly (one fp32 rounding of log 2 and its like)."""
+    f = torch.empty(0, device="cuda")
+    off = torch.zeros(n + 1, dtype=torch.int64, device="cuda")
+    adv = torch.randn(n, device="cuda")
+    for aggregate in ("token_mean", "seq_mean"):
+        stats = torch.full((4,), 9.0, device="cuda")
+        ws = torch.full((vp.vp_policy_loss_workspace_bytes(0, n),), 255, dtype=torch.uint8, device="cuda")
+        vp.vp_policy_loss(f, f, f, adv, None, off, 0.2, 0.2, 0.1, aggregate, stats, f.clone(), ws, adv_per_token=False)
+        vp.vp_policy_loss_backward(f, f, f, adv, None, off, 0.2, 0.2, 0.1, aggregate, f.clone(), ws, adv_per_token=False)
+        assert not stats.any()
+    for kind, loss in (("sigmoid", np.log(2.0)), ("ipo", 25.0)):
+        stats, rewards = torch.full((3,), 9.0, device="cuda"), torch.full((n,), 9.0, device="cuda")
+        ws = torch.full((vp.vp_preference_loss_workspace_bytes(0, n // 2),), 255, dtype=torch.uint8, device="cuda")
+        vp.vp_preference_loss(f, None, None, off, 0.1, 0.0, 0.0, kind, True, stats, rewards, f.clone(), ws)
+        vp.vp_preference_loss_backward(None, off, f.clone(), ws)
+        got = stats.cpu().numpy()
+        assert abs(got[0] - loss) <= 2.0 ** -22 * loss and got[1] == 0 and got[2] == 0
+        assert not rewards.any()
