@@ -95,6 +95,29 @@ __device__ __forceinline__ long first_seq(const SeqArgs& a, long t, int lane) {
     return lo;
 }
 
+// e^q - q - 1 and e^q - 1.  As differences from e^q they lose the digits that e^q shares with 1 + q: all of them at the |q| of a
+// policy that has just left its reference.  Below 1/2 the series of the first (to q^9 / 9!, which leaves out less than u / 25 of it)
+// stands instead, of the right sign by its form, and the second follows from it; from there on the differences are good to 20 u and 4 u.
+// Here and in policy_token the products that are fused with a sum are named, so that every kernel rounds alike: the gradient call
+// repeats the joint call's bits.
+__device__ __forceinline__ void kl_terms(float q, float& kl, float& x) {
+    if (fabsf(q) < 0.5f) {
+        float h = 1.f / 362880;
+        h = fmaf(q, h, 1.f / 40320);
+        h = fmaf(q, h, 1.f / 5040);
+        h = fmaf(q, h, 1.f / 720);
+        h = fmaf(q, h, 1.f / 120);
+        h = fmaf(q, h, 1.f / 24);
+        h = fmaf(q, h, 1.f / 6);
+        h = fmaf(q, h, 0.5f);
+        kl = __fmul_rn(__fmul_rn(q, q), h);
+        x = __fadd_rn(q, kl);
+    } else {
+        x = __fsub_rn(expf(q), 1.f);
+        kl = x - q;
+    }
+}
+
 // Terms of one token of the policy loss.  `clipped` compares in fp32, so a ratio exactly on a bound counts as unclipped.
 struct Policy { float l, grad, kl, clipped, r; };
 __device__ __forceinline__ Policy policy_token(const SeqArgs& a, float logp, float old_logp, float ref, float adv) {
@@ -103,13 +126,13 @@ __device__ __forceinline__ Policy policy_token(const SeqArgs& a, float logp, flo
     const bool clip = (adv > 0.f && p.r > a.hi) || (adv < 0.f && p.r < a.lo);
     p.clipped = clip ? 1.f : 0.f;
     p.l = -((clip ? (adv > 0.f ? a.hi : a.lo) : p.r) * adv);
-    p.grad = clip ? 0.f : -adv * p.r;
+    p.grad = clip ? 0.f : __fmul_rn(-adv, p.r);
     p.kl = 0.f;
     if (a.ref_logp) {
-        const float q = ref - logp, e = expf(q);
-        p.kl = e - q - 1.f;
+        float x;
+        kl_terms(ref - logp, p.kl, x);
         p.l += a.kl_coef * p.kl;
-        p.grad += a.kl_coef * (1.f - e);
+        p.grad = fmaf(-a.kl_coef, x, p.grad);
     }
     return p;
 }

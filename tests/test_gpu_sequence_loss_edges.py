@@ -69,3 +69,68 @@ def test_sequences_but_no_tokens(n):
         got = stats.cpu().numpy()
         assert abs(got[0] - loss) <= 2.0 ** -22 * loss and got[1] == 0 and got[2] == 0
         assert not rewards.any()
+
+
+# ------------------------------------------------------------------------------------------------ KL near the reference
+U = 2.0 ** -24
+
+
+def kl_terms(logp, ref):
+    """q, e^q - q - 1 and e^q - 1 in float64 of the fp32 inputs (at |q| >= 1e-7 the difference keeps eight digits there)."""
+    q = ref.astype(np.float64) - logp.astype(np.float64)
+    return q, np.expm1(q) - q, np.expm1(q)
+
+
+def run_policy(logp, old, ref, adv, off, kl_coef, aggregate):
+    T, n = len(logp), len(off) - 1
+    dev = [torch.from_numpy(np.ascontiguousarray(a)).cuda() for a in (logp, old, ref, adv)]
+    stats, d = torch.full((4,), float("nan"), device="cuda"), torch.full((T,), float("nan"), device="cuda")
+    ws = torch.full((vp.vp_policy_loss_workspace_bytes(T, n),), 255, dtype=torch.uint8, device="cuda")
+    args = (*dev, None, torch.tensor(off, dtype=torch.int64, device="cuda"), 0.2, 0.2, kl_coef, aggregate)
+    vp.vp_policy_loss(*args, stats, d, ws, adv_per_token=True)
+    again = torch.full_like(d, float("nan"))
+    vp.vp_policy_loss_backward(*args, again, ws, adv_per_token=True)
+    assert torch.equal(d, again)                                         # the gradient call repeats the joint call's bits
+    return stats.cpu().numpy().astype(np.float64), d.cpu().numpy().astype(np.float64)
+
+
+def test_kl_of_single_tokens():
+    """One token, so the statistic is its estimate.  Relative error: at most 35 u of the form (1 ulp of e^q over
+    the result, at |q| = 1/8 or beyond), q's rounding (2 + |q|) u, the mean's 2 u."""
+    logp = np.array([-1.0], np.float32)
+    for size in (1e-6, 1e-5, 1e-4, 1e-3, 1e-2, 0.1, 0.12499, 0.12501, 0.3, 1.0, 5.0):
+        for sign in (1.0, -1.0):
+            ref = (logp + np.float32(sign * size)).astype(np.float32)
+            q, kl, _ = kl_terms(logp, ref)
+            stats, _ = run_policy(logp, logp, ref, np.zeros(1, np.float32), [0, 1], 0.125, "token_mean")
+            tol = (40 + abs(q[0])) * U * kl[0]
+            assert stats[1] >= 0 and abs(stats[1] - kl[0]) <= tol, (size, sign, stats[1], kl[0])
+            assert abs(stats[0] - 0.125 * kl[0]) <= tol
+
+
+@pytest.mark.parametrize("aggregate", ["token_mean", "seq_mean"])
+@pytest.mark.parametrize("lens", [[700, 0, 41, 759], [9000, 1, 11000]])
+@pytest.mark.parametrize("spread", [1e-4, 1e-3, 3e-2, 0.3, 1.0])
+def test_kl_near_the_reference(spread, lens, aggregate):
+    """A policy that has just left its reference: mean and gradient keep their digits, whatever the distance.  With advantages
+    of 0 the loss is the KL term alone.  All terms have one sign, so errors are relative:
+        mean       (37 + |q|) u per token and (T / 1024 + 40) u of the sums, 4 u around them
+        gradient   2 u of e^q - 1, (1 + |q|) u of q, one each for kl_coef x, its weight, their product; 4 u spare"""
+    rng = np.random.default_rng(3)
+    off = np.concatenate([[0], np.cumsum(lens)])
+    T = int(off[-1])
+    logp = -np.abs(rng.standard_normal(T) * 1.5).astype(np.float32) - np.float32(0.5)
+    ref = (logp + rng.standard_normal(T) * spread).astype(np.float32)
+    q, kl, x = kl_terms(logp, ref)
+    stats, grad = run_policy(logp, logp, ref, np.zeros(T, np.float32), off, 0.125, aggregate)
+    biggest = np.abs(q).max()
+    rel = (37 + biggest + T / 1024 + 40 + 4) * U
+    if aggregate == "token_mean":
+        w = np.full(T, 1.0 / T)
+    else:
+        have = [n for n in lens if n]
+        w = np.concatenate([np.full(n, 1.0 / n / len(have)) for n in have])
+    assert stats[1] >= 0 and abs(stats[1] - kl.mean()) <= rel * kl.mean()
+    assert abs(stats[0] - 0.125 * (w * kl).sum()) <= rel * 0.125 * (w * kl).sum()
+    want = -0.125 * w * x
+    assert np.all(np.abs(grad - want) <= (10 + np.abs(q)) * U * np.abs(want))
