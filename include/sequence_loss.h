@@ -7,7 +7,8 @@
  * rising; entries are clamped to [0, T], so a wrong one gives a wrong result but no access out of range).  Tokens outside
  * every sequence, and tokens whose mask byte is 0, take part in nothing: their values may be anything (NaN, infinity) and
  * their gradient is 0.  mask NULL: every token of every sequence counts.  All values are fp32, sums over tokens are fp32
- * inside a tile of tokens and double across tiles, in a fixed order: the same call gives the same bits every time.
+ * inside a tile of tokens and double across tiles (and in what is formed from them: a pair's difference, a sequence's
+ * weight), in a fixed order: the same call gives the same bits every time.
  *
  * Status codes are those of vp_ce.h.  Every call only enqueues work on `stream` of the current device.  Workspaces are
  * DEVICE buffers, 16-byte aligned, owned by the caller; they need no initialisation.  A workspace keeps, until its next

@@ -46,7 +46,7 @@ struct SeqArgs {
     int adv_per_token, by_seq;                  // by_seq: the loss needs sums per sequence
     float lo, hi, kl_coef;
     float2 *first, *last;                       // [n_tiles] pieces: (sum, count)
-    float2* seq_sum;                            // [n_seqs] (sum, count)
+    float2* seq_sum;                            // [n_seqs] (sum, count); from preference_finish on a double
     float* tile_stats;                          // [5][n_stats] count, sum of l, KL, clipped, r of a block's (or warp's) tiles
     long n_stats;
     float* weight;                              // [n_seqs + 1] weight of a sequence's tokens; the last: of every token
@@ -309,6 +309,11 @@ __device__ __forceinline__ void policy_finish(const SeqArgs& a) {
     }
 }
 
+// A sequence's joined sum in the place of its (sum, count): D is a small difference of sums that may be large, so it is formed from
+// what the join has, in double.
+__device__ __forceinline__ float2 as_float2(double v) { return make_float2(__int_as_float(__double2loint(v)), __int_as_float(__double2hiint(v))); }
+__device__ __forceinline__ double as_double(float2 v) { return __hiloint2double(__float_as_int(v.y), __float_as_int(v.x)); }
+
 __device__ __forceinline__ void preference_finish(const SeqArgs& a) {
     __shared__ double part[32][3];
     const long pairs = a.n_seqs / 2;
@@ -318,34 +323,35 @@ __device__ __forceinline__ void preference_finish(const SeqArgs& a) {
         const double2 w = join_pieces(a, s, threadIdx.x % width, width);
         if (threadIdx.x % width == 0 && s < a.n_seqs) {
             const double n = a.average ? (w.y > 0 ? w.y : 1.0) : 1.0;
-            a.seq_sum[s] = make_float2(static_cast<float>(w.x / n), static_cast<float>(n));
+            a.seq_sum[s] = as_float2(w.x / n);
+            a.weight[s] = static_cast<float>(n);                            // the divisor, until the slope is known
             if (a.rewards) a.rewards[s] = static_cast<float>(a.beta * (w.x / n));
         }
     }
     __syncthreads();
     double v[3] = {0, 0, 0};
     for (long i = threadIdx.x; i < pairs; i += blockDim.x) {
-        const float2 c = a.seq_sum[i], r = a.seq_sum[pairs + i];
-        const float diff = c.x - r.x;
-        float l, slope;
+        const double diff = as_double(a.seq_sum[i]) - as_double(a.seq_sum[pairs + i]);
+        double l, slope;
         if (a.kind == VPCE_PREF_SIGMOID) {
-            const float z = static_cast<float>(a.beta) * diff - static_cast<float>(a.margin), eps = static_cast<float>(a.smoothing);
+            // z carries D's digits; the curve itself is smooth enough for fp32 (a few u of the loss and of beta)
+            const float z = static_cast<float>(a.beta * diff - a.margin), eps = static_cast<float>(a.smoothing);
             const float tail = log1pf(expf(-fabsf(z)));                     // log(1 + e^-|z|)
             const float neg = (z < 0.f ? -z : 0.f) + tail;                  // -log sigmoid(z)
             const float pos = (z > 0.f ? z : 0.f) + tail;                   // -log sigmoid(-z)
             l = (1.f - eps) * neg + eps * pos;
-            slope = static_cast<float>(a.beta) * (eps - 1.f / (1.f + expf(z)));
+            slope = a.beta * (eps - 1.f / (1.f + expf(z)));
         } else {
-            const float g = diff - static_cast<float>(1.0 / (2.0 * a.beta));
+            const double g = diff - 1.0 / (2.0 * a.beta);
             l = g * g;
-            slope = 2.f * g;
+            slope = 2.0 * g;
         }
         v[0] += l;
-        v[1] += diff > 0.f ? 1.0 : 0.0;
+        v[1] += diff > 0.0 ? 1.0 : 0.0;
         v[2] += a.beta * diff;
-        slope /= static_cast<float>(pairs);
-        a.weight[i] = slope / c.y;
-        a.weight[pairs + i] = -slope / r.y;
+        slope /= static_cast<double>(pairs);
+        a.weight[i] = static_cast<float>(slope / a.weight[i]);
+        a.weight[pairs + i] = static_cast<float>(-slope / a.weight[pairs + i]);
     }
     block_sum<3>(v, part);
     if (threadIdx.x == 0)

@@ -134,3 +134,40 @@ def test_kl_near_the_reference(spread, lens, aggregate):
     assert abs(stats[0] - 0.125 * (w * kl).sum()) <= rel * 0.125 * (w * kl).sum()
     want = -0.125 * w * x
     assert np.all(np.abs(grad - want) <= (10 + np.abs(q)) * U * np.abs(want))
+
+
+# ------------------------------------------------------------------------------------------------ close pairs of large sums
+@pytest.mark.parametrize("n", [4000, 100000])
+def test_difference_of_large_sums(n):
+    """Sequences of n tokens of -1 - 2^-10 and the like, without a reference: sums near -n whose difference is a fraction of
+    their fp32 spacing.  All values are multiples of 2^-10 and a tile's sums (up to 2^13 tokens of size under 2) fit fp32
+    exactly, so D is known exactly and what follows is rounded a few times: stats 4 u, slopes (beta, z, the curve, one rounding
+    of the weight) 10 u."""
+    step = 2.0 ** -10
+    a, b = np.full(n, -1.0 - step), np.full(n, -1.0 - step)
+    a[n // 3] += step                                                    # D = 2^-10 in the first pair
+    c, d = b.copy(), b.copy()
+    c[7] -= 3 * step                                                     # D = -3 * 2^-10 in the second
+    logp = np.concatenate([a, c, b, d]).astype(np.float32)               # preferred ones first
+    off = torch.arange(5, dtype=torch.int64, device="cuda") * n
+    x = torch.from_numpy(logp).cuda()
+    ws = torch.full((vp.vp_preference_loss_workspace_bytes(4 * n, 2),), 255, dtype=torch.uint8, device="cuda")
+    stats, rewards, g = torch.empty(3, device="cuda"), torch.empty(4, device="cuda"), torch.empty(4 * n, device="cuda")
+    D = np.array([step, -3 * step])
+    for kind, beta, margin, average in (("sigmoid", 64.0, 0.5, False), ("ipo", 128.0, 0.0, False), ("ipo", 1024.0, 0.0, True)):
+        vp.vp_preference_loss(x, None, None, off, beta, margin, 0.0, kind, average, stats, rewards, g, ws)
+        diff, count = (D / n, n) if average else (D, 1)
+        if kind == "sigmoid":
+            z = beta * diff - margin
+            loss, slope = np.log1p(np.exp(-z)).mean(), -beta / (1 + np.exp(z))
+        else:
+            loss, slope = ((diff - 0.5 / beta) ** 2).mean(), 2 * (diff - 0.5 / beta)
+        got = stats.cpu().numpy().astype(np.float64)
+        # with `average` the means are rounded to double at their own size, 2^-53 of 1: that is beta 2^-52 / |D| of D, far below u
+        assert abs(got[0] - loss) <= 8 * U * loss and got[1] == 0.5
+        assert abs(got[2] - beta * diff.mean()) <= 4 * U * abs(beta * diff.mean())
+        w = g.view(4, n).cpu().numpy().astype(np.float64)
+        for i in range(2):
+            for row, sign in ((i, 1.0), (2 + i, -1.0)):
+                want = sign * slope[i] / 2 / count
+                assert np.all(np.abs(w[row] - want) <= 10 * U * abs(want)), (kind, i, w[row][0], want)
