@@ -8,11 +8,40 @@ workspace, ``O(T_chunk * block_v)``, whatever V is.
 """
 from __future__ import annotations
 
+import functools
 from typing import Optional
 
 import torch
 
 from . import binding as _b
+
+
+class _Refused(torch.autograd.Function):
+    """The identity, with a derivative that raises."""
+
+    @staticmethod
+    def forward(ctx, grad):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("a second derivative was asked for through a function of this package that has only its first")
+
+
+def first_derivative_only(backward):
+    """For the backward pass of a Function that fills its gradients through raw pointers: under ``create_graph=True`` they
+    would come back without a graph, and what is differentiated through them would silently miss its second-order term.
+    Here they refuse to be differentiated.  (torch's ``once_differentiable`` does so only where the upstream gradient
+    itself requires one, which the gradient of a loss does not.)"""
+    @functools.wraps(backward)
+    def wrapper(ctx, *upstream):
+        with torch.no_grad():
+            grads = backward(ctx, *upstream)
+        if not torch.is_grad_enabled():
+            return grads
+        wrap = lambda g: None if g is None else _Refused.apply(g.detach().requires_grad_())  # noqa: E731
+        return tuple(wrap(g) for g in grads)
+    return wrapper
 
 
 def _pick_chunk(T: int, T_chunk: Optional[int]) -> int:

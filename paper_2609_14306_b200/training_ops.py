@@ -3,7 +3,8 @@ same names as the C entry points, and the torch.autograd front ends ``layer_norm
 ``preference_loss``.
 
 Like the head's binding, the functions check device, dtype, shape and contiguity, pass raw device pointers and the current
-stream, and turn non-zero status codes into ``VpceError``.  There is no CPU or PyTorch fallback.
+stream, and turn non-zero status codes into ``VpceError``.  There is no CPU or PyTorch fallback.  The gradients have no
+derivative of their own: differentiating them again raises.
 """
 from __future__ import annotations
 
@@ -13,6 +14,7 @@ from typing import Optional, Sequence, Tuple
 
 import torch
 
+from .autograd import first_derivative_only
 from .binding import VpceError, load_library, vp_ce_status_string
 
 _F32, _BF16, _F16 = torch.float32, torch.bfloat16, torch.float16
@@ -198,6 +200,7 @@ class _LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @first_derivative_only
     def backward(ctx, dy):
         x, weight, stats = ctx.saved_tensors
         rows, d = x.shape
@@ -301,6 +304,7 @@ class _PolicyLoss(torch.autograd.Function):
         return stats[0].clone(), stats
 
     @staticmethod
+    @first_derivative_only
     def backward(ctx, g, _):
         *inputs, ws = ctx.saved_tensors
         dlogp = torch.empty_like(inputs[0])
@@ -367,6 +371,7 @@ class _PreferenceLoss(torch.autograd.Function):
         return stats[0].clone(), stats, rewards
 
     @staticmethod
+    @first_derivative_only
     def backward(ctx, g, _stats, _rewards):
         mask, seq_offsets, ws = ctx.saved_tensors
         dlogp = torch.empty(ctx.like[0], dtype=_F32, device=ctx.like[1])
