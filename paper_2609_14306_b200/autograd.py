@@ -71,6 +71,7 @@ class _VocabProjCE(torch.autograd.Function):
         return loss
 
     @staticmethod
+    @first_derivative_only
     def backward(ctx, grad_loss):
         H, W, labels, lse = ctx.saved_tensors
         block_v, ignore_index, T_chunk, base = ctx.cfg
@@ -127,6 +128,7 @@ class _MaskedMean(torch.autograd.Function):
         return mean[0]
 
     @staticmethod
+    @first_derivative_only
     def backward(ctx, g):
         labels, n_valid = ctx.saved_tensors
         dloss = torch.empty(labels.numel(), dtype=torch.float32, device=labels.device)

@@ -29,7 +29,20 @@ def preference_loss():
     return vp.preference_loss(x, torch.tensor([0, 25, 60], device="cuda"))[0], (x,)
 
 
-@pytest.mark.parametrize("case", [layer_norm, policy_loss, preference_loss])
+def head(mean=False):
+    H = (0.2 * torch.randn(128, 64, device="cuda")).bfloat16().requires_grad_(True)
+    W = (0.2 * torch.randn(512, 64, device="cuda")).bfloat16().requires_grad_(True)
+    labels = torch.randint(0, 512, (128,), device="cuda")
+    if mean:
+        return vp.vocab_proj_cross_entropy_mean(H, W, labels, block_v=256), (H, W)
+    return vp.vocab_proj_cross_entropy(H, W, labels, block_v=256).sum(), (H, W)
+
+
+def head_mean():
+    return head(mean=True)
+
+
+@pytest.mark.parametrize("case", [layer_norm, policy_loss, preference_loss, head, head_mean])
 def test_second_derivatives_are_refused(case):
     torch.manual_seed(0)
     loss, inputs = case()
