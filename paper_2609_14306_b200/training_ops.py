@@ -194,8 +194,7 @@ class _LayerNorm(torch.autograd.Function):
         stats = torch.empty(2, rows, dtype=_F32, device=x.device)
         vp_ln_forward(x2, weight, bias, eps, y.view(-1, d) if rows else y.reshape(0, d), stats[0], stats[1])
         ctx.save_for_backward(x2, weight, stats)
-        ctx.has_bias = bias is not None
-        ctx.bias_dtype = None if bias is None else bias.dtype
+        ctx.bias_like = None if bias is None else (bias.shape, bias.dtype)
         ctx.shape = x.shape
         return y
 
@@ -210,7 +209,7 @@ class _LayerNorm(torch.autograd.Function):
             dy = dy.contiguous()
         dx = torch.empty(rows, d, dtype=x.dtype, device=x.device) if need_x else None
         dw = torch.empty_like(weight) if need_w and weight is not None else None
-        db = torch.empty(d, dtype=ctx.bias_dtype, device=x.device) if need_b and ctx.has_bias else None
+        db = torch.empty(ctx.bias_like[0], dtype=ctx.bias_like[1], device=x.device) if need_b and ctx.bias_like else None
         ws = None
         if dw is not None or db is not None:
             ws = torch.empty(vp_ln_workspace_bytes(rows, d), dtype=torch.uint8, device=x.device)
