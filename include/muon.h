@@ -53,9 +53,23 @@ int muon_step(float* p, float* m, const void* grad, int g_dtype, void* w_bf16, i
               double lr, double mu, int nesterov, double weight_decay, double scale, const double* coeffs, int steps,
               double eps, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Reads back the status word that the last call wrote to its workspace (synchronises `stream`): 0, or
- * VPCE_DEV_WAIT_EXPIRED (vp_ce.h) when a wait inside the kernels ran out (vp_ce_set_wait_limit_ns). */
+/*
+ * Reads back the status word that the last call wrote to its workspace (synchronises `stream`): 0, or
+ * VPCE_DEV_WAIT_EXPIRED (vp_ce.h) when a wait inside the kernels ran out (vp_ce_set_wait_limit_ns).  The call has then
+ * given up: m is updated, but each element of p, w_bf16 and O holds either its old or its new value.  What was in flight
+ * has ended, the context stays usable and the next call on the workspace starts clean.
+ */
 int muon_device_status(const void* workspace, int32_t* status_out, void* stream);
+
+/*
+ * TEST HOOK: makes a signal of the next launch "get lost", so that the give-up path can be exercised without any invalid
+ * access.  kernel_kind 0, the kernel of large matrices: the operand copies of k-block `index` of the first tile of its
+ * work list are not issued in the CTAs named by `cta_ranks` (bit 0: the leader of a CTA pair, bit 1: the other one).
+ * kernel_kind 1, the one-launch kernel of small matrices: the end of product `index` (three a step) of the first matrix
+ * is not signalled.  One-shot: the launch that consumes it disarms it; kernel_kind < 0 disarms.  VPCE_INVALID_ARG for
+ * values out of range.
+ */
+int muon_debug_drop(int kernel_kind, int index, int cta_ranks);
 
 #ifdef __cplusplus
 }

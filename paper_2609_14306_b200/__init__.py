@@ -48,7 +48,7 @@ _TRAINING_OPS = frozenset((
     "vp_ln_forward", "vp_ln_backward", "vp_ln_workspace_bytes",
     "vp_policy_loss", "vp_policy_loss_backward", "vp_policy_loss_workspace_bytes",
     "vp_preference_loss", "vp_preference_loss_backward", "vp_preference_loss_workspace_bytes",
-    "muon_step", "muon_orthogonalize", "muon_workspace_bytes", "muon_device_status", "muon_rms_scale",
+    "muon_step", "muon_orthogonalize", "muon_workspace_bytes", "muon_device_status", "muon_debug_drop", "muon_rms_scale",
 ))
 
 

@@ -27,6 +27,18 @@ namespace {
 using namespace vpmuon;
 
 constexpr double DEFAULT_COEFFS[3] = {3.4445, -4.7750, 2.0315};
+// muon_debug_drop: kernel kind in bits 0-7, index in bits 8-23, CTA ranks in bits 24-27; -1: nothing armed.
+std::atomic<int> g_drop{-1};
+// Takes what is armed for a launch of this kind.
+void take_drop(GemmParams* q, int kind) {
+    q->drop = -1;
+    int armed = g_drop.load(std::memory_order_relaxed);
+    if (armed >= 0 && (armed & 0xff) == kind && g_drop.compare_exchange_strong(armed, -1)) {
+        q->drop = (armed >> 8) & 0xffff;
+        q->drop_ranks = armed >> 24 & 0xf;
+    }
+}
+
 constexpr double MAX_BOUND = 8.0;               // of |X|_2 along the iteration: its square and the polynomial still fit fp16
 
 int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
@@ -257,7 +269,9 @@ int run(const void* g, int g_dtype, float* m, float mu, int nesterov, int64_t ba
     q.steps = steps;
     std::copy(plan.alpha, plan.alpha + 3 * steps, q.alpha);
     std::copy(plan.beta, plan.beta + 3 * steps, q.beta);
-    if (const int cg = small_cg(L.R, L.C)) {
+    const int cg = small_cg(L.R, L.C);
+    take_drop(&q, cg ? 1 : 0);
+    if (cg) {
         if (batch > 1 && cudaMemsetAsync(q.status, 0, sizeof(int), st) != cudaSuccess) return VPCE_CUDA_ERROR;
         if (cg == 2) q.ldx = static_cast<int>((L.C + 127) / 128 * 128);     // two halves of whole chunks
         const cudaError_t e = g_dtype == VPCE_F32 ? launch_small<float>(q, pp, cg, st)
@@ -328,6 +342,13 @@ int muon_step(float* p, float* m, const void* grad, int g_dtype, void* w_bf16, i
                    static_cast<float>(lr * scale)};
     return run(grad, g_dtype, m, static_cast<float>(mu), nesterov != 0, batch, rows, cols, t, coeffs, steps, eps, workspace,
                workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+
+int muon_debug_drop(int kernel_kind, int index, int cta_ranks) {
+    if (kernel_kind < 0) { g_drop.store(-1, std::memory_order_relaxed); return VPCE_OK; }
+    if (kernel_kind > 1 || index < 0 || index > 0xffff || cta_ranks <= 0 || cta_ranks > 3) return VPCE_INVALID_ARG;
+    g_drop.store(kernel_kind | (index << 8) | (cta_ranks << 24), std::memory_order_relaxed);
+    return VPCE_OK;
 }
 
 int muon_device_status(const void* workspace, int32_t* status_out, void* stream) {

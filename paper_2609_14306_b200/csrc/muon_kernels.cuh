@@ -55,6 +55,7 @@ struct GemmParams {
     int *status, *next;                     // next: work-list position to be taken, zero before the launch
     int* done;                              // [batch][DONE_PITCH] epilogue warps that have finished a tile of this matrix, zero before the launch
     unsigned long long wait_limit_ns;
+    int drop, drop_ranks;                   // test hook (muon_debug_drop): the k-block or product that is lost, -1: none
 };
 
 __device__ __forceinline__ void tma2_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
@@ -553,15 +554,18 @@ muon_products_kernel(const __grid_constant__ Maps maps, const __grid_constant__ 
                 const CUtensorMap* mb = w.mode == GRAM ? &maps.x_r[xb] : w.mode == POLY ? &maps.a_r : &maps.x_mn[xb];
                 const int num_kb = steps_of_k(p, w);
                 const int arow = w.i * TM + static_cast<int>(rank) * 128, bcol = w.j * w.bn + static_cast<int>(rank) * (w.bn / 2);
+                const int lost = t == 0 && (p.drop_ranks >> rank & 1) ? p.drop : -1;   // test hook
                 for (int kb = 0; kb < num_kb; ++kb) {
                     if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, p.wait_limit_ns)) { ok = false; break; }
                     if (leader) mbar_arrive_expect_tx(full_bar(stage), 2 * (A_BYTES + w.bn / 2 * 128));
                     const uint32_t bar = mapa_shared(full_bar(stage), 0);
                     const uint32_t sa = base + stage * STAGE_BYTES;
                     // rows and chunks beyond the matrix arrive as zeros
-                    tma2_load_4d(sa, ma, bar, 0, arow, kb, w.b);
-                    if (w.mode == APPLY) tma2_load_4d(sa + A_BYTES, mb, bar, 0, kb * KB, bcol / 64, w.b);
-                    else tma2_load_4d(sa + A_BYTES, mb, bar, 0, bcol, kb, w.b);
+                    if (kb != lost) {
+                        tma2_load_4d(sa, ma, bar, 0, arow, kb, w.b);
+                        if (w.mode == APPLY) tma2_load_4d(sa + A_BYTES, mb, bar, 0, kb * KB, bcol / 64, w.b);
+                        else tma2_load_4d(sa + A_BYTES, mb, bar, 0, bcol, kb, w.b);
+                    }
                     ++issued;
                     if (++stage == STAGES) { stage = 0; phase ^= 1u; }
                 }
@@ -763,20 +767,22 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) muon_small_kernel(const __gr
     using S = SmallShape<CG>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ double part[SMALL_WARPS];
-    __shared__ uint64_t bar_slot;
+    __shared__ uint64_t bar_slot, drain_slot;
     __shared__ uint32_t tmem_slot;
-    __shared__ int abort_word;
+    __shared__ int abort_word, gave_up_word;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     const uint32_t bar = smem_u32(&bar_slot);
     volatile int* abort_flag = &abort_word;
+    volatile int* gave_up = &gave_up_word;                                  // 1 + the product that a warp of either CTA gave up, 0: none
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CG == 2 ? static_cast<int>(cluster_ctarank()) : 0;
     const int b = blockIdx.x / CG;
     const int chunks = p.ldx / 64;                                          // CG = 2: an even number (ldx a multiple of 128)
 
     if (threadIdx.x == 0) {
-        abort_word = 0;
+        abort_word = gave_up_word = 0;
         mbar_init(bar, 1);
+        mbar_init(smem_u32(&drain_slot), 1);
         fence_barrier_init();
         if (gridDim.x == CG && rank == 0) *p.status = 0;                    // of several matrices the host clears it
     }
@@ -903,6 +909,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) muon_small_kernel(const __gr
     const int quad = warp & 3, first = warp >> 2, row = quad * 32 + lane;
     const uint32_t tmem_row = tmem + (static_cast<uint32_t>(quad * 32) << 16);
     uint32_t parity = 0;
+    bool got = true;                                                        // the product before has come to its end (alike in a warp)
     for (int k = 0; k < 3 * p.steps; ++k) {
         const int mode = k % 3;
         // what was written to either CTA's shared memory is read by the tensor cores next
@@ -928,12 +935,25 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) muon_small_kernel(const __gr
                     else umma_f16(tmem + 256 * n, ad, bd, idesc, q != 0 ? 1u : 0u);
                 }
             }
-            if (CG == 2) umma2_commit_both(bar);
+            if (k == p.drop && b == 0) {}                                   // test hook: the signal is lost
+            else if (CG == 2) umma2_commit_both(bar);
             else umma_commit(bar);
         }
-        mbar_wait(bar, parity, abort_flag, p.wait_limit_ns);                // on expiry: the status word is set below, nobody leaves early
+        // All threads of the CTA or pair leave here or none: only waits for product k write k + 1, and all waits for the products
+        // before it lie before the barrier.  (Behind the product's start, where it costs nothing; of a product that should not have
+        // been started nothing is used.)
+        if (const int lost = *gave_up; lost != 0 && lost <= k) { got = false; break; }
+        got = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.wait_limit_ns));
         parity ^= 1u;
         tc_fence_after();
+        if (!got) {                                                         // nothing that the product may still read is written
+            if (lane < CG) {
+                if (CG == 2) asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(mapa_shared(smem_u32(&gave_up_word), lane)), "r"(k + 1) : "memory");
+                else *gave_up = k + 1;
+            }
+            __syncwarp();
+            continue;
+        }
         if (k + 1 == 3 * p.steps) break;
         const float alpha = p.alpha[k], beta = p.beta[k];
         const int blocks = (mode == APPLY ? p.ldx : S::ROWS) / 32;
@@ -956,8 +976,15 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) muon_small_kernel(const __gr
         }
     }
     // ---- the last X, to the caller's arrays, 16 columns at a time
+    if (!got && threadIdx.x == 0 && rank == 0) {                            // give-up path: the products in flight end first
+        if (CG == 2) umma2_commit_local(smem_u32(&drain_slot));
+        else umma_commit(smem_u32(&drain_slot));
+        const unsigned long long t0 = globaltimer_ns();
+        while (!mbar_try_wait(smem_u32(&drain_slot), 0) && globaltimer_ns() - t0 < p.wait_limit_ns) {}
+    }
+    __syncwarp();
 #pragma unroll 1
-    for (int n = first; n < p.ldx / 16; n += SMALL_WARPS / 4) {
+    for (int n = first; got && n < p.ldx / 16; n += SMALL_WARPS / 4) {
         if (16 * n >= p.C || quad * 32 >= rows_here) break;                 // uniform in the warp
         auto from_x = [&](int q, float* f) {
             const int c = 16 * n + 8 * q;

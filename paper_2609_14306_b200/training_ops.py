@@ -44,6 +44,7 @@ def _lib() -> ctypes.CDLL:
             "muon_orthogonalize": (i32, [vp, i32, vp, i32, i64, i64, i64, vp, i32, f64, vp, sz, vp]),
             "muon_step": (i32, [vp, vp, vp, i32, vp, i64, i64, i64, f64, f64, i32, f64, f64, vp, i32, f64, vp, sz, vp]),
             "muon_device_status": (i32, [vp, ctypes.POINTER(ctypes.c_int32), vp]),
+            "muon_debug_drop": (i32, [i32, i32, i32]),
         }
         for name, (res, args) in signatures.items():
             fn = getattr(lib, name)
@@ -461,3 +462,10 @@ def muon_device_status(workspace, stream=None) -> int:
     out = ctypes.c_int32(-1)
     _call(_lib().muon_device_status, dev, _workspace(workspace, dev)[0], ctypes.byref(out), _stream(stream, dev))
     return int(out.value)
+
+
+def muon_debug_drop(kernel_kind: int, index: int = 0, cta_ranks: int = 1) -> None:
+    """Test hook: a signal of the next Muon launch of that kind gets lost (see include/muon.h); kernel_kind < 0 disarms."""
+    code = _lib().muon_debug_drop(kernel_kind, index, cta_ranks)
+    if code:
+        _fail(code)
