@@ -38,6 +38,10 @@ extern "C" {
  *   dlogp               fp32 [T], written with upstream * dloss/dlogp (every element), or NULL: forward only
  *   upstream            DEVICE fp32 scalar or NULL (= 1)
  * T == 0 or n_seqs == 0: stats (and dlogp) are 0.
+ *
+ * A batch in parts (over ranks, or accumulated): the mean is over the tokens (or sequences) of one call.  With n valid
+ * tokens here and N in all parts, upstream = n / N gives this part's gradient of the mean over all of them, and the sum of
+ * the parts' loss n / N is that mean; with VPCE_SEQ_MEAN, n and N count sequences that have a valid token.
  */
 enum { VPCE_TOKEN_MEAN = 0, VPCE_SEQ_MEAN = 1 };
 size_t vp_policy_loss_workspace_bytes(int64_t T, int64_t n_seqs);

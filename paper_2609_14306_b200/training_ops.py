@@ -319,7 +319,10 @@ def policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Te
     """(loss, stats) of the clipped policy objective over packed sequences; loss is a scalar, differentiable in logp.
 
     With the head of this package, ``logp = -vocab_proj_cross_entropy(H, W, labels)``.  Tokens whose mask is false (prompts,
-    padding) may hold anything and get no gradient.  stats [4]: loss, mean KL estimate, clipped share, mean ratio."""
+    padding) may hold anything and get no gradient.  stats [4]: loss, mean KL estimate, clipped share, mean ratio.
+
+    The mean is over this call's tokens (or sequences).  Of a batch in parts, over ranks or accumulated, back-propagate
+    ``loss * (n / N)`` of each part: n valid tokens here (``mask.sum()``), N in all parts."""
     cfg = (float(clip_low), float(clip_high), float(kl_coef), aggregate, adv_per_token)
     return _PolicyLoss.apply(logp, old_logp, ref_logp, advantages, mask, seq_offsets, cfg)
 

@@ -171,3 +171,39 @@ def test_difference_of_large_sums(n):
             for row, sign in ((i, 1.0), (2 + i, -1.0)):
                 want = sign * slope[i] / 2 / count
                 assert np.all(np.abs(w[row] - want) <= 10 * U * abs(want)), (kind, i, w[row][0], want)
+
+
+# ------------------------------------------------------------------------------------------------ a batch in parts
+@pytest.mark.parametrize("aggregate", ["token_mean", "seq_mean"])
+def test_parts_of_a_batch_add_up_to_the_whole(aggregate):
+    """Each part's loss times its share of the valid tokens (sequences), back-propagated, is the whole batch's gradient.  Both
+    sides round their weight and two products, 4 u each, and the share 2 u: 10 u element by element."""
+    rng = np.random.default_rng(4)
+    lens = [300, 0, 41, 500, 7, 260]
+    off = np.concatenate([[0], np.cumsum(lens)])
+    T = int(off[-1])
+    logp = torch.from_numpy(-np.abs(rng.standard_normal(T)).astype(np.float32)).cuda()
+    old, mask = logp + 0.1 * torch.randn(T, device="cuda"), torch.from_numpy(rng.random(T) < 0.7).cuda()
+    adv, ref = torch.randn(len(lens), device="cuda"), logp - 0.05
+
+    def share(lo, hi):
+        if aggregate == "token_mean":
+            return mask[off[lo]:off[hi]].sum().float()
+        return torch.tensor(float(sum(bool(mask[off[s]:off[s + 1]].any()) for s in range(lo, hi))), device="cuda")
+
+    def loss(x, lo, hi):
+        t = slice(int(off[lo]), int(off[hi]))
+        o = torch.from_numpy(off[lo:hi + 1] - off[lo]).cuda()
+        return vp.policy_loss(x[t], old[t], adv[lo:hi], o, mask=mask[t], ref_logp=ref[t], kl_coef=0.1, aggregate=aggregate)[0]
+
+    whole, parts = (logp.clone().requires_grad_(True) for _ in range(2))
+    full = loss(whole, 0, 6)
+    full.backward()
+    N, total = share(0, 6), 0.0
+    for lo, hi in ((0, 3), (3, 6)):
+        part = loss(parts, lo, hi) * (share(lo, hi) / N)
+        part.backward()
+        total += float(part.detach())
+    assert torch.all((parts.grad - whole.grad).abs() <= 10 * U * whole.grad.abs())
+    # sums: (T / 1024 + 40) u of the mean term, 8 u around them, on both sides; a term is at most 2 |A| (ratios below 2)
+    assert abs(total - float(full.detach())) <= 2 * (T / 1024 + 48) * U * 2 * float(adv.abs().max())
