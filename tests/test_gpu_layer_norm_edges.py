@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2609_14306_b200 as vp
+import test_gpu_layer_norm as ln
 
 pytestmark = pytest.mark.gpu
 
@@ -20,3 +21,13 @@ def test_gradients_have_their_parameters_shapes(shape):
     (vp.layer_norm(x.detach(), flat_w, flat_b) * up).sum().backward()
     assert w.grad.shape == shape and b.grad.shape == shape
     assert torch.equal(w.grad.reshape(48), flat_w.grad) and torch.equal(b.grad.reshape(48), flat_b.grad)
+
+
+# fp32 rows leave the row kernels where two rows and the weights no longer fit shared memory: above 14336 columns forward and 11320
+# backward; 16-bit rows above 16384 columns; aligned rows of up to 512 bytes have kernels of their own.
+@pytest.mark.parametrize("dtype,d", [(torch.float32, d) for d in (11316, 11319, 11320, 11321, 11324, 14332, 14336, 14337, 14340, 16384, 16385)]
+                         + [(torch.bfloat16, d) for d in (16376, 16383, 16384, 16385, 16392)]
+                         + [(torch.float16, d) for d in (255, 256, 257, 264)] + [(torch.float32, d) for d in (127, 128, 129, 132)])
+@pytest.mark.parametrize("rows", [1, 5, 300])
+def test_both_sides_of_the_switches_between_the_kernels(rows, d, dtype):
+    ln.check(*ln.make(rows, d, dtype, torch.float32, seed=d + rows))

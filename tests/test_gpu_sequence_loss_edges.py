@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2609_14306_b200 as vp
+import test_gpu_sequence_loss as seq
 
 pytestmark = pytest.mark.gpu
 
@@ -207,3 +208,66 @@ def test_parts_of_a_batch_add_up_to_the_whole(aggregate):
     assert torch.all((parts.grad - whole.grad).abs() <= 10 * U * whole.grad.abs())
     # sums: (T / 1024 + 40) u of the mean term, 8 u around them, on both sides; a term is at most 2 |A| (ratios below 2)
     assert abs(total - float(full.detach())) <= 2 * (T / 1024 + 48) * U * 2 * float(adv.abs().max())
+
+
+# ------------------------------------------------------------------------------------------------ where the paths meet
+SWITCH = [[8192], [8193], [8191, 1], [8000, 193], [1] * 1023 + [0], [1] * 1025, [8] * 1024, [8] * 1024 + [0], [8] * 1023 + [0, 9]]
+
+
+@pytest.mark.parametrize("i", range(len(SWITCH)))
+def test_both_sides_of_the_switch_between_the_paths(i):
+    """One launch serves up to 8192 tokens in up to 1024 sequences; both sides of either limit, against the oracle."""
+    off, T, logp, old, ref, mask, adv, adv_seq = seq.make(SWITCH[i], seed=40 + i)
+    for aggregate in ("token_mean", "seq_mean"):
+        seq.check_policy(off, T, logp, old, ref, mask, adv, 0.05, aggregate, True)
+        seq.check_policy(off, T, logp, old, None, None, adv_seq, 0.0, aggregate, False, upstream=0.5)
+    if len(SWITCH[i]) % 2 == 0:
+        seq.check_preference(off, T, logp, ref, mask, 0.1, 0.2, 0.05, "sigmoid", False)
+        seq.check_preference(off, T, logp, ref, mask, 0.1, 0.0, 0.0, "ipo", True)
+
+
+@pytest.mark.parametrize("n_seqs", [1024, 1025])
+def test_same_tokens_on_both_paths(n_seqs):
+    """An empty sequence at the end is the difference between the paths and none to the result: they agree to the oracle's bounds
+    twice over (token by token 2 (8 + |q| ...) u, here 64 u)."""
+    lens = [7] * 1024
+    off, T, logp, old, ref, mask, adv, _ = seq.make(lens, seed=3)
+    base = seq.policy(off, T, logp, old, ref, mask, adv, 0.1, "token_mean", True)
+    more = seq.policy(np.concatenate([off] + [[T]] * (n_seqs - 1024)), T, logp, old, ref, mask, adv, 0.1, "token_mean", True)
+    assert np.all(np.abs(base[0] - more[0]) <= 128 * U * np.maximum(np.abs(base[0]), 1.0))
+    assert np.all(np.abs(base[1] - more[1]) <= 64 * U * np.abs(base[1]))
+
+
+# ------------------------------------------------------------------------------------------------ two streams
+def test_early_started_launches_on_two_streams():
+    """The later launches of a large call start before the one in front of them has ended.  Calls of both losses in flight on two
+    streams, back to back on each, give what they give alone."""
+    rng = np.random.default_rng(6)
+    off = torch.tensor([0, 20000, 20001, 45000, 70000], device="cuda")
+    T = 70000
+    logp = torch.from_numpy(-np.abs(rng.standard_normal(T)).astype(np.float32)).cuda()
+    old, ref, adv = logp + 0.1 * torch.randn(T, device="cuda"), logp - 0.05, torch.randn(T, device="cuda")
+    mask = torch.from_numpy(rng.random(T) < 0.7).cuda()
+
+    def policy_call(out, stream=None):
+        vp.vp_policy_loss(logp, old, ref, adv, mask, off, 0.2, 0.2, 0.1, "seq_mean", *out, adv_per_token=True, stream=stream)
+
+    def preference_call(out, stream=None):
+        vp.vp_preference_loss(logp, ref, mask, off, 0.1, 0.0, 0.0, "ipo", True, out[0], None, *out[1:], stream=stream)
+
+    def buffers(stats):
+        ws = max(vp.vp_policy_loss_workspace_bytes(T, 4), vp.vp_preference_loss_workspace_bytes(T, 2))
+        return torch.zeros(stats, device="cuda"), torch.zeros(T, device="cuda"), torch.zeros(ws, dtype=torch.uint8, device="cuda")
+
+    want = buffers(4), buffers(3)
+    policy_call(want[0]), preference_call(want[1])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [(buffers(4), buffers(3)) for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, (a, b) in zip(streams, got):
+            policy_call(a, s), preference_call(b, s)
+    torch.cuda.synchronize()
+    for pair in got:
+        for g, w in zip(pair, want):
+            assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])
