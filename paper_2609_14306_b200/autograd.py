@@ -35,10 +35,10 @@ def first_derivative_only(backward):
     itself requires one, which the gradient of a loss does not.)"""
     @functools.wraps(backward)
     def wrapper(ctx, *upstream):
+        if not torch.is_grad_enabled():
+            return backward(ctx, *upstream)
         with torch.no_grad():
             grads = backward(ctx, *upstream)
-        if not torch.is_grad_enabled():
-            return grads
         wrap = lambda g: None if g is None else _Refused.apply(g.detach().requires_grad_())  # noqa: E731
         return tuple(wrap(g) for g in grads)
     return wrapper
