@@ -164,6 +164,7 @@ __device__ __forceinline__ void fetch_row(const RowArgs& a, int r, uint8_t* slot
         total += bytes[i];
     }
     const uint32_t dst = vpce::smem_u32(slot);
+    if (!VEC) vpce::fence_proxy_async();                    // plain stores to a slot come before a later row's bulk copy to it
     if (NA == 2) {
         asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + 2 * a.cap), "l"(a.mean + r) : "memory");
         asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + 2 * a.cap + 4), "l"(a.rstd + r) : "memory");
