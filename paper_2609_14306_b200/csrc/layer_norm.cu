@@ -1,21 +1,26 @@
 // Layer normalisation, forward and backward (layer_norm.h).
 //
-// Row kernels (d <= 16384): a group of 1 to 16 warps owns a row at a time, 8 to 32 elements a thread.  Rows arrive by bulk
+// Row kernels (16-bit rows of up to 16384 columns, fp32 ones of up to 14336 forward and 11320 backward: two rows in flight and the
+// weights as fp32 have to fit shared memory): a group of 1 to 16 warps owns a row at a time, 8 to 32 elements a thread.  Rows arrive by bulk
 // copies into a ring in shared memory, several rows ahead: what is in flight does not depend on registers or on how many warps
 // wait at a reduction.  A thread owns the same columns in every row: in the backward pass it sums dy xh and dy of its columns
 // in registers over all rows of its group, so the weight's gradient costs no second pass over the data, only one partial sum
 // per block.  The variance is taken from the centred values in registers.  Bound: memory, two passes over the rows forward,
 // three backward; at 16-bit types the arithmetic is nearly as scarce, so it runs on pairs (fp32x2 instructions).  Measured on
-// 65536 x 7168 bf16, fp32 weights: 299 us forward, 426 us backward (6.3 and 6.6 TB/s, the rate of a plain copy), 796 us for
-// both in sustained repetition, where the lowered clock shows the arithmetic; 16384 x 2880: 102 us for both.  Registers without
-// a spill matter most: 24 to 60 bytes of spill in the row loop cost 10 to 25 %.
+// 65536 x 7168 bf16, fp32 weights: 299 us forward, 426 us backward (6.3 and 6.6 TB/s, the rate of a plain copy), 845 us for
+// both in sustained repetition (796 on another board), where the lowered clock shows the arithmetic; 16384 x 2880: 102 us for both.
+// Spills matter: 24 to 60 bytes in the row loop cost 10 to 25 %.  The aligned row kernels have none; the unaligned backward ones of
+// 24 and 32 elements a thread have 4 and 20 bytes.
 //   VEC      every row starts on a 16-byte boundary: 16-byte accesses
 //   !VEC     any alignment: the copies take the 16-byte granules that a row touches (cut at the tensor's ends, whose few
 //            elements are copied one by one), threads read single elements at the row's offset, neighbours side by side:
-//            2.8 to 3.8 TB/s forward and 2.6 to 3.6 backward in 16 bits, where VEC has 4.8 to 5.3 and 4.4 to 5.1 (2^26 elements)
+//            2.8 to 4.3 TB/s forward and 2.7 to 3.6 backward in 16 bits, where VEC has 4.7 to 5.7 and 3.4 to 5.3 (2^26 elements,
+//            512 to 16384 columns: 0.58 to 0.79 of its rate); 5.3 and 4.8 in fp32, where VEC has 5.4 and 5.9
 //
 // Generic kernels (wider rows): one block per row, elements read one at a time in the order of the threads, three passes over
-// a row that the caches hold after the first.
+// a row that the caches hold after the first, and a pass of their own for the column sums.  Slow: 2^26 elements take 187 and 567 us
+// at 16384 columns of fp32 (floor 82 and 123), 555 backward at 12288 (row kernel forward: 97), 175 and 542 at 20000 of bf16 (floor
+// 41 and 62).
 //
 // Narrow kernels (aligned rows of up to 512 bytes): several rows to a warp, see there.
 
@@ -116,7 +121,7 @@ struct RowArgs {
 // The same, longer.  With more than 112 bytes of arguments the compiler keeps them in registers instead of reading them where they
 // are used.  That serves the forward kernels (2^26 bf16 elements: 54 us instead of 58 at 10000 columns, 52 instead of 56 at 64)
 // and the backward pass on unaligned rows (120 instead of 170 at 2881); on aligned rows that spills and
-// takes 91 instead of 78.
+// takes 91 instead of 78.  So with nvcc 12.9; a compiler that decides otherwise costs that much speed and nothing else.
 struct LongRowArgs : RowArgs { int64_t none; };
 template <typename Args> Args args_of(const RowArgs& a) {
     Args r{};
@@ -176,7 +181,9 @@ __device__ __forceinline__ void fetch_row(const RowArgs& a, int r, uint8_t* slot
         if (bytes[i]) bulk_load(dst + i * a.cap + at[i], from[i], bytes[i], bar);
 }
 
-// All waits are for bulk copies of this block's own and end; the limit is that of a copy that never lands (a bad pointer).
+// All waits are for bulk copies of this block's own from arrays that the caller vouches for, so they end.  The limit only keeps a copy
+// that never lands from hanging the GPU; what is computed then is undefined and not reported: a flag in the row loop, in any of the
+// forms tried, costs the widest backward kernel 24 to 150 bytes of spill.
 __device__ __forceinline__ void wait_row(uint32_t bar, uint32_t parity) {
     for (int i = 0; i < (1 << 26); ++i)
         if (vpce::mbar_try_wait(bar, parity)) return;

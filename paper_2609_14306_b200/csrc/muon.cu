@@ -174,8 +174,8 @@ int64_t tiles_of(int mode, int64_t R, int64_t C, int bn) {
     return mode == APPLY ? mt * nj : mt * nj - (TM / bn) * (mt * (mt - 1) / 2);
 }
 
-// Tile width of a product.  The tensor cores take as long for a 256 x 64 or 256 x 128 step as for 256 x 256 (the left operand's
-// 128 rows per SM bound it: 494 against 530 cycles per 64 of K), so narrow tiles only pay when they find idle SMs: they then
+// Tile width of a product.  A 256 x 128 step was measured at 494 cycles per 64 of K, a 256 x 256 step at 530.  (What holds the narrow
+// one back was not isolated: its products alone are 256 cycles.)  So narrow tiles only pay when they find idle SMs: they then
 // cut the tile's epilogue.  Hence the narrowest width whose tiles all run at once, else 256.  A step against one with 256
 // throughout: 512 x 512 126 and 172 us, 1024 x 1024 164 and 211, 501 x 1999 162 and 209, 1024 x 4096 255 and 289.
 // APPLY's right operand comes in chunks of 64 columns per CTA, so 128 is its least.
