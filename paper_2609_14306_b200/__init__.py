@@ -51,6 +51,12 @@ _TRAINING_OPS = frozenset((
     "muon_step", "muon_orthogonalize", "muon_workspace_bytes", "muon_device_status", "muon_debug_drop", "muon_rms_scale",
 ))
 
+# the operators from the residual stream to log probabilities (RMS norm); their binding needs torch
+_HEAD_OPS = frozenset((
+    "rms_norm", "rms_norm_fp8", "fp8_blocks",
+    "vp_rms_forward", "vp_rms_forward_fp8", "vp_rms_backward", "vp_rms_workspace_bytes",
+))
+
 
 def __getattr__(name):
     # the autograd front end needs torch; import it lazily so the C-ABI binding works without it
@@ -63,6 +69,10 @@ def __getattr__(name):
     if name in _TRAINING_OPS:
         from . import training_ops as _ops
         value = globals()[name] = getattr(_ops, name)
+        return value
+    if name in _HEAD_OPS:
+        from . import head_ops as _head
+        value = globals()[name] = getattr(_head, name)
         return value
     if name in ("RingDTP", "DistTransport", "CudaMeetings", "choose_schedule", "shard_interval"):
         from . import ring as _ring
