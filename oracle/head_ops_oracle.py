@@ -37,3 +37,43 @@ def group_scales(y):
 def spread_columns(scales, d):
     """A row's scales as one for each of its d columns."""
     return torch.repeat_interleave(scales.to(F64), BLOCK, dim=1)[:, :d]
+
+
+def block_scales(w):
+    """Scale of each 128 x 128 block of w: max|w| / 448, 1 where that is 0."""
+    m = torch.stack([torch.stack([p.abs().max() for p in torch.split(r, BLOCK, dim=1)]) for r in torch.split(w.to(F64), BLOCK, dim=0)])
+    return torch.where(m > 0, m / 448, torch.ones_like(m))
+
+
+def spread_blocks(scales, rows, d):
+    """Blocks' scales as one for each element of a [rows, d] weight."""
+    return torch.repeat_interleave(spread_columns(scales, d), BLOCK, dim=0)[:rows]
+
+
+def token_logp(h, w, tokens, temperature, ignore_index=-100):
+    """dict of logits (before the temperature), lse, entropy and logp of given tokens (0 where ignored or outside the vocabulary)."""
+    x = h.to(F64) @ w.to(F64).mT
+    logq = torch.log_softmax(x / temperature, dim=1)
+    p = torch.exp(logq)
+    out = {"x": x, "lse": torch.logsumexp(x / temperature, dim=1), "entropy": -(p * logq).sum(1), "logq": logq}
+    if tokens is not None:
+        t = tokens.long()
+        valid = (t != ignore_index) & (t >= 0) & (t < w.shape[0])
+        out["valid"] = valid
+        out["logp"] = torch.where(valid, logq.gather(1, t.clamp(0, w.shape[0] - 1)[:, None])[:, 0], torch.zeros((), dtype=F64, device=h.device))
+    return out
+
+
+def token_logp_grad(h, w, tokens, dlogp, dent, temperature, ignore_index=-100):
+    """(dH, dW, G): gradients for upstream gradients dlogp and dent (either may be None), and that of the logits."""
+    o = token_logp(h, w, tokens, temperature, ignore_index)
+    p = torch.exp(o["logq"])
+    g = torch.zeros_like(p)
+    if dlogp is not None:
+        u = torch.where(o["valid"], dlogp.to(F64), torch.zeros((), dtype=F64, device=h.device))
+        g -= p * u[:, None]
+        g.scatter_add_(1, tokens.long().clamp(0, w.shape[0] - 1)[:, None], u[:, None])
+    if dent is not None:
+        g -= dent.to(F64)[:, None] * p * (o["logq"] + o["entropy"][:, None])
+    g /= temperature
+    return g @ w.to(F64), g.mT @ h.to(F64), g

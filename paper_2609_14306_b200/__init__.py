@@ -51,10 +51,12 @@ _TRAINING_OPS = frozenset((
     "muon_step", "muon_orthogonalize", "muon_workspace_bytes", "muon_device_status", "muon_debug_drop", "muon_rms_scale",
 ))
 
-# the operators from the residual stream to log probabilities (RMS norm); their binding needs torch
+# the operators from the residual stream to log probabilities; their binding needs torch
 _HEAD_OPS = frozenset((
-    "rms_norm", "rms_norm_fp8", "fp8_blocks",
+    "rms_norm", "rms_norm_fp8", "fp8_blocks", "quantize_blocks_fp8", "token_log_probs", "token_log_probs_fp8", "TokenLogProbs",
     "vp_rms_forward", "vp_rms_forward_fp8", "vp_rms_backward", "vp_rms_workspace_bytes",
+    "vp_token_logp_forward", "vp_token_logp_backward", "vp_token_logp_workspace_bytes", "vp_token_logp_debug_drop",
+    "vp_token_logp_fp8_forward", "vp_token_logp_fp8_workspace_bytes", "vp_fp8_quantize_blocks",
 ))
 
 

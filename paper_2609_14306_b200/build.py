@@ -10,12 +10,15 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 REPO_DIR = os.path.dirname(PKG_DIR)
 SOURCES = [os.path.join(PKG_DIR, "csrc", "vp_ce.cu"), os.path.join(PKG_DIR, "csrc", "stream_adamw.cu"),
            os.path.join(PKG_DIR, "csrc", "layer_norm.cu"), os.path.join(PKG_DIR, "csrc", "sequence_loss.cu"),
-           os.path.join(PKG_DIR, "csrc", "muon.cu"), os.path.join(PKG_DIR, "csrc", "rms_norm.cu")]
+           os.path.join(PKG_DIR, "csrc", "muon.cu"), os.path.join(PKG_DIR, "csrc", "rms_norm.cu"),
+           os.path.join(PKG_DIR, "csrc", "token_logp.cu"), os.path.join(PKG_DIR, "csrc", "fp8_blocks.cu")]
 HEADERS = [os.path.join(REPO_DIR, "include", "vp_ce.h"), os.path.join(REPO_DIR, "include", "stream_adamw.h"),
            os.path.join(PKG_DIR, "csrc", "sm100_ptx.cuh"), os.path.join(PKG_DIR, "csrc", "vp_ce_kernels.cuh"),
            os.path.join(REPO_DIR, "include", "vp_ce_types.h"), os.path.join(REPO_DIR, "include", "layer_norm.h"),
            os.path.join(REPO_DIR, "include", "sequence_loss.h"), os.path.join(REPO_DIR, "include", "muon.h"),
            os.path.join(REPO_DIR, "include", "rms_norm.h"), os.path.join(PKG_DIR, "csrc", "row_kernels.cuh"),
+           os.path.join(REPO_DIR, "include", "token_logp.h"), os.path.join(REPO_DIR, "include", "fp8_blocks.h"),
+           os.path.join(PKG_DIR, "csrc", "token_logp_kernels.cuh"),
            os.path.join(PKG_DIR, "csrc", "muon_kernels.cuh"), os.path.join(PKG_DIR, "csrc", "vp_ce_f32.inc"), os.path.join(PKG_DIR, "csrc", "vp_ce_fixup.cuh")]
 LIB_PATH = os.path.join(PKG_DIR, "libvpce.so")
 

@@ -1,0 +1,834 @@
+// Device code of the token log probabilities (token_logp.h): the strip kernel (a CTA pair per 256 x 256 tile of logits), the kernel
+// for few tokens (one pass over the weight) and the kernel that joins what either leaves per token.
+//
+// Per token and slice of the vocabulary the first two leave (m, z, u, n): with t = (x - m) / temperature * log2(e) for logit x,
+//     m = max x,   z = sum 2^t,   u = sum t 2^t,   n = how many candidates for the alternatives lie beside it
+// two of which join like two online softmax states: m = max(m1, m2), and with t' = (m1 - m) / temperature * log2(e)
+//     z1 -> z1 2^t',   u1 -> 2^t' (u1 + t' z1)
+// Then lse = m / temperature + ln z and the entropy is ln z - ln 2 u / z: no difference of large numbers anywhere.
+#pragma once
+
+#include <climits>
+
+#include "sm100_ptx.cuh"
+#include "vp_ce.h"
+
+namespace vptl {
+
+using namespace vpce;
+
+constexpr int MAX_TOP = 20;                                 // alternatives per token
+constexpr float LOG2E_F = 1.4426950408889634f, LN2_F = 0.6931471805599453f;
+constexpr float MINUS_INF = -__builtin_huge_valf();
+
+constexpr int KB_BYTES = 128;                               // a k-block: 128 bytes of every row (64 bf16 or 128 e4m3)
+constexpr int TILE_M = 128, TILE_N = 256, HALF_N = 128;     // rows per CTA, columns per pair tile, columns per epilogue thread
+constexpr int EPI_WARPS = 8, EPI_THREADS = 32 * EPI_WARPS, THREADS = 64 + EPI_THREADS;
+
+struct Params {
+    int rows, cols;                         // tokens of this launch, vocabulary columns of this launch
+    int row0, col0;                         // first token (coordinates of H's map), first column (coordinates of W's map)
+    int kbs;                                // k-blocks
+    int m_tiles, n_tiles;                   // strip kernel: 256-token and 256-column tiles
+    int slices;                             // slices per token in `part` and `cand`
+    int V;
+    float scale;                            // log2(e) / temperature
+    const int32_t* tokens;                  // of this launch's first token; null: none
+    float4* part;                           // [rows][slices]: m, z, u, number of candidates
+    uint2* cand;                            // [rows][slices][top]: logit, column
+    int top;
+    unsigned* floor;                        // [rows]: a lower bound on the token's top-th largest logit (ordered bits; 0: none)
+    float* chosen;                          // [rows]: logit of the given token
+    const float *hs, *ws;                   // 8 bits: scales of H's rows [.][kbs], of W's blocks [.][kbs]
+    int* status;
+    unsigned long long wait_limit_ns;
+    int drop_kb;                            // test hook: the copies of this k-block of the first tile get lost; < 0: off
+};
+
+// Floats as unsigned numbers of the same order; 0 stands below all of them.
+__device__ __forceinline__ unsigned ordered(float v) {
+    const unsigned b = __float_as_uint(v);
+    return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float from_ordered(unsigned o) {
+    return o == 0u ? MINUS_INF : __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu));
+}
+// The number just below v: "> below(v)" accepts v itself.
+__device__ __forceinline__ float below(float v) {
+    const unsigned o = ordered(v);
+    return v == MINUS_INF || o == 0u ? MINUS_INF : from_ordered(o - 1u);
+}
+
+using f2 = unsigned long long;
+__device__ __forceinline__ f2 pair(float a, float b) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float2 split(f2 v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+
+// kind::f8f6f4 (K = 32): e4m3 x e4m3 -> fp32.
+__device__ __forceinline__ void umma_f8(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma2_f8(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// 32 lanes x 8 or 16 consecutive fp32 columns.
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float* v) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+}
+
+// ------------------------------------------------------------------------------------ one token's slice, held by one thread
+struct State { float m, z, u; };
+
+// The state with its sums about another maximum m >= s.m.  A state without a maximum has seen nothing (z = u = 0), or NaN only.
+__device__ __forceinline__ void move(State& s, float m, float scale) {
+    if (s.m != MINUS_INF) {
+        const float t = (s.m - m) * scale, f = ex2f(t);
+        s.u = f * fmaf(t, s.z, s.u);
+        s.z *= f;
+    }
+    s.m = m;
+}
+
+// Folds 32 logits (columns of which the first `valid` exist) into the state.
+__device__ __forceinline__ float fold32(State& s, float* v, int valid, float scale) {
+    if (valid < 32) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) if (j >= valid) v[j] = MINUS_INF;
+    }
+    float cmax = v[0];
+#pragma unroll
+    for (int j = 1; j < 32; ++j) cmax = fmaxf(cmax, v[j]);
+    const float m = fmaxf(s.m, cmax);
+    const f2 scale2 = pair(scale, scale), minus = pair(-m, -m);
+    f2 z0 = 0ull, u0 = 0ull, z1 = 0ull, u1 = 0ull;
+    if (valid < 32) {
+        float z = 0.f, u = 0.f;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const float t = (v[j] - m) * scale, e = ex2f(t);
+            if (j < valid) { z += e; u = fmaf(t, e, u); }
+        }
+        z0 = pair(z, 0.f); u0 = pair(u, 0.f);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+            const f2 ta = mul2(add2(pair(v[j], v[j + 1]), minus), scale2), tb = mul2(add2(pair(v[j + 2], v[j + 3]), minus), scale2);
+            const float2 a = split(ta), b = split(tb);
+            const f2 ea = pair(ex2f(a.x), ex2f(a.y)), eb = pair(ex2f(b.x), ex2f(b.y));
+            z0 = add2(z0, ea); z1 = add2(z1, eb);
+            u0 = fma2(ta, ea, u0); u1 = fma2(tb, eb, u1);
+        }
+    }
+    const float2 z = split(add2(z0, z1)), u = split(add2(u0, u1));
+    move(s, m, scale);
+    s.z += z.x + z.y;
+    s.u += u.x + u.y;
+    return cmax;
+}
+
+// A thread's best `top` logits of its slice, unordered, in shared memory: entry j of a thread at j * EPI_THREADS (both arrays).
+// What comes is taken if it is above `lim`; columns come in ascending order, so among equals the lower column stays.
+struct Best {
+    float* val;
+    uint8_t* col;
+    int n, top, at;                                         // entries, their most, where the least is (once full)
+    float lim;
+    __device__ __forceinline__ void offer(float x, int c) {
+        if (!(x > lim)) return;
+        if (n < top) { val[n * EPI_THREADS] = x; col[n * EPI_THREADS] = static_cast<uint8_t>(c); if (++n < top) return; }
+        else { val[at * EPI_THREADS] = x; col[at * EPI_THREADS] = static_cast<uint8_t>(c); }
+        // the least entry, of equals the one with the highest column, goes next
+        float least = val[0];
+        int cl = col[0];
+        at = 0;
+#pragma unroll 4
+        for (int j = 1; j < top; ++j) {
+            const float y = val[j * EPI_THREADS];
+            const int cy = col[j * EPI_THREADS];
+            if (y < least || (y == least && cy > cl)) { least = y; cl = cy; at = j; }
+        }
+        lim = least;
+    }
+};
+
+// ------------------------------------------------------------------------------------ the strip kernel
+// Two CTAs of a cluster per 256 x 256 tile (cta_group::2), persistent, tiles dealt round robin with the token tiles fastest (the tokens
+// of a launch stay in L2, the weight streams).  Warps: 0 copies, 1 issues the products, 2 to 9 the epilogue: a thread has one
+// token's 128 columns.
+//   bf16   the accumulator of a tile is complete in tensor memory; two of them, so the epilogue of one runs beside the products of
+//          the next
+//   8 bits every k-block of 128 has its own scale, so its product is its own accumulator, and the epilogue threads add it to their
+//          128 sums in registers with fp32 factors; the two buffers alternate by k-block
+constexpr int SMEM_MAX = 227 * 1024;
+constexpr int STAGE = TILE_M * KB_BYTES + HALF_N * KB_BYTES;       // 32 KB
+constexpr int LIST_BYTES = EPI_THREADS * MAX_TOP * 5, SCRATCH_BYTES = EPI_THREADS * 8 * 4;
+template <bool F8, bool TOP> struct Strip {
+    static constexpr int STAGES = TOP ? 6 : 7;
+    static constexpr int BARS = 2 * STAGES + 5;
+    static constexpr int LISTS = STAGES * STAGE + 512;              // offset behind barriers and slots
+    static constexpr int SMEM = 1024 + LISTS + (TOP ? LIST_BYTES + (F8 ? SCRATCH_BYTES : 0) : 0);
+    static_assert(8 * BARS + 16 <= 512 && SMEM <= SMEM_MAX, "shared memory per CTA");
+};
+
+template <bool F8, bool TOP>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+tl_strip_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ CUtensorMap tmW, const Params p) {
+    using S = Strip<F8, TOP>;
+    constexpr int STAGES = S::STAGES;
+    constexpr int KE = F8 ? 128 : 64;                               // elements of a k-block
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    uint8_t* const smem = smem_raw + (base - raw);
+    const uint32_t bars = base + STAGES * STAGE;
+    auto full_bar = [&](int s) { return bars + 8u * s; };                        // used in the leader only
+    auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
+    auto tfull_bar = [&](int a) { return bars + 8u * (2 * STAGES + a); };
+    auto tempty_bar = [&](int a) { return bars + 8u * (2 * STAGES + 2 + a); };   // used in the leader only
+    const uint32_t drain_bar = bars + 8u * (2 * STAGES + 4);
+    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + STAGES * STAGE + 8 * S::BARS);
+    volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const bool leader = rank == 0;
+    if (threadIdx.x == 0) {
+        *abort_flag = 0;
+        for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 2 * EPI_WARPS); }
+        mbar_init(drain_bar, 1);
+        fence_barrier_init();
+        fence_proxy_async();
+        prefetch_tensormap(&tmH);
+        prefetch_tensormap(&tmW);
+    }
+    if (warp == 1) {
+        tmem2_alloc(smem_u32(tmem_slot), 512);
+        tmem2_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    const int tiles = p.m_tiles * p.n_tiles, first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    constexpr uint32_t IDESC = F8 ? make_idesc(TILE_N, false, false, 2 * TILE_M, 0u) : make_idesc(TILE_N, false, false, 2 * TILE_M, 1u);
+
+    if (warp == 0) {
+        // ---------------------------------------------------------------- copies (both CTAs)
+        if (lane == 0) {
+            int stage = 0; uint32_t phase = 0; bool ok = true;
+            long issued = 0;
+            const uint64_t keep = make_policy(2), stream = make_policy(0);
+            for (int tile = first; ok && tile < tiles; tile += step) {
+                const int nt = tile / p.m_tiles, mt = tile - nt * p.m_tiles;
+                const int r0 = p.row0 + mt * 2 * TILE_M + static_cast<int>(rank) * TILE_M;
+                const int c0 = p.col0 + nt * TILE_N + static_cast<int>(rank) * HALF_N;
+                for (int kb = 0; kb < p.kbs; ++kb) {
+                    if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, p.wait_limit_ns)) { ok = false; break; }
+                    if (leader) mbar_arrive_expect_tx(full_bar(stage), 2 * STAGE);
+                    const uint32_t bar = mapa_shared(full_bar(stage), 0), sa = base + stage * STAGE;
+                    if (!(tile == 0 && kb == p.drop_kb)) {
+                        tma2_load_2d(sa, &tmH, bar, kb * KE, r0, keep);
+                        tma2_load_2d(sa + TILE_M * KB_BYTES, &tmW, bar, kb * KE, c0, stream);
+                    }
+                    ++issued;
+                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                }
+            }
+            if ((!ok || *abort_flag) && leader) {
+                // give-up path (the leader's barriers count both CTAs' bytes): let copies in flight land
+                const long back = issued < STAGES ? issued : STAGES;
+                int s = stage; uint32_t ph = phase;
+                for (long i = 0; i < back; ++i) {
+                    if (--s < 0) { s = STAGES - 1; ph ^= 1u; }
+                    const unsigned long long t0 = globaltimer_ns();
+                    while (!mbar_try_wait(full_bar(s), ph) && globaltimer_ns() - t0 < p.wait_limit_ns) {}
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------------------------------------------------------- products (leader)
+        if (lane == 0 && leader) {
+            int stage = 0; uint32_t phase = 0; bool ok = true;
+            int unit = 0;                                               // accumulators so far
+            for (int tile = first; ok && tile < tiles; tile += step) {
+                for (int kb = 0; kb < p.kbs; ++kb) {
+                    const int ab = unit & 1;
+                    if ((F8 || kb == 0) && !mbar_wait_cluster(tempty_bar(ab), ((unit >> 1) & 1) ^ 1u, abort_flag, p.wait_limit_ns)) { ok = false; break; }
+                    if (!mbar_wait(full_bar(stage), phase, abort_flag, p.wait_limit_ns)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t sa = base + stage * STAGE, tmem_d = tmem_base + ab * TILE_N;
+                    const uint64_t adesc = make_smem_desc(sa, 16, 1024), bdesc = make_smem_desc(sa + TILE_M * KB_BYTES, 16, 1024);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {                       // 32 bytes of every row per instruction
+                        const uint32_t more = (F8 ? k != 0 : (kb | k) != 0) ? 1u : 0u;
+                        if (F8) umma2_f8(tmem_d, adesc + 2 * k, bdesc + 2 * k, IDESC, more);
+                        else umma2_f16(tmem_d, adesc + 2 * k, bdesc + 2 * k, IDESC, more);
+                    }
+                    umma2_commit_both(empty_bar(stage));
+                    if (F8 || kb + 1 == p.kbs) { umma2_commit_both(tfull_bar(ab)); ++unit; }
+                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok || *abort_flag) {
+                umma2_commit_local(drain_bar);
+                const unsigned long long t0 = globaltimer_ns();
+                while (!mbar_try_wait(drain_bar, 0) && globaltimer_ns() - t0 < p.wait_limit_ns) {}
+            }
+        }
+    } else {
+        // ---------------------------------------------------------------- epilogue (both CTAs)
+        const int quad = warp & 3, half = (warp - 2) >> 2;
+        const int et = threadIdx.x - 64;
+        const uint32_t tmem_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + half * HALF_N;
+        Best best;
+        best.top = p.top;
+        best.val = reinterpret_cast<float*>(smem + S::LISTS) + et;
+        best.col = smem + S::LISTS + EPI_THREADS * MAX_TOP * 4 + et;
+        float* const scratch = reinterpret_cast<float*>(smem + S::LISTS + LIST_BYTES) + et;
+        auto release = [&](int ab) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(mapa_shared(tempty_bar(ab), 0));
+        };
+        bool ok = true;
+        int unit = 0;
+        for (int tile = first; ok && tile < tiles; tile += step) {
+            const int nt = tile / p.m_tiles, mt = tile - nt * p.m_tiles;
+            const int row = mt * 2 * TILE_M + static_cast<int>(rank) * TILE_M + quad * 32 + lane;
+            const bool row_ok = row < p.rows;
+            const int c0 = nt * TILE_N + half * HALF_N;                 // first column within the launch
+            const int valid = p.cols - c0;                              // columns that exist (may be <= 0)
+            const int token = p.tokens && row_ok ? p.tokens[row] : -1;
+            const int rel = token - (p.col0 + c0);                      // the token's column within this thread's, if 0 <= rel < 128
+            State s{MINUS_INF, 0.f, 0.f};
+            if (TOP) { best.n = 0; best.lim = row_ok ? below(from_ordered(__ldcg(p.floor + row))) : __builtin_huge_valf(); }
+            auto pick = [&](const float* v, int c) {                    // c: first of 32 columns
+                if (static_cast<unsigned>(rel - c) < 32u && rel < valid) {
+                    float x = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) if (j == rel - c) x = v[j];
+                    p.chosen[row] = x;
+                }
+            };
+            if constexpr (!F8) {
+                const int ab = unit & 1;
+                ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(ab), (unit >> 1) & 1, abort_flag, p.wait_limit_ns));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t acc = tmem_row + ab * TILE_N;
+#pragma unroll 1
+                for (int c = 0; c < HALF_N; c += 32) {
+                    if (c >= valid) break;
+                    float v[32];
+                    __syncwarp();
+                    tmem_ld32(acc + c, v);
+                    tmem_ld_wait();
+                    pick(v, c);
+                    const float cmax = fold32(s, v, valid - c, p.scale);
+                    if (TOP && __any_sync(0xffffffffu, cmax > best.lim)) {
+#pragma unroll 1
+                        for (int h = c; h < c + 32; h += 8) {
+                            float w[8];
+                            tmem_ld8(acc + h, w);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) if (h + j < valid) best.offer(w[j], h + j);
+                            __syncwarp();
+                        }
+                    }
+                }
+                ++unit;
+                release(ab);
+            } else {
+                f2 acc[HALF_N / 2];
+#pragma unroll
+                for (int j = 0; j < HALF_N / 2; ++j) acc[j] = 0ull;
+                const float* hs = p.hs + static_cast<size_t>(p.row0 + (row_ok ? row : 0)) * p.kbs;
+                const float* ws = p.ws + static_cast<size_t>(min(p.col0 + c0, p.V - 1) / 128) * p.kbs;
+                float f = __ldg(hs) * __ldg(ws);
+                for (int kb = 0; kb < p.kbs; ++kb) {
+                    const float next = kb + 1 < p.kbs ? __ldg(hs + kb + 1) * __ldg(ws + kb + 1) : 0.f;
+                    const int ab = unit & 1;
+                    ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(ab), (unit >> 1) & 1, abort_flag, p.wait_limit_ns));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t from = tmem_row + ab * TILE_N;
+                    const f2 factor = pair(f, f);
+                    __syncwarp();
+#pragma unroll
+                    for (int c = 0; c < HALF_N; c += 32) {
+                        float v[32];
+                        tmem_ld32(from + c, v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) acc[c / 2 + j] = fma2(pair(v[2 * j], v[2 * j + 1]), factor, acc[c / 2 + j]);
+                    }
+                    ++unit;
+                    release(ab);
+                    f = next;
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int c = 0; c < HALF_N; c += 32) {
+                    if (c < valid) {
+                        float v[32];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) { const float2 t = split(acc[c / 2 + j]); v[2 * j] = t.x; v[2 * j + 1] = t.y; }
+                        pick(v, c);
+                        const float cmax = fold32(s, v, valid - c, p.scale);
+                        if (TOP && __any_sync(0xffffffffu, cmax > best.lim)) {
+#pragma unroll
+                            for (int h = c; h < c + 32; h += 8) {
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) scratch[j * EPI_THREADS] = v[h - c + j];
+#pragma unroll 1
+                                for (int j = 0; j < 8; ++j) if (h + j < valid) best.offer(scratch[j * EPI_THREADS], h + j);
+                            }
+                            __syncwarp();
+                        }
+                    }
+                }
+            }
+            if (row_ok) {
+                const size_t at = static_cast<size_t>(row) * p.slices + 2 * nt + half;
+                p.part[at] = make_float4(s.m, s.z, s.u, TOP ? __int_as_float(best.n) : 0.f);
+                if (TOP) {
+                    uint2* const to = p.cand + at * p.top;
+                    for (int j = 0; j < best.n; ++j)
+                        to[j] = make_uint2(__float_as_uint(best.val[j * EPI_THREADS]), static_cast<unsigned>(p.col0 + c0 + best.col[j * EPI_THREADS]));
+                    if (best.n == p.top) atomicMax(p.floor + row, ordered(best.lim));
+                }
+            }
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();                          // no CTA leaves while its pair may still signal it or read its memory
+    if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, VPCE_DEV_WAIT_EXPIRED);
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tmem2_dealloc(tmem_base, 512);
+    }
+}
+
+// ------------------------------------------------------------------------------------ a token's list, held by one warp
+// Lane j has the (j + 1)-th best entry, larger logits first, among equals the lower column.
+struct List {
+    float val;
+    int id;
+    int lane, top;
+    __device__ __forceinline__ void clear() { val = MINUS_INF; id = INT_MAX; }
+    __device__ __forceinline__ static bool better(float a, int ia, float b, int ib) { return a > b || (a == b && ia < ib); }
+    // Every lane offers (x, c) if `has`; what is no better than the last entry is passed over.
+    __device__ __forceinline__ void offer(bool has, float x, int c) {
+        float last = __shfl_sync(0xffffffffu, val, top - 1);
+        int last_id = __shfl_sync(0xffffffffu, id, top - 1);
+        unsigned todo = __ballot_sync(0xffffffffu, has && better(x, c, last, last_id));
+        while (todo) {
+            const int from = __ffs(todo) - 1;
+            const float nx = __shfl_sync(0xffffffffu, x, from);
+            const int nc = __shfl_sync(0xffffffffu, c, from);
+            const int at = __popc(__ballot_sync(0xffffffffu, better(val, id, nx, nc)));
+            const float up = __shfl_up_sync(0xffffffffu, val, 1);
+            const int up_id = __shfl_up_sync(0xffffffffu, id, 1);
+            if (lane >= at) { val = lane == at ? nx : up; id = lane == at ? nc : up_id; }
+            last = __shfl_sync(0xffffffffu, val, top - 1);
+            last_id = __shfl_sync(0xffffffffu, id, top - 1);
+            todo &= todo - 1;
+            todo &= __ballot_sync(0xffffffffu, better(x, c, last, last_id));
+        }
+    }
+};
+
+// ------------------------------------------------------------------------------------ the kernel for few tokens
+// Up to 64 tokens: bound by reading W once.  W's rows are the products' M side (128 at a time), the tokens their N side (16, 32 or 64),
+// so no tensor-core work is spent on rows that are not there, and every CTA streams its own share of the vocabulary (a
+// multiple of 32 rows) through a ring of 6 to 8 stages.  The logits of a tile go through shared memory, so that a warp has a token's
+// 128 logits side by side: it keeps the token's state (a lane its own part) and list in registers from tile to tile.
+constexpr int FEW_TOKENS = 64, FEW_ROWS = 32;                       // W's rows per copy
+constexpr int FEW_BUFS = 4;
+template <int NT, bool F8> struct Few {
+    static constexpr int STAGES = NT == 64 ? 6 : 8;
+    static constexpr int STAGE_BYTES = TILE_M * KB_BYTES + NT * KB_BYTES;
+    static constexpr int BARS = 2 * STAGES + 2 * FEW_BUFS + 1;
+    static constexpr int PITCH = TILE_M + 4;                        // floats between tokens of the logits' tile
+    static constexpr int TILE = STAGES * STAGE_BYTES + 512;
+    static constexpr int SCALES = TILE + NT * PITCH * 4;            // 8 bits: [k-block][token]
+    static constexpr int SMEM_FIXED = 1024 + SCALES;
+    static constexpr int TMEM_COLS = FEW_BUFS * NT;
+    static_assert(8 * BARS + 16 <= 512 && STAGE_BYTES % 1024 == 0, "layout");
+};
+constexpr int FEW_MAX_KBS = 128;                                    // 8 bits: scales of 64 tokens in 32 KB
+
+__device__ __forceinline__ void epi_sync() { asm volatile("bar.sync 1, %0;" ::"n"(EPI_THREADS) : "memory"); }
+
+template <int NT, bool F8, bool TOP>
+__global__ void __launch_bounds__(THREADS, 1)
+tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ CUtensorMap tmW, const Params p) {
+    using S = Few<NT, F8>;
+    constexpr int STAGES = S::STAGES, KE = F8 ? 128 : 64, HALF = NT / 2, PER_WARP = NT / EPI_WARPS;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    uint8_t* const smem = smem_raw + (base - raw);
+    const uint32_t bars = base + STAGES * S::STAGE_BYTES;
+    auto full_bar = [&](int s) { return bars + 8u * s; };
+    auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
+    auto tfull_bar = [&](int a) { return bars + 8u * (2 * STAGES + a); };
+    auto tempty_bar = [&](int a) { return bars + 8u * (2 * STAGES + FEW_BUFS + a); };
+    const uint32_t drain_bar = bars + 8u * (2 * STAGES + 2 * FEW_BUFS);
+    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + STAGES * S::STAGE_BYTES + 8 * S::BARS);
+    volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        *abort_flag = 0;
+        for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+        for (int a = 0; a < FEW_BUFS; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), EPI_WARPS); }
+        mbar_init(drain_bar, 1);
+        fence_barrier_init();
+        fence_proxy_async();
+        prefetch_tensormap(&tmH);
+        prefetch_tensormap(&tmW);
+    }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(tmem_slot), S::TMEM_COLS);
+        tmem_relinquish();
+    }
+    float* const scales = reinterpret_cast<float*>(smem + S::SCALES);
+    if (F8)
+        for (int i = threadIdx.x; i < NT * p.kbs; i += THREADS) {
+            const int kb = i / NT, t = i - kb * NT;
+            scales[i] = t < p.rows ? p.hs[static_cast<size_t>(p.row0 + t) * p.kbs + kb] : 0.f;
+        }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    // this CTA's rows of W
+    const long units = (p.cols + FEW_ROWS - 1) / FEW_ROWS;
+    const int v0 = static_cast<int>(units * blockIdx.x / gridDim.x) * FEW_ROWS;
+    const int v1 = min(p.cols, static_cast<int>(units * (blockIdx.x + 1) / gridDim.x) * FEW_ROWS);
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int stage = 0; uint32_t phase = 0; bool ok = true;
+            long issued = 0;
+            const uint64_t keep = make_policy(2), stream = make_policy(1);
+            for (int r = v0; ok && r < v1; r += TILE_M) {
+                const int boxes = (min(v1 - r, TILE_M) + FEW_ROWS - 1) / FEW_ROWS;
+                for (int kb = 0; kb < p.kbs; ++kb) {
+                    if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, p.wait_limit_ns)) { ok = false; break; }
+                    mbar_arrive_expect_tx(full_bar(stage), boxes * FEW_ROWS * KB_BYTES + NT * KB_BYTES);
+                    const uint32_t sa = base + stage * S::STAGE_BYTES;
+                    if (!(blockIdx.x == 0 && r == v0 && kb == p.drop_kb)) {
+                        for (int b = 0; b < boxes; ++b)
+                            tma_load_2d_hint(sa + b * FEW_ROWS * KB_BYTES, &tmW, full_bar(stage), kb * KE, p.col0 + r + b * FEW_ROWS, stream);
+                        tma_load_2d_hint(sa + TILE_M * KB_BYTES, &tmH, full_bar(stage), kb * KE, p.row0, keep);
+                    }
+                    ++issued;
+                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok || *abort_flag) {
+                const long back = issued < STAGES ? issued : STAGES;
+                int s = stage; uint32_t ph = phase;
+                for (long i = 0; i < back; ++i) {
+                    if (--s < 0) { s = STAGES - 1; ph ^= 1u; }
+                    const unsigned long long t0 = globaltimer_ns();
+                    while (!mbar_try_wait(full_bar(s), ph) && globaltimer_ns() - t0 < p.wait_limit_ns) {}
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t IDESC = F8 ? make_idesc(NT, false, false, TILE_M, 0u) : make_idesc(NT, false, false, TILE_M, 1u);
+            int stage = 0; uint32_t phase = 0; bool ok = true;
+            int unit = 0;
+            for (int r = v0; ok && r < v1; r += TILE_M) {
+                for (int kb = 0; kb < p.kbs; ++kb) {
+                    const int ab = unit % FEW_BUFS;
+                    if ((F8 || kb == 0) && !mbar_wait(tempty_bar(ab), ((unit / FEW_BUFS) & 1) ^ 1u, abort_flag, p.wait_limit_ns)) { ok = false; break; }
+                    if (!mbar_wait(full_bar(stage), phase, abort_flag, p.wait_limit_ns)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t sa = base + stage * S::STAGE_BYTES, tmem_d = tmem_base + ab * NT;
+                    const uint64_t adesc = make_smem_desc(sa, 16, 1024), bdesc = make_smem_desc(sa + TILE_M * KB_BYTES, 16, 1024);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t more = (F8 ? k != 0 : (kb | k) != 0) ? 1u : 0u;
+                        if (F8) umma_f8(tmem_d, adesc + 2 * k, bdesc + 2 * k, IDESC, more);
+                        else umma_f16(tmem_d, adesc + 2 * k, bdesc + 2 * k, IDESC, more);
+                    }
+                    umma_commit(empty_bar(stage));
+                    if (F8 || kb + 1 == p.kbs) { umma_commit(tfull_bar(ab)); ++unit; }
+                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok || *abort_flag) {
+                umma_commit(drain_bar);
+                const unsigned long long t0 = globaltimer_ns();
+                while (!mbar_try_wait(drain_bar, 0) && globaltimer_ns() - t0 < p.wait_limit_ns) {}
+            }
+        }
+    } else {
+        const int quad = warp & 3, half = (warp - 2) >> 2, ew = warp - 2;
+        const uint32_t tmem_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + half * HALF;
+        float* const tile = reinterpret_cast<float*>(smem + S::TILE);
+        State s[PER_WARP];
+        List list[PER_WARP];
+        int token[PER_WARP];
+#pragma unroll
+        for (int i = 0; i < PER_WARP; ++i) {
+            s[i] = State{MINUS_INF, 0.f, 0.f};
+            list[i].lane = lane; list[i].top = p.top; list[i].clear();
+            const int t = ew * PER_WARP + i;
+            token[i] = p.tokens && t < p.rows ? p.tokens[t] : -1;
+        }
+        auto load_half = [&](uint32_t at, float* v) {
+            if constexpr (HALF == 8) tmem_ld8(at, v);
+            else if constexpr (HALF == 16) tmem_ld16(at, v);
+            else tmem_ld32(at, v);
+            tmem_ld_wait();
+        };
+        auto release = [&](int ab) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(tempty_bar(ab));
+        };
+        bool ok = true;
+        int unit = 0;
+        // A warp whose wait has run out goes on through the barriers with the others, without waiting or reading.
+        for (int r = v0; r < v1; r += TILE_M) {
+            float acc[HALF];
+#pragma unroll
+            for (int j = 0; j < HALF; ++j) acc[j] = 0.f;
+            auto wait = [&](int ab) {
+                if (ok) ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(ab), (unit / FEW_BUFS) & 1, abort_flag, p.wait_limit_ns));
+                return ok;
+            };
+            if constexpr (!F8) {
+                const int ab = unit % FEW_BUFS;
+                if (wait(ab)) {
+                    tc_fence_after();
+                    load_half(tmem_row + ab * NT, acc);
+                    ++unit;
+                    release(ab);
+                }
+            } else {
+                const float* ws = p.ws + static_cast<size_t>(min(p.col0 + r + quad * 32 + lane, p.V - 1) / 128) * p.kbs;
+                float f = __ldg(ws);
+                for (int kb = 0; kb < p.kbs; ++kb) {
+                    const float next = kb + 1 < p.kbs ? __ldg(ws + kb + 1) : 0.f;
+                    const int ab = unit % FEW_BUFS;
+                    if (!wait(ab)) break;
+                    tc_fence_after();
+                    float v[HALF];
+                    load_half(tmem_row + ab * NT, v);
+                    ++unit;
+                    release(ab);
+                    const float4* hs = reinterpret_cast<const float4*>(scales + kb * NT + half * HALF);
+#pragma unroll
+                    for (int j = 0; j < HALF / 4; ++j) {
+                        const float4 h = hs[j];
+                        acc[4 * j] = fmaf(v[4 * j], f * h.x, acc[4 * j]);
+                        acc[4 * j + 1] = fmaf(v[4 * j + 1], f * h.y, acc[4 * j + 1]);
+                        acc[4 * j + 2] = fmaf(v[4 * j + 2], f * h.z, acc[4 * j + 2]);
+                        acc[4 * j + 3] = fmaf(v[4 * j + 3], f * h.w, acc[4 * j + 3]);
+                    }
+                    f = next;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < HALF; ++j) tile[(half * HALF + j) * S::PITCH + quad * 32 + lane] = acc[j];
+            epi_sync();
+#pragma unroll
+            for (int i = 0; i < PER_WARP; ++i) {
+                const int t = ew * PER_WARP + i;
+                if (t < p.rows) {
+                    float x[4];
+                    float m = s[i].m;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        x[q] = tile[t * S::PITCH + 32 * q + lane];
+                        const int c = r + 32 * q + lane;
+                        if (c < v1) {
+                            m = fmaxf(m, x[q]);
+                            if (p.col0 + c == token[i]) p.chosen[t] = x[q];
+                        }
+                    }
+                    move(s[i], m, p.scale);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (r + 32 * q + lane < v1) {
+                            const float d = (x[q] - m) * p.scale, e = ex2f(d);
+                            s[i].z += e;
+                            s[i].u = fmaf(d, e, s[i].u);
+                        }
+                    }
+                    if (TOP) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int c = r + 32 * q + lane;
+                            list[i].offer(c < v1, x[q], p.col0 + c);
+                        }
+                    }
+                }
+            }
+            epi_sync();                                                 // the tile may be written again
+        }
+        // one slice per CTA and token
+        if (ok) {
+#pragma unroll
+            for (int i = 0; i < PER_WARP; ++i) {
+                const int t = ew * PER_WARP + i;
+                if (t < p.rows) {
+                    float m = s[i].m;
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    move(s[i], m, p.scale);
+                    float z = s[i].z, u = s[i].u;
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) {
+                        z += __shfl_xor_sync(0xffffffffu, z, o);
+                        u += __shfl_xor_sync(0xffffffffu, u, o);
+                    }
+                    const size_t at = static_cast<size_t>(t) * p.slices + blockIdx.x;
+                    const int n = TOP ? __popc(__ballot_sync(0xffffffffu, lane < p.top && list[i].id != INT_MAX)) : 0;
+                    if (lane == 0) p.part[at] = make_float4(m, z, u, __int_as_float(n));
+                    if (TOP && lane < n) p.cand[at * p.top + lane] = make_uint2(__float_as_uint(list[i].val), static_cast<unsigned>(list[i].id));
+                }
+            }
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, VPCE_DEV_WAIT_EXPIRED);
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem_base, S::TMEM_COLS);
+    }
+}
+
+// ------------------------------------------------------------------------------------ joining the slices
+struct JoinParams {
+    int rows, slices, top, first, last;
+    float scale, inv_temp;                      // log2(e) / temperature, 1 / temperature
+    const float4* part;
+    const uint2* cand;
+    float4* run;                                // [rows]: state over the launches so far
+    uint2* run_list;                            // [rows][top]
+    unsigned* floor;
+    const int32_t* tokens;
+    const float* chosen;
+    int ignore_index, V;
+    float *logp, *lse, *entropy, *top_logp;
+    int32_t* top_ids;
+    int* status;
+};
+
+constexpr int JOIN_THREADS = 128;
+// A warp per token, its lanes over the slices, 32 at a time, always in the same order.
+template <bool TOP>
+__global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams p) {
+    const int row = blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (row >= p.rows) return;
+    State s{MINUS_INF, 0.f, 0.f};
+    List list;
+    list.lane = lane; list.top = TOP ? p.top : 1; list.clear();
+    if (!p.first) {
+        const float4 r = p.run[row];
+        if (lane == 0) s = State{r.x, r.y, r.z};
+        if (TOP && lane < p.top) {
+            const uint2 e = p.run_list[static_cast<size_t>(row) * p.top + lane];
+            list.val = __uint_as_float(e.x);
+            list.id = static_cast<int>(e.y);
+        }
+    }
+    const float4* part = p.part + static_cast<size_t>(row) * p.slices;
+    const uint2* cand = p.cand + static_cast<size_t>(row) * p.slices * (TOP ? p.top : 0);
+    for (int i0 = 0; i0 < p.slices; i0 += 32) {
+        const int i = i0 + lane;
+        float4 q = make_float4(MINUS_INF, 0.f, 0.f, 0.f);
+        if (i < p.slices) q = part[i];
+        State o{q.x, q.y, q.z};
+        const float m = fmaxf(s.m, o.m);
+        move(s, m, p.scale);
+        move(o, m, p.scale);
+        s.z += o.z;
+        s.u += o.u;
+        if (TOP) {
+            const int n = i < p.slices ? __float_as_int(q.w) : 0;
+            const int most = __reduce_max_sync(0xffffffffu, n);
+            for (int j = 0; j < most; ++j) {
+                uint2 e = make_uint2(0u, 0u);
+                if (j < n) e = cand[static_cast<size_t>(i) * p.top + j];
+                list.offer(j < n, __uint_as_float(e.x), static_cast<int>(e.y));
+            }
+        }
+    }
+    // over the lanes
+    float m = s.m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    move(s, m, p.scale);
+    float z = s.z, u = s.u;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        z += __shfl_xor_sync(0xffffffffu, z, o);
+        u += __shfl_xor_sync(0xffffffffu, u, o);
+    }
+    if (!p.last) {
+        if (lane == 0) p.run[row] = make_float4(m, z, u, 0.f);
+        if (TOP) {
+            if (lane < p.top) p.run_list[static_cast<size_t>(row) * p.top + lane] = make_uint2(__float_as_uint(list.val), static_cast<unsigned>(list.id));
+            if (lane == p.top - 1 && list.id != INT_MAX) p.floor[row] = ordered(list.val);
+        }
+        return;
+    }
+    const float lz = logf(z);
+    if (lane == 0) {
+        if (p.lse) p.lse[row] = fmaf(m, p.inv_temp, lz);
+        if (p.entropy) p.entropy[row] = fmaxf(lz - LN2_F * (u / z), 0.f) + (z == z ? 0.f : z);
+        if (p.logp) {
+            const int t = p.tokens[row];
+            float out = 0.f;
+            if (t != p.ignore_index) {
+                if (static_cast<unsigned>(t) < static_cast<unsigned>(p.V)) out = (p.chosen[row] - m) * p.inv_temp - lz;
+                else atomicOr(p.status, VPCE_DEV_LABEL_OUT_OF_RANGE);
+            }
+            p.logp[row] = out;
+        }
+    }
+    if (TOP && lane < p.top) {
+        const bool some = list.id != INT_MAX;
+        p.top_logp[static_cast<size_t>(row) * p.top + lane] = some ? (list.val - m) * p.inv_temp - lz : MINUS_INF;
+        p.top_ids[static_cast<size_t>(row) * p.top + lane] = some ? list.id : -1;
+    }
+}
+
+}  // namespace vptl

@@ -41,6 +41,7 @@
 #include <tuple>
 #include <vector>
 
+#include "token_logp.h"
 #include "vp_ce.h"
 #include "vp_ce_kernels.cuh"
 #include "vp_ce_fixup.cuh"
@@ -227,7 +228,7 @@ cudaError_t launch_gemm(const CUtensorMap& tmA, const CUtensorMap& tmB, const CU
     const int tiles = p.m_tiles * p.n_tiles;
     if (tiles <= 0 || p.num_kb <= 0) return cudaSuccess;
     const int grid = tiles < num_sms() ? tiles : num_sms();
-    ProfEntry pe{EPI, nullptr, nullptr};
+    ProfEntry pe{kind_of(EPI), nullptr, nullptr};
     bool prof = false;
     {
         std::lock_guard<std::mutex> lk(g_prof_mu);
@@ -235,7 +236,7 @@ cudaError_t launch_gemm(const CUtensorMap& tmA, const CUtensorMap& tmB, const CU
     }
     if (prof && cudaEventCreate(&pe.a) == cudaSuccess && cudaEventCreate(&pe.b) == cudaSuccess) cudaEventRecord(pe.a, st);
     else prof = false;
-    kern<<<grid, NUM_THREADS, SMEM, st>>>(tmA, tmB, tmC, finish_params(p, EPI));
+    kern<<<grid, NUM_THREADS, SMEM, st>>>(tmA, tmB, tmC, finish_params(p, kind_of(EPI)));
     if (prof) {
         cudaEventRecord(pe.b, st);
         std::lock_guard<std::mutex> lk(g_prof_mu);
@@ -258,7 +259,7 @@ cudaError_t launch_pair(const CUtensorMap& tmA, const CUtensorMap& tmB, const CU
     const int n_cut = (EPI == EPI_DH || EPI == EPI_DW) ? std::min(p.n_cut, tiles) : 0;
     const int entries = tiles + n_cut * (std::max(p.k_split, 1) - 1);          // split tiles count once per part
     const int grid = 2 * (entries < max_pairs ? entries : max_pairs);
-    ProfEntry pe{EPI, nullptr, nullptr};
+    ProfEntry pe{kind_of(EPI), nullptr, nullptr};
     bool prof = false;
     {
         std::lock_guard<std::mutex> lk(g_prof_mu);
@@ -266,7 +267,7 @@ cudaError_t launch_pair(const CUtensorMap& tmA, const CUtensorMap& tmB, const CU
     }
     if (prof && cudaEventCreate(&pe.a) == cudaSuccess && cudaEventCreate(&pe.b) == cudaSuccess) cudaEventRecord(pe.a, st);
     else prof = false;
-    kern<<<grid, NUM_THREADS, SMEM, st>>>(tmA, tmB, tmC, finish_params(p, EPI));
+    kern<<<grid, NUM_THREADS, SMEM, st>>>(tmA, tmB, tmC, finish_params(p, kind_of(EPI)));
     if (prof) {
         cudaEventRecord(pe.b, st);
         std::lock_guard<std::mutex> lk(g_prof_mu);
@@ -507,6 +508,10 @@ struct GradCtx {
     int bn, pmask, ignore_index, V;
     int64_t d;
     bool pair_ok, mn3d;
+    // gradients of log probabilities and entropies instead of the loss's (vp_token_logp_backward)
+    bool score = false;
+    float inv_temp = 1.f;
+    const float *entropy = nullptr, *dent = nullptr;          // of the batch's first token
 };
 
 bool make_grad_ctx(GradCtx* c, const void* X, int64_t x_rows, const void* W, int64_t w_rows, int64_t d,
@@ -578,7 +583,12 @@ cudaError_t grad_meeting(const GradCtx& c, int phases, int x_row0, int rows, int
         p.status = c.status;
         apply_tuning(p, EPI_RESID);
         p.tile_counter = counters.take();
-        if ((c.pmask & 1) && p.m_tiles >= 2) e = launch_pair<BN_VOCAB, false, false, EPI_RESID>(c.tmX_k, c.tmW_khalf, c.tmG_st, p, st);
+        const bool pairs = (c.pmask & 1) && p.m_tiles >= 2;
+        if (c.score) {
+            p.entropy = c.entropy; p.dent = c.dent; p.inv_temp = c.inv_temp;
+            e = pairs ? launch_pair<BN_VOCAB, false, false, EPI_RESID_SCORE>(c.tmX_k, c.tmW_khalf, c.tmG_st, p, st)
+                      : launch_gemm<BN_VOCAB, false, false, EPI_RESID_SCORE>(c.tmX_k, c.tmW_k, c.tmG_st, p, st);
+        } else if (pairs) e = launch_pair<BN_VOCAB, false, false, EPI_RESID>(c.tmX_k, c.tmW_khalf, c.tmG_st, p, st);
         else e = launch_gemm<BN_VOCAB, false, false, EPI_RESID>(c.tmX_k, c.tmW_k, c.tmG_st, p, st);
         if (e != cudaSuccess) return e;
     }
@@ -702,11 +712,14 @@ vpce_status forward_impl(const void* H, const void* W, const int32_t* labels, in
     return counters.failed ? VPCE_CUDA_ERROR : VPCE_OK;
 }
 
+// What the backward pass of token_logp.h adds to the head's: dloss is then the gradient of the log probability (or null).
+struct ScoreGrad { const float *entropy, *dent; float inv_temp; };
+
 vpce_status backward_impl(const void* H, const void* W, const int32_t* labels, const float* lse,
                           const float* dloss, void* dH, float* dW, int64_t T, int64_t d, int64_t V,
                           int64_t block_v, int32_t ignore_index, int64_t T_chunk, int64_t chunk_index_base,
                           int accumulate_dW, void* workspace, size_t workspace_bytes, void* stream,
-                          bool clear_status) {
+                          bool clear_status, const ScoreGrad* score = nullptr) {
     WsLayout L;
     if (T == 0) {                                                      // empty batch: dW gets no contribution
         if (!accumulate_dW && dW && V > 0 && d > 0 &&
@@ -735,7 +748,7 @@ vpce_status backward_impl(const void* H, const void* W, const int32_t* labels, c
         g_launches.fetch_add(1, std::memory_order_relaxed);
     }
     CounterPool counters(reinterpret_cast<int*>(ws + L.counters), st);
-    if (!dloss) {
+    if (!dloss && !score) {
         vpce_count_valid_kernel<<<1, 1024, 0, st>>>(labels, T, static_cast<int>(V), ignore_index, c.inv_n, nullptr, c.status);
         g_launches.fetch_add(1, std::memory_order_relaxed);
     }
@@ -753,6 +766,12 @@ vpce_status backward_impl(const void* H, const void* W, const int32_t* labels, c
             // the chunk's tokens are sorted by target before its first meeting; after its last one the exact one-hot
             // terms of ALL shards are added in one go (every token's residue is on record by then)
             FixRange fix{0, i == P - 1 ? static_cast<int>(V) : 0, static_cast<const __nv_bfloat16*>(W), dW, i == 0};
+            if (score) {
+                c.score = true;
+                c.inv_temp = score->inv_temp;
+                c.entropy = score->entropy ? score->entropy + tok0 : nullptr;
+                c.dent = score->dent ? score->dent + tok0 : nullptr;
+            }
             if (grad_meeting(c, phases, static_cast<int>(tok0), rows, static_cast<int>(v_lo), cols, static_cast<int>(v_lo),
                              labels + tok0, lse + tok0, dloss ? dloss + tok0 : nullptr, i == 0, i == P - 1, acc,
                              dH ? static_cast<__nv_bfloat16*>(dH) + tok0 * d : nullptr, dW ? dW + v_lo * d : nullptr,
@@ -1126,3 +1145,15 @@ vpce_status vp_ce_forward_static(const void* H, const void* W, const int32_t* la
 }  // extern "C"
 
 #include "vp_ce_f32.inc"
+
+// ------------------------------------------------------------------------------------ token_logp.h, backward
+extern "C" int vp_token_logp_backward(const void* H, const void* W, const int32_t* tokens, const float* lse, const float* entropy,
+                                      const float* dlogp, const float* dent, void* dH, float* dW, int64_t T, int64_t d, int64_t V,
+                                      double temperature, int64_t block_v, int32_t ignore_index, int64_t T_chunk,
+                                      int64_t chunk_index_base, int accumulate_dW, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!(temperature > 0.0) || !(temperature < 1e30)) return VPCE_INVALID_ARG;
+    if (T > 0 && ((!dlogp && !dent) || (dent && !entropy))) return VPCE_INVALID_ARG;
+    const ScoreGrad score{entropy, dent, static_cast<float>(1.0 / temperature)};
+    return backward_impl(H, W, tokens, lse, dlogp, dH, dW, T, d, V, block_v, ignore_index, T_chunk, chunk_index_base, accumulate_dW, workspace,
+                         workspace_bytes, stream, true, &score);
+}

@@ -21,7 +21,10 @@ constexpr int SMEM_EXTRA = 2048;           // barriers + alignment slack
 // boxes (64 bf16 or 32 fp32 columns) that leave through TMA stores / reductions.
 constexpr int G_STAGING_BYTES = 4 * 2 * 4096;
 
-enum Epilogue { EPI_FOLD = 0, EPI_RESID = 1, EPI_DH = 2, EPI_DW = 3 };
+enum Epilogue { EPI_FOLD = 0, EPI_RESID = 1, EPI_DH = 2, EPI_DW = 3,
+                EPI_RESID_SCORE = 4 };                 // the residual of log probabilities and entropies (token_logp.h)
+// The kernel kind under which a launch is timed and its test hook armed.
+constexpr int kind_of(int epi) { return epi == EPI_RESID_SCORE ? static_cast<int>(EPI_RESID) : epi; }
 
 struct GemmParams {
     int m_tiles, n_tiles, num_kb;
@@ -61,6 +64,10 @@ struct GemmParams {
     // completes and the waits run out.  drop_kb < 0: off.  drop_ranks: bit r set = CTA rank r of the pair drops
     // (bit 0 alone for the single-CTA kernel).
     int drop_kb, drop_ranks;
+    // RESID_SCORE (dloss is then the gradient of the log probability; it and dent may be null)
+    const float* entropy;                  // chunk base
+    const float* dent;                     // chunk base
+    float inv_temp;                        // 1 / temperature
 };
 
 template <int BN, int EPI = EPI_FOLD> struct StageCfg {
@@ -145,6 +152,11 @@ __device__ __forceinline__ void epilogue_fold(const GemmParams& p, int mt, int n
 // The bf16 residual tile leaves through shared memory: each epilogue warp owns 32 rows; per 64
 // columns it fills a 32 x 128-byte box (128-byte swizzle: 16-byte chunk j of row r sits at chunk
 // j ^ (r & 7)) and one lane issues a TMA store, so global writes are whole 128-byte lines.
+//
+// SCORE: with x = v / temperature for logit v and p = exp(x - lse) the residual of a log probability's gradient dlogp and an entropy's
+// gradient dent is  (dlogp (onehot - p) - dent p (x - lse + entropy)) / temperature = p (a + b v) - dl onehot  with
+// dl = -dlogp / temperature, a = dl - dent (entropy - lse) / temperature, b = -dent / temperature^2.
+template <bool SCORE = false>
 __device__ __forceinline__ void epilogue_resid(const GemmParams& p, const CUtensorMap* tmG, uint32_t stage_smem,
                                                int mt, int nt, int row, int lane, uint32_t tmem_row) {
     const int grow = mt * BM + row;
@@ -154,7 +166,19 @@ __device__ __forceinline__ void epilogue_resid(const GemmParams& p, const CUtens
     // a label outside [0, V) is treated as ignored and flagged (once per row: by the strip's first tile)
     if (row_ok && !valid && label != p.ignore_index && nt == 0) atomicOr(p.status, VPCE_DEV_LABEL_OUT_OF_RANGE);
     float dl = 0.f, lseL = 0.f;
-    if (valid) dl = p.dloss ? p.dloss[grow] : *p.inv_n_valid;
+    float score_a = 0.f, score_b = 0.f, to_exp2 = LOG2E;
+    if constexpr (SCORE) {
+        if (valid && p.dloss) dl = -p.dloss[grow] * p.inv_temp;
+        score_a = dl;
+        if (row_ok && p.dent) {
+            const float de = p.dent[grow] * p.inv_temp;
+            score_a = fmaf(-de, p.entropy[grow] - p.lse[grow], dl);
+            score_b = -de * p.inv_temp;
+        }
+        to_exp2 = LOG2E * p.inv_temp;
+    } else {
+        if (valid) dl = p.dloss ? p.dloss[grow] : *p.inv_n_valid;
+    }
     if (row_ok) lseL = p.lse[grow] * LOG2E;
     const int lrel = valid ? label - (p.v_lo + nt * BN_VOCAB) : -1;
     const uint64_t pol_c = make_policy(p.hint_c);
@@ -174,7 +198,9 @@ __device__ __forceinline__ void epilogue_resid(const GemmParams& p, const CUtens
             const int jj = lrel - c * 32;
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-                float g = dl * ex2f(fmaf(v[j], LOG2E, -lseL));
+                float g;
+                if constexpr (SCORE) g = fmaf(score_b, v[j], score_a) * ex2f(fmaf(v[j], to_exp2, -lseL));
+                else g = dl * ex2f(fmaf(v[j], LOG2E, -lseL));
                 if (j == jj) g -= dl;
                 v[j] = (j < nvalid) ? g : 0.f;
             }
@@ -491,6 +517,7 @@ vpce_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
             const uint32_t tmem_row = tmem_base + ab * ACC_STRIDE + (static_cast<uint32_t>(quad * 32) << 16);
             if (EPI == EPI_FOLD) epilogue_fold(p, mt, nt, row, tmem_row);
             else if (EPI == EPI_RESID) epilogue_resid(p, &tmC, g_staging + (warp - 2) * 8192, mt, nt, row, lane, tmem_row);
+            else if (EPI == EPI_RESID_SCORE) epilogue_resid<true>(p, &tmC, g_staging + (warp - 2) * 8192, mt, nt, row, lane, tmem_row);
             else epilogue_f32_tile(&tmC, g_staging + (warp - 2) * 8192, nt * BN, p.c_row0 + mt * BM + quad * 32, lane,
                                    tmem_row, tile_n(nt), p.accumulate != 0);
             tc_fence_before();
@@ -805,6 +832,7 @@ vpce_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
             if (EPI == EPI_FOLD) epilogue_fold(p, mt, nt, row, tmem_row);
             else if (EPI == EPI_RESID && TF32) epilogue_resid_f32(p, &tmC, g_staging + (warp - 2) * 8192, mt, nt, row, lane, tmem_row);
             else if (EPI == EPI_RESID) epilogue_resid(p, &tmC, g_staging + (warp - 2) * 8192, mt, nt, row, lane, tmem_row);
+            else if (EPI == EPI_RESID_SCORE) epilogue_resid<true>(p, &tmC, g_staging + (warp - 2) * 8192, mt, nt, row, lane, tmem_row);
             else {
                 // parts of a split tile add in the order of their index: wait for this warp's rows of the part before
                 int* flag = w.slot >= 0 ? p.split_flags + w.slot * 8 + static_cast<int>(rank) * 4 + quad : nullptr;

@@ -1,5 +1,6 @@
-"""ctypes binding of the operators from the residual stream to log probabilities (rms_norm.h): argument marshalling only, same
-names as the C entry points, and the front ends ``rms_norm`` (torch.autograd) and ``rms_norm_fp8``.
+"""ctypes binding of the operators from the residual stream to log probabilities (rms_norm.h, token_logp.h, fp8_blocks.h): argument
+marshalling only, same names as the C entry points, and the front ends ``rms_norm`` and ``token_log_probs`` (torch.autograd),
+``rms_norm_fp8``, ``quantize_blocks_fp8`` and ``token_log_probs_fp8``.
 
 As in the other bindings, the functions check device, dtype, shape and contiguity, pass raw device pointers and the current stream,
 and turn non-zero status codes into ``VpceError``.  There is no CPU or PyTorch fallback.  The gradients have no derivative of
@@ -8,13 +9,13 @@ their own: differentiating them again raises.
 from __future__ import annotations
 
 import ctypes
-from typing import Optional, Tuple, Union
+from typing import NamedTuple, Optional, Tuple, Union
 
 import torch
 
-from .autograd import first_derivative_only
+from .autograd import _pick_chunk, _workspace as _ce_workspace, first_derivative_only
 from .binding import load_library
-from .training_ops import _DTYPE_CODE, _F32, _call, _device, _opt, _ptr, _rows, _stream, _workspace
+from .training_ops import _BF16, _DTYPE_CODE, _F32, _call, _device, _fail, _opt, _ptr, _rows, _stream, _workspace
 
 _F8 = torch.float8_e4m3fn
 FP8_BLOCK = 128                                            # columns (and rows of a weight) that share a scale
@@ -32,6 +33,13 @@ def _lib() -> ctypes.CDLL:
             "vp_rms_forward_fp8": (i32, [vp, i32, i64, i64, i64, vp, i64, vp, i32, f64, vp, i64, vp, vp, i64, vp, vp]),
             "vp_rms_workspace_bytes": (sz, [i64, i64]),
             "vp_rms_backward": (i32, [vp, i64, vp, i64, vp, i64, i32, i64, i64, vp, i32, vp, vp, i64, vp, vp, sz, vp]),
+            "vp_token_logp_workspace_bytes": (sz, [i64, i64, i64, i32]),
+            "vp_token_logp_forward": (i32, [vp, vp, vp, i64, i64, i64, f64, i32, vp, vp, vp, vp, vp, i32, vp, sz, vp]),
+            "vp_token_logp_backward": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, f64, i64, i32, i64, i64, i32, vp, sz, vp]),
+            "vp_token_logp_debug_drop": (i32, [i32]),
+            "vp_token_logp_fp8_workspace_bytes": (sz, [i64, i64, i64, i32]),
+            "vp_token_logp_fp8_forward": (i32, [vp, vp, vp, vp, vp, i64, i64, i64, f64, i32, vp, vp, vp, vp, vp, i32, vp, sz, vp]),
+            "vp_fp8_quantize_blocks": (i32, [vp, i32, i64, i64, i64, vp, i64, vp, vp]),
         }
         for name, (res, args) in signatures.items():
             fn = getattr(lib, name)
@@ -190,3 +198,215 @@ def rms_norm_fp8(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residua
     vp_rms_forward_fp8(x2, None if residual is None else _as_rows(residual, d), None if weight is None else weight.contiguous(), float(eps),
                        q.view(x2.shape), scales, None if z is None else z.view(x2.shape), None)
     return (q, scales) if z is None else (q, scales, z)
+
+
+# --------------------------------------------------------------------------- quantisation in blocks (fp8_blocks.h)
+def vp_fp8_quantize_blocks(w, q, scales, stream=None) -> None:
+    """q [rows, d] float8_e4m3fn and scales [ceil(rows / 128), ceil(d / 128)] float32 of the weight w [rows, d], w = q * scale.  See
+    include/fp8_blocks.h."""
+    dev = _device(w, "w")
+    if w.dim() != 2 or w.dtype not in _DTYPE_CODE:
+        raise TypeError(f"w must be [rows, d] in bfloat16, float16 or float32, got {list(w.shape)} {w.dtype}")
+    rows, d = w.shape
+    wp, ws = _rows(w, w.dtype, "w", rows, d, dev)
+    qp, qs = _rows(q, _F8, "q", rows, d, dev)
+    _call(_lib().vp_fp8_quantize_blocks, dev, wp, _DTYPE_CODE[w.dtype], rows, d, ws, qp, qs,
+          _ptr(scales, _F32, "scales", fp8_blocks(rows) * fp8_blocks(d), dev), _stream(stream, dev))
+
+
+def quantize_blocks_fp8(w: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(q, scales) of a weight [rows, d]: float8_e4m3fn and one float32 scale for each 128 x 128 block, w = q * scale.
+
+    What ``token_log_probs_fp8`` takes as its weight.  There is no gradient."""
+    _device(w, "w")
+    if w.dim() != 2:
+        raise ValueError(f"w must be [rows, d], got {list(w.shape)}")
+    w = w.detach()
+    rows, d = w.shape
+    w = _as_rows(w, d)
+    q = torch.empty(rows, d, dtype=_F8, device=w.device)
+    scales = torch.empty(fp8_blocks(rows), fp8_blocks(d), dtype=_F32, device=w.device)
+    vp_fp8_quantize_blocks(w, q, scales)
+    return q, scales
+
+
+# --------------------------------------------------------------------------- token log probabilities (token_logp.h)
+MAX_TOP = 20                                               # alternatives per token
+
+_I32 = torch.int32
+
+
+def vp_token_logp_workspace_bytes(T: int, d: int, V: int, top: int) -> int:
+    return _lib().vp_token_logp_workspace_bytes(T, d, V, top)
+
+
+def vp_token_logp_fp8_workspace_bytes(T: int, d: int, V: int, top: int) -> int:
+    return _lib().vp_token_logp_fp8_workspace_bytes(T, d, V, top)
+
+
+def _head_shapes(H, W, h: str, w: str):
+    dev = _device(H, h)
+    _device(W, w)
+    if H.dim() != 2 or W.dim() != 2 or H.shape[1] != W.shape[1]:
+        raise ValueError(f"{h} must be [T, d] and {w} [V, d], got {list(H.shape)} and {list(W.shape)}")
+    return dev, H.shape[0], H.shape[1], W.shape[0]
+
+
+def _logp_outputs(dev, T, tokens, logp, lse, entropy, top_logp, top_ids):
+    if (tokens is None) != (logp is None):
+        raise ValueError("tokens and logp go together")
+    if (top_logp is None) != (top_ids is None):
+        raise ValueError("top_logp and top_ids go together")
+    top = 0
+    if top_logp is not None:
+        if top_logp.dim() != 2 or top_logp.shape[0] != T:
+            raise ValueError(f"top_logp must be [{T}, alternatives], got {list(top_logp.shape)}")
+        top = top_logp.shape[1]
+    return top, (_opt(logp, _F32, "logp", T, dev), _opt(lse, _F32, "lse", T, dev), _opt(entropy, _F32, "entropy", T, dev),
+                 _opt(top_logp, _F32, "top_logp", T * top, dev), _opt(top_ids, _I32, "top_ids", T * top, dev), top)
+
+
+def vp_token_logp_forward(H, W, tokens, temperature: float, ignore_index: int, logp, lse, entropy, top_logp, top_ids, workspace,
+                          stream=None) -> None:
+    """logp, lse, entropy [T] and the alternatives top_logp, top_ids [T, top] of H [T, d] and W [V, d] (bfloat16) at the given tokens
+    [T] (int32).  tokens and logp, lse, entropy, top_logp and top_ids may be None.  See include/token_logp.h."""
+    dev, T, d, V = _head_shapes(H, W, "H", "W")
+    top, outs = _logp_outputs(dev, T, tokens, logp, lse, entropy, top_logp, top_ids)
+    wsp, wsn = _workspace(workspace, dev)
+    _call(_lib().vp_token_logp_forward, dev, _ptr(H, _BF16, "H", T * d, dev), _ptr(W, _BF16, "W", V * d, dev),
+          _opt(tokens, _I32, "tokens", T, dev), T, d, V, temperature, ignore_index, *outs, wsp, wsn, _stream(stream, dev))
+
+
+def vp_token_logp_fp8_forward(Hq, Hs, Wq, Ws, tokens, temperature: float, ignore_index: int, logp, lse, entropy, top_logp, top_ids,
+                              workspace, stream=None) -> None:
+    """The same from 8-bit operands: Hq [T, d] and Wq [V, d] float8_e4m3fn with their float32 scales Hs [T, ceil(d / 128)] and Ws
+    [ceil(V / 128), ceil(d / 128)].  See include/token_logp.h."""
+    dev, T, d, V = _head_shapes(Hq, Wq, "Hq", "Wq")
+    top, outs = _logp_outputs(dev, T, tokens, logp, lse, entropy, top_logp, top_ids)
+    wsp, wsn = _workspace(workspace, dev)
+    _call(_lib().vp_token_logp_fp8_forward, dev, _ptr(Hq, _F8, "Hq", T * d, dev), _ptr(Hs, _F32, "Hs", T * fp8_blocks(d), dev),
+          _ptr(Wq, _F8, "Wq", V * d, dev), _ptr(Ws, _F32, "Ws", fp8_blocks(V) * fp8_blocks(d), dev), _opt(tokens, _I32, "tokens", T, dev), T, d,
+          V, temperature, ignore_index, *outs, wsp, wsn, _stream(stream, dev))
+
+
+def vp_token_logp_backward(H, W, tokens, lse, entropy, dlogp, dent, temperature: float, ignore_index: int, dH, dW, block_v: int, T_chunk: int,
+                           accumulate_dW: bool, workspace, chunk_index_base: int = 0, stream=None) -> None:
+    """dH [T, d] (bfloat16) and dW [V, d] (float32, overwritten or added to) from the upstream gradients dlogp and dent [T] (one of
+    them may be None, as may dH or dW) and the forward call's lse and entropy (the latter with dent only).  workspace:
+    vp_ce_workspace_bytes(T_chunk, d, block_v).  See include/token_logp.h."""
+    dev, T, d, V = _head_shapes(H, W, "H", "W")
+    wsp, wsn = _workspace(workspace, dev)
+    _call(_lib().vp_token_logp_backward, dev, _ptr(H, _BF16, "H", T * d, dev), _ptr(W, _BF16, "W", V * d, dev),
+          _ptr(tokens, _I32, "tokens", T, dev), _ptr(lse, _F32, "lse", T, dev), _opt(entropy, _F32, "entropy", T, dev),
+          _opt(dlogp, _F32, "dlogp", T, dev), _opt(dent, _F32, "dent", T, dev), _opt(dH, _BF16, "dH", T * d, dev),
+          _opt(dW, _F32, "dW", V * d, dev), T, d, V, temperature, block_v, ignore_index, T_chunk, chunk_index_base, 1 if accumulate_dW else 0,
+          wsp, wsn, _stream(stream, dev))
+
+
+def vp_token_logp_debug_drop(k_block: int) -> None:
+    """Test hook: the next forward launch loses the copies of one k-block (see include/token_logp.h); < 0 disarms."""
+    code = _lib().vp_token_logp_debug_drop(k_block)
+    if code:
+        _fail(code)
+
+
+class TokenLogProbs(NamedTuple):
+    """Log probability of each given token (None without tokens), entropy of its distribution, and the alternatives' log
+    probabilities and ids [T, top_k] (None where top_k is 0)."""
+    logp: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    top_logp: Optional[torch.Tensor]
+    top_ids: Optional[torch.Tensor]
+
+
+def _check_top(top_k: int, V: int) -> int:
+    top_k = int(top_k)
+    if not 0 <= top_k <= min(MAX_TOP, V):
+        raise ValueError(f"top_k must lie between 0 and {min(MAX_TOP, V)}, got {top_k}")
+    return top_k
+
+
+def _empty_outputs(T: int, top: int, tokens, device):
+    f32 = lambda *shape: torch.empty(*shape, dtype=_F32, device=device)  # noqa: E731
+    return (None if tokens is None else f32(T), f32(T), f32(T), f32(T, top) if top else None,
+            torch.empty(T, top, dtype=_I32, device=device) if top else None)
+
+
+class _TokenLogProbs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, H, W, tokens, top, temperature, ignore_index, block_v, T_chunk, dW_accum):
+        H, W = H.contiguous(), W.contiguous()
+        tokens = None if tokens is None else tokens.to(_I32).contiguous()
+        T, d = H.shape
+        logp, lse, entropy, top_logp, top_ids = _empty_outputs(T, top, tokens, H.device)
+        n = vp_token_logp_workspace_bytes(T, d, W.shape[0], top)
+        if n == 0:
+            raise ValueError(f"unsupported shape: d must be a multiple of 8, got {d}")
+        vp_token_logp_forward(H, W, tokens, temperature, ignore_index, logp, lse, entropy, top_logp, top_ids,
+                              torch.empty(n, dtype=torch.uint8, device=H.device))
+        ctx.save_for_backward(H, W, tokens, lse, entropy)
+        ctx.cfg = (temperature, ignore_index, block_v, T_chunk)
+        ctx.dW_accum = dW_accum
+        ctx.set_materialize_grads(False)
+        if top:
+            ctx.mark_non_differentiable(top_logp, top_ids)
+        return logp, entropy, top_logp, top_ids
+
+    @staticmethod
+    @first_derivative_only
+    def backward(ctx, dlogp, dent, _top_logp, _top_ids):
+        H, W, tokens, lse, entropy = ctx.saved_tensors
+        temperature, ignore_index, block_v, T_chunk = ctx.cfg
+        accum = ctx.dW_accum
+        need_dH, need_dW = ctx.needs_input_grad[0], accum is not None or ctx.needs_input_grad[1]
+        if not (need_dH or need_dW) or (dlogp is None and dent is None):
+            return (None,) * 9
+        T, d = H.shape
+        T_chunk = _pick_chunk(T, T_chunk)
+        ws = _ce_workspace(T_chunk, d, block_v, H.device)
+        dH = torch.empty_like(H) if need_dH else None
+        dW = None
+        if need_dW:
+            dW = accum if accum is not None else torch.empty(W.shape, dtype=_F32, device=W.device)
+        if tokens is None:
+            tokens = torch.full((T,), ignore_index, dtype=_I32, device=H.device)
+        grads = [None if g is None else g.to(_F32).contiguous() for g in (dlogp, dent)]
+        vp_token_logp_backward(H, W, tokens, lse, entropy, *grads, temperature, ignore_index, dH, dW, block_v, T_chunk, accum is not None, ws)
+        # with an fp32 accumulation buffer the weight gradient lives there (main-grad style); autograd gets none
+        grad_W = None if (accum is not None or dW is None) else dW.to(W.dtype)
+        return (dH, grad_W) + (None,) * 7
+
+
+def token_log_probs(H: torch.Tensor, W: torch.Tensor, tokens: Optional[torch.Tensor] = None, top_k: int = 0, temperature: float = 1.0,
+                    ignore_index: int = -100, block_v: int = 8192, T_chunk: Optional[int] = None,
+                    dW_accum: Optional[torch.Tensor] = None) -> TokenLogProbs:
+    """Log probabilities of ``tokens`` under softmax(H @ W.T / temperature), with entropy and ``top_k`` alternatives.
+
+    H ``[T, d]`` and W ``[V, d]`` are bfloat16 CUDA tensors, ``tokens`` ``[T]`` integer (``ignore_index``: logp 0, no gradient), or
+    None where only entropy and alternatives are asked for.  logp and entropy are differentiable in H and W; the logits are never
+    materialised.  Alternatives come larger first, among equals the lower id; at most 20.  ``block_v`` and ``T_chunk`` are the backward
+    pass's, as is ``dW_accum`` (float32 ``[V, d]``: the weight gradient is added into it and ``W.grad`` stays untouched); see
+    ``vocab_proj_cross_entropy``."""
+    _, _, _, V = _head_shapes(H, W, "H", "W")
+    if H.dtype is not _BF16 or W.dtype is not _BF16:
+        raise TypeError("H and W must be bfloat16 CUDA tensors")
+    return TokenLogProbs(*_TokenLogProbs.apply(H, W, tokens, _check_top(top_k, V), float(temperature), int(ignore_index), int(block_v), T_chunk,
+                                               dW_accum))
+
+
+def token_log_probs_fp8(Hq: torch.Tensor, Hs: torch.Tensor, Wq: torch.Tensor, Ws: torch.Tensor, tokens: Optional[torch.Tensor] = None,
+                        top_k: int = 0, temperature: float = 1.0, ignore_index: int = -100) -> TokenLogProbs:
+    """``token_log_probs`` from 8-bit operands, without a gradient: for scoring and generation.
+
+    Hq ``[T, d]`` with Hs ``[T, ceil(d / 128)]`` is what ``rms_norm_fp8`` returns, Wq ``[V, d]`` with Ws what ``quantize_blocks_fp8``
+    returns."""
+    _, T, d, V = _head_shapes(Hq, Wq, "Hq", "Wq")
+    top = _check_top(top_k, V)
+    tokens = None if tokens is None else tokens.to(_I32).contiguous()
+    logp, lse, entropy, top_logp, top_ids = _empty_outputs(T, top, tokens, Hq.device)
+    n = vp_token_logp_fp8_workspace_bytes(T, d, V, top)
+    if n == 0:
+        raise ValueError(f"unsupported shape: d must be a multiple of 16, at most 16384, got {d}")
+    vp_token_logp_fp8_forward(Hq.contiguous(), Hs.contiguous(), Wq.contiguous(), Ws.contiguous(), tokens, float(temperature), int(ignore_index), logp,
+                              lse, entropy, top_logp, top_ids, torch.empty(n, dtype=torch.uint8, device=Hq.device))
+    return TokenLogProbs(logp, entropy, top_logp, top_ids)
