@@ -97,7 +97,9 @@ struct CounterPool {
         }
         return base + next++;
     }
-    int* take_n(int k) {                                      // k consecutive zeroed counters
+    // k consecutive zeroed counters.  All that one launch needs is taken at once: a second call may zero the pool again and hand
+    // the launch's first ones out to a later launch, which would find what this one has left in them.
+    int* take_n(int k) {
         if (next + k > NUM_TILE_COUNTERS) {
             failed = failed || cudaMemsetAsync(base, 0, 4 * NUM_TILE_COUNTERS, st) != cudaSuccess;
             next = 0;
@@ -487,7 +489,8 @@ cudaError_t fold_meeting(const FoldCtx& c, int x_row0, int rows, int w_row0, int
     return cudaGetLastError();
 }
 
-// Tail split of a gradient GEMM launched as CTA pairs (p.m_tiles, p.n_tiles, p.group_n, p.num_kb set; out_cols = N).
+// Tail split of a gradient GEMM launched as CTA pairs (p.m_tiles, p.n_tiles, p.group_n, p.num_kb set; out_cols = N), and the
+// launch's tile counter.
 void set_split(GemmParams& p, int64_t out_cols, CounterPool& counters, int width_unit = 128) {
     const int left = static_cast<int>(out_cols - static_cast<int64_t>(p.n_tiles - 1) * 256);
     const int last_width = left >= 256 ? 256 : (left + width_unit - 1) / width_unit * width_unit;
@@ -495,7 +498,9 @@ void set_split(GemmParams& p, int64_t out_cols, CounterPool& counters, int width
     p.n_cut = c.n_cut;
     p.k_split = c.ks;
     p.k_stagger = c.stagger;
-    p.split_flags = c.n_cut > 0 ? counters.take_n(8 * c.n_cut) : nullptr;
+    int* taken = counters.take_n(8 * c.n_cut + 1);
+    p.tile_counter = taken + 8 * c.n_cut;
+    p.split_flags = c.n_cut > 0 ? taken : nullptr;
 }
 
 // Tensor maps and workspace pointers of the backward meetings of one call.
@@ -614,7 +619,6 @@ cudaError_t grad_meeting(const GradCtx& c, int phases, int x_row0, int rows, int
         ph.b_3d = c.mn3d;
         set_split(ph, d, counters);
         apply_tuning(ph, EPI_DH);
-        ph.tile_counter = counters.take();
         if ((c.pmask & 2) && c.pair_ok && ph.m_tiles >= 2) e = launch_pair<256, false, true, EPI_DH>(c.tmG_k, c.tmW_mn2, tmAcc, ph, st);
         else e = launch_grad<false, true, EPI_DH>(c.bn, c.tmG_k, c.tmW_mn, tmAcc, ph, st);
         if (e != cudaSuccess) return e;
@@ -644,7 +648,6 @@ cudaError_t grad_meeting(const GradCtx& c, int phases, int x_row0, int rows, int
         pw.a_3d = c.mn3d; pw.b_3d = c.mn3d;
         set_split(pw, d, counters);
         apply_tuning(pw, EPI_DW);
-        pw.tile_counter = counters.take();
         if ((c.pmask & 4) && c.pair_ok && pw.m_tiles >= 2) e = launch_pair<256, true, true, EPI_DW>(c.tmG_mn, c.tmX_mn2, tmDW, pw, st);
         else e = launch_grad<true, true, EPI_DW>(c.bn, c.tmG_mn, c.tmX_mn, tmDW, pw, st);
         if (e != cudaSuccess) return e;
