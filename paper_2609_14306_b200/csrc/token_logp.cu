@@ -139,6 +139,20 @@ template <bool F8, bool TOP> cudaError_t launch_few(int nt, const CUtensorMap& h
     return launch_few<64, F8, TOP>(h, w, p, st);
 }
 
+// Brought up while the kernel before it still runs (it waits for that one's end before it reads anything).
+template <bool TOP, bool FEW> cudaError_t launch_join(int blocks, const JoinParams& j, cudaStream_t st) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(JOIN_THREADS);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, tl_join_kernel<TOP, FEW>, j);
+}
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 constexpr int64_t D_MOST_BF16 = 1 << 20, D_MOST_F8 = FEW_MAX_KBS * 128;
@@ -186,9 +200,9 @@ int forward(const void* H, const float* Hs, const void* W, const float* Ws, cons
     j.ignore_index = ignore_index; j.V = p.V; j.status = p.status;
 
     for (int64_t t0 = 0; t0 < T; t0 += pl.chunk) {
-        // the status word before the first chunk, the tokens' bounds before every one
+        // strips: the status word before the first chunk, the tokens' bounds before every one
         const size_t from = t0 == 0 ? 0 : pl.floor, to = top > 0 ? pl.chosen : pl.floor;
-        if (from < to && cudaMemsetAsync(ws + from, 0, to - from, st) != cudaSuccess) return VPCE_CUDA_ERROR;
+        if (!pl.few && from < to && cudaMemsetAsync(ws + from, 0, to - from, st) != cudaSuccess) return VPCE_CUDA_ERROR;
         p.rows = j.rows = static_cast<int>(std::min(pl.chunk, T - t0));
         p.row0 = static_cast<int>(t0);
         p.tokens = j.tokens = tokens ? tokens + t0 : nullptr;
@@ -211,9 +225,9 @@ int forward(const void* H, const float* Hs, const void* W, const float* Ws, cons
             j.first = c0 == 0;
             j.last = c0 + strip >= V;
             const int blocks = (j.rows + JOIN_THREADS / 32 - 1) / (JOIN_THREADS / 32);
-            if (top) tl_join_kernel<true><<<blocks, JOIN_THREADS, 0, st>>>(j);
-            else tl_join_kernel<false><<<blocks, JOIN_THREADS, 0, st>>>(j);
-            if (cudaGetLastError() != cudaSuccess) return VPCE_CUDA_ERROR;
+            if (pl.few) e = top ? launch_join<true, true>(blocks, j, st) : launch_join<false, true>(blocks, j, st);
+            else e = top ? launch_join<true, false>(blocks, j, st) : launch_join<false, false>(blocks, j, st);
+            if (e != cudaSuccess) return VPCE_CUDA_ERROR;
             p.drop_kb = -1;
         }
     }

@@ -23,7 +23,9 @@ constexpr float MINUS_INF = -__builtin_huge_valf();
 
 constexpr int KB_BYTES = 128;                               // a k-block: 128 bytes of every row (64 bf16 or 128 e4m3)
 constexpr int TILE_M = 128, TILE_N = 256, HALF_N = 128;     // rows per CTA, columns per pair tile, columns per epilogue thread
-constexpr int EPI_WARPS = 8, EPI_THREADS = 32 * EPI_WARPS, THREADS = 64 + EPI_THREADS;
+// Warps: 0 copies, 1 issues the products, 2 and 3 have nothing to do (the first four are one warp group, which gives up registers), 4 to 11
+// are the epilogue.
+constexpr int EPI_WARPS = 8, EPI_THREADS = 32 * EPI_WARPS, EPI_FIRST = 128, THREADS = EPI_FIRST + EPI_THREADS;
 
 struct Params {
     int rows, cols;                         // tokens of this launch, vocabulary columns of this launch
@@ -96,6 +98,33 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
           "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(taddr) : "memory");
 }
+
+// 64 consecutive columns.
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float* v) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+        "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+        "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+          "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+          "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+          "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+          "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+        : "r"(taddr) : "memory");
+}
+// Registers of the 8-bit strip kernel: launched with 168 a thread (384 threads: 64512), 40 are left to the first warp group's and the
+// epilogue's have 232: 128 x 40 + 256 x 232 = 64512.
+__device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 40;"); }
+__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 232;"); }
+// Programmatic launch: the grid that follows may be brought up; what it does after its wait comes after this one's end.
+__device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // ------------------------------------------------------------------------------------ one token's slice, held by one thread
 struct State { float m, z, u; };
@@ -174,8 +203,7 @@ struct Best {
 
 // ------------------------------------------------------------------------------------ the strip kernel
 // Two CTAs of a cluster per 256 x 256 tile (cta_group::2), persistent, tiles dealt round robin with the token tiles fastest (the tokens
-// of a launch stay in L2, the weight streams).  Warps: 0 copies, 1 issues the products, 2 to 9 the epilogue: a thread has one
-// token's 128 columns.
+// of a launch stay in L2, the weight streams).  An epilogue thread has one token's 128 columns.
 //   bf16   the accumulator of a tile is complete in tensor memory; two of them, so the epilogue of one runs beside the products of
 //          the next
 //   8 bits every k-block of 128 has its own scale, so its product is its own accumulator, and the epilogue threads add it to their
@@ -234,6 +262,7 @@ tl_strip_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__
     const int tiles = p.m_tiles * p.n_tiles, first = blockIdx.x >> 1, step = gridDim.x >> 1;
     constexpr uint32_t IDESC = F8 ? make_idesc(TILE_N, false, false, 2 * TILE_M, 0u) : make_idesc(TILE_N, false, false, 2 * TILE_M, 1u);
 
+    if (F8 && warp < EPI_FIRST / 32) give_registers();
     if (warp == 0) {
         // ---------------------------------------------------------------- copies (both CTAs)
         if (lane == 0) {
@@ -297,10 +326,11 @@ tl_strip_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__
                 while (!mbar_try_wait(drain_bar, 0) && globaltimer_ns() - t0 < p.wait_limit_ns) {}
             }
         }
-    } else {
+    } else if (warp >= EPI_FIRST / 32) {
         // ---------------------------------------------------------------- epilogue (both CTAs)
-        const int quad = warp & 3, half = (warp - 2) >> 2;
-        const int et = threadIdx.x - 64;
+        if (F8) take_registers();
+        const int quad = warp & 3, half = (warp - EPI_FIRST / 32) >> 2;
+        const int et = threadIdx.x - EPI_FIRST;
         const uint32_t tmem_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + half * HALF_N;
         Best best;
         best.top = p.top;
@@ -367,9 +397,16 @@ tl_strip_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__
                 for (int j = 0; j < HALF_N / 2; ++j) acc[j] = 0ull;
                 const float* hs = p.hs + static_cast<size_t>(p.row0 + (row_ok ? row : 0)) * p.kbs;
                 const float* ws = p.ws + static_cast<size_t>(min(p.col0 + c0, p.V - 1) / 128) * p.kbs;
-                float f = __ldg(hs) * __ldg(ws);
+                // factors of the next k-blocks, AHEAD of them under way
+                constexpr int AHEAD = 4;
+                float fh[AHEAD], fw[AHEAD];
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) { fh[i] = i < p.kbs ? __ldg(hs + i) : 0.f; fw[i] = i < p.kbs ? __ldg(ws + i) : 0.f; }
                 for (int kb = 0; kb < p.kbs; ++kb) {
-                    const float next = kb + 1 < p.kbs ? __ldg(hs + kb + 1) * __ldg(ws + kb + 1) : 0.f;
+                    const float f = fh[0] * fw[0];
+#pragma unroll
+                    for (int i = 0; i + 1 < AHEAD; ++i) { fh[i] = fh[i + 1]; fw[i] = fw[i + 1]; }
+                    if (kb + AHEAD < p.kbs) { fh[AHEAD - 1] = __ldg(hs + kb + AHEAD); fw[AHEAD - 1] = __ldg(ws + kb + AHEAD); }
                     const int ab = unit & 1;
                     ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(ab), (unit >> 1) & 1, abort_flag, p.wait_limit_ns));
                     if (!ok) break;
@@ -378,16 +415,15 @@ tl_strip_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__
                     const f2 factor = pair(f, f);
                     __syncwarp();
 #pragma unroll
-                    for (int c = 0; c < HALF_N; c += 32) {
-                        float v[32];
-                        tmem_ld32(from + c, v);
+                    for (int c = 0; c < HALF_N; c += 64) {
+                        float v[64];
+                        tmem_ld64(from + c, v);
                         tmem_ld_wait();
+                        if (c + 64 == HALF_N) release(ab);              // all of it is in registers
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) acc[c / 2 + j] = fma2(pair(v[2 * j], v[2 * j + 1]), factor, acc[c / 2 + j]);
+                        for (int j = 0; j < 32; ++j) acc[c / 2 + j] = fma2(pair(v[2 * j], v[2 * j + 1]), factor, acc[c / 2 + j]);
                     }
                     ++unit;
-                    release(ab);
-                    f = next;
                 }
                 if (!ok) break;
 #pragma unroll
@@ -422,6 +458,7 @@ tl_strip_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__
                 }
             }
         }
+        launch_next();
     }
 
     tc_fence_before();
@@ -443,26 +480,66 @@ struct List {
     int lane, top;
     __device__ __forceinline__ void clear() { val = MINUS_INF; id = INT_MAX; }
     __device__ __forceinline__ static bool better(float a, int ia, float b, int ib) { return a > b || (a == b && ia < ib); }
-    // Every lane offers (x, c) if `has`; what is no better than the last entry is passed over.
-    __device__ __forceinline__ void offer(bool has, float x, int c) {
-        float last = __shfl_sync(0xffffffffu, val, top - 1);
-        int last_id = __shfl_sync(0xffffffffu, id, top - 1);
-        unsigned todo = __ballot_sync(0xffffffffu, has && better(x, c, last, last_id));
-        while (todo) {
-            const int from = __ffs(todo) - 1;
+    __device__ __forceinline__ unsigned todo(bool has, float x, int c) const {
+        const float last = __shfl_sync(0xffffffffu, val, top - 1);
+        const int last_id = __shfl_sync(0xffffffffu, id, top - 1);
+        return __ballot_sync(0xffffffffu, has && better(x, c, last, last_id));
+    }
+    __device__ __forceinline__ void insert(unsigned from_lanes, float x, int c) {
+        while (from_lanes) {
+            const int from = __ffs(from_lanes) - 1;
+            from_lanes &= from_lanes - 1;
             const float nx = __shfl_sync(0xffffffffu, x, from);
             const int nc = __shfl_sync(0xffffffffu, c, from);
             const int at = __popc(__ballot_sync(0xffffffffu, better(val, id, nx, nc)));
             const float up = __shfl_up_sync(0xffffffffu, val, 1);
             const int up_id = __shfl_up_sync(0xffffffffu, id, 1);
             if (lane >= at) { val = lane == at ? nx : up; id = lane == at ? nc : up_id; }
-            last = __shfl_sync(0xffffffffu, val, top - 1);
-            last_id = __shfl_sync(0xffffffffu, id, top - 1);
-            todo &= todo - 1;
-            todo &= __ballot_sync(0xffffffffu, better(x, c, last, last_id));
         }
     }
 };
+// A step of a bitonic network over the warp, for N independent sequences: lanes `mask` apart are put in order.
+template <int N> __device__ __forceinline__ void in_order(float* x, int* c, int mask, bool better_first) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float ox = __shfl_xor_sync(0xffffffffu, x[i], mask);
+        const int oc = __shfl_xor_sync(0xffffffffu, c[i], mask);
+        if (List::better(x[i], c[i], ox, oc) != better_first) { x[i] = ox; c[i] = oc; }
+    }
+}
+// Every lane offers (x[i], c[i]) to list i where bit i of `has` is set.  A few candidates are inserted one after the other (a chain of
+// three dependent exchanges each); more are sorted, all lists' at once, and merged (15 and 6 steps).
+template <int N> __device__ __forceinline__ void offer(List* list, unsigned has, float* x, int* c) {
+    unsigned todo[N];
+    int most = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) { todo[i] = list[i].todo((has >> i) & 1u, x[i], c[i]); most = max(most, __popc(todo[i])); }
+    if (most == 0) return;
+    if (most <= 4) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) list[i].insert(todo[i], x[i], c[i]);
+        return;
+    }
+    const int lane = list[0].lane;
+#pragma unroll
+    for (int i = 0; i < N; ++i) if (!((todo[i] >> lane) & 1u)) { x[i] = MINUS_INF; c[i] = INT_MAX; }
+#pragma unroll
+    for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+        for (int j = k >> 1; j > 0; j >>= 1) in_order<N>(x, c, j, ((lane & j) == 0) == ((lane & k) == 0));
+    // the better half of the list and the turned-round newcomers is a bitonic sequence
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float ox = __shfl_xor_sync(0xffffffffu, x[i], 31);
+        const int oc = __shfl_xor_sync(0xffffffffu, c[i], 31);
+        x[i] = list[i].val; c[i] = list[i].id;
+        if (List::better(ox, oc, x[i], c[i])) { x[i] = ox; c[i] = oc; }
+    }
+#pragma unroll
+    for (int j = 16; j > 0; j >>= 1) in_order<N>(x, c, j, (lane & j) == 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) { list[i].val = x[i]; list[i].id = c[i]; }
+}
 
 // ------------------------------------------------------------------------------------ the kernel for few tokens
 // Up to 64 tokens: bound by reading W once.  W's rows are the products' M side (128 at a time), the tokens their N side (16, 32 or 64),
@@ -470,16 +547,16 @@ struct List {
 // multiple of 32 rows) through a ring of 6 to 8 stages.  The logits of a tile go through shared memory, so that a warp has a token's
 // 128 logits side by side: it keeps the token's state (a lane its own part) and list in registers from tile to tile.
 constexpr int FEW_TOKENS = 64, FEW_ROWS = 32;                       // W's rows per copy
-constexpr int FEW_BUFS = 4;
 template <int NT, bool F8> struct Few {
     static constexpr int STAGES = NT == 64 ? 6 : 8;
+    static constexpr int BUFS = NT == 16 ? 16 : 8;                  // accumulators: 8 bits use one per k-block
     static constexpr int STAGE_BYTES = TILE_M * KB_BYTES + NT * KB_BYTES;
-    static constexpr int BARS = 2 * STAGES + 2 * FEW_BUFS + 1;
+    static constexpr int BARS = 2 * STAGES + 2 * BUFS + 1;
     static constexpr int PITCH = TILE_M + 4;                        // floats between tokens of the logits' tile
     static constexpr int TILE = STAGES * STAGE_BYTES + 512;
     static constexpr int SCALES = TILE + NT * PITCH * 4;            // 8 bits: [k-block][token]
     static constexpr int SMEM_FIXED = 1024 + SCALES;
-    static constexpr int TMEM_COLS = FEW_BUFS * NT;
+    static constexpr int TMEM_COLS = BUFS * NT;
     static_assert(8 * BARS + 16 <= 512 && STAGE_BYTES % 1024 == 0, "layout");
 };
 constexpr int FEW_MAX_KBS = 128;                                    // 8 bits: scales of 64 tokens in 32 KB
@@ -490,7 +567,8 @@ template <int NT, bool F8, bool TOP>
 __global__ void __launch_bounds__(THREADS, 1)
 tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ CUtensorMap tmW, const Params p) {
     using S = Few<NT, F8>;
-    constexpr int STAGES = S::STAGES, KE = F8 ? 128 : 64, HALF = NT / 2, PER_WARP = NT / EPI_WARPS;
+    constexpr int STAGES = S::STAGES, BUFS = S::BUFS, KE = F8 ? 128 : 64, HALF = NT / 2;
+    constexpr int PER_WARP = NT / EPI_WARPS, BATCH = PER_WARP < 4 ? PER_WARP : 4;     // tokens of a warp, at a time
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     uint8_t* const smem = smem_raw + (base - raw);
@@ -498,16 +576,18 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
     auto full_bar = [&](int s) { return bars + 8u * s; };
     auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
     auto tfull_bar = [&](int a) { return bars + 8u * (2 * STAGES + a); };
-    auto tempty_bar = [&](int a) { return bars + 8u * (2 * STAGES + FEW_BUFS + a); };
-    const uint32_t drain_bar = bars + 8u * (2 * STAGES + 2 * FEW_BUFS);
+    auto tempty_bar = [&](int a) { return bars + 8u * (2 * STAGES + BUFS + a); };
+    const uint32_t drain_bar = bars + 8u * (2 * STAGES + 2 * BUFS);
     uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + STAGES * S::STAGE_BYTES + 8 * S::BARS);
     volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    launch_next();
     if (threadIdx.x == 0) {
         *abort_flag = 0;
+        if (blockIdx.x == 0) *p.status = 0;             // only the join, which comes later, sets bits in it
         for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-        for (int a = 0; a < FEW_BUFS; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), EPI_WARPS); }
+        for (int a = 0; a < BUFS; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), EPI_WARPS); }
         mbar_init(drain_bar, 1);
         fence_barrier_init();
         fence_proxy_async();
@@ -570,8 +650,8 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
             int unit = 0;
             for (int r = v0; ok && r < v1; r += TILE_M) {
                 for (int kb = 0; kb < p.kbs; ++kb) {
-                    const int ab = unit % FEW_BUFS;
-                    if ((F8 || kb == 0) && !mbar_wait(tempty_bar(ab), ((unit / FEW_BUFS) & 1) ^ 1u, abort_flag, p.wait_limit_ns)) { ok = false; break; }
+                    const int ab = unit % BUFS;
+                    if ((F8 || kb == 0) && !mbar_wait(tempty_bar(ab), ((unit / BUFS) & 1) ^ 1u, abort_flag, p.wait_limit_ns)) { ok = false; break; }
                     if (!mbar_wait(full_bar(stage), phase, abort_flag, p.wait_limit_ns)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t sa = base + stage * S::STAGE_BYTES, tmem_d = tmem_base + ab * NT;
@@ -593,8 +673,8 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
                 while (!mbar_try_wait(drain_bar, 0) && globaltimer_ns() - t0 < p.wait_limit_ns) {}
             }
         }
-    } else {
-        const int quad = warp & 3, half = (warp - 2) >> 2, ew = warp - 2;
+    } else if (warp >= EPI_FIRST / 32) {
+        const int quad = warp & 3, half = (warp - EPI_FIRST / 32) >> 2, ew = warp - EPI_FIRST / 32;
         const uint32_t tmem_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + half * HALF;
         float* const tile = reinterpret_cast<float*>(smem + S::TILE);
         State s[PER_WARP];
@@ -604,7 +684,7 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
         for (int i = 0; i < PER_WARP; ++i) {
             s[i] = State{MINUS_INF, 0.f, 0.f};
             list[i].lane = lane; list[i].top = p.top; list[i].clear();
-            const int t = ew * PER_WARP + i;
+            const int t = i * EPI_WARPS + ew;
             token[i] = p.tokens && t < p.rows ? p.tokens[t] : -1;
         }
         auto load_half = [&](uint32_t at, float* v) {
@@ -626,11 +706,11 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
 #pragma unroll
             for (int j = 0; j < HALF; ++j) acc[j] = 0.f;
             auto wait = [&](int ab) {
-                if (ok) ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(ab), (unit / FEW_BUFS) & 1, abort_flag, p.wait_limit_ns));
+                if (ok) ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(ab), (unit / BUFS) & 1, abort_flag, p.wait_limit_ns));
                 return ok;
             };
             if constexpr (!F8) {
-                const int ab = unit % FEW_BUFS;
+                const int ab = unit % BUFS;
                 if (wait(ab)) {
                     tc_fence_after();
                     load_half(tmem_row + ab * NT, acc);
@@ -642,7 +722,7 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
                 float f = __ldg(ws);
                 for (int kb = 0; kb < p.kbs; ++kb) {
                     const float next = kb + 1 < p.kbs ? __ldg(ws + kb + 1) : 0.f;
-                    const int ab = unit % FEW_BUFS;
+                    const int ab = unit % BUFS;
                     if (!wait(ab)) break;
                     tc_fence_after();
                     float v[HALF];
@@ -665,35 +745,47 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
             for (int j = 0; j < HALF; ++j) tile[(half * HALF + j) * S::PITCH + quad * 32 + lane] = acc[j];
             epi_sync();
 #pragma unroll
-            for (int i = 0; i < PER_WARP; ++i) {
-                const int t = ew * PER_WARP + i;
-                if (t < p.rows) {
-                    float x[4];
-                    float m = s[i].m;
+            for (int i0 = 0; i0 < PER_WARP; i0 += BATCH) {
+                if (i0 * EPI_WARPS + ew >= p.rows) break;
+                float x[4][BATCH];
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) x[q][i] = tile[((i0 + i) * EPI_WARPS + ew) * S::PITCH + 32 * q + lane];
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    State& st = s[i0 + i];
+                    float m = st.m;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        x[q] = tile[t * S::PITCH + 32 * q + lane];
                         const int c = r + 32 * q + lane;
                         if (c < v1) {
-                            m = fmaxf(m, x[q]);
-                            if (p.col0 + c == token[i]) p.chosen[t] = x[q];
+                            m = fmaxf(m, x[q][i]);
+                            if (p.col0 + c == token[i0 + i]) p.chosen[(i0 + i) * EPI_WARPS + ew] = x[q][i];
                         }
                     }
-                    move(s[i], m, p.scale);
+                    move(st, m, p.scale);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         if (r + 32 * q + lane < v1) {
-                            const float d = (x[q] - m) * p.scale, e = ex2f(d);
-                            s[i].z += e;
-                            s[i].u = fmaf(d, e, s[i].u);
+                            const float d = (x[q][i] - m) * p.scale, e = ex2f(d);
+                            st.z += e;
+                            st.u = fmaf(d, e, st.u);
                         }
                     }
-                    if (TOP) {
+                }
+                if (TOP) {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int c = r + 32 * q + lane;
-                            list[i].offer(c < v1, x[q], p.col0 + c);
+                    for (int q = 0; q < 4; ++q) {
+                        const int c = r + 32 * q + lane;
+                        unsigned has = 0;
+                        int id[BATCH];
+#pragma unroll
+                        for (int i = 0; i < BATCH; ++i) {
+                            id[i] = p.col0 + c;
+                            if (c < v1 && (i0 + i) * EPI_WARPS + ew < p.rows) has |= 1u << i;
                         }
+                        offer<BATCH>(list + i0, has, x[q], id);
                     }
                 }
             }
@@ -703,7 +795,7 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
         if (ok) {
 #pragma unroll
             for (int i = 0; i < PER_WARP; ++i) {
-                const int t = ew * PER_WARP + i;
+                const int t = i * EPI_WARPS + ew;
                 if (t < p.rows) {
                     float m = s[i].m;
 #pragma unroll
@@ -726,7 +818,9 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
 
     tc_fence_before();
     __syncthreads();
-    if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, VPCE_DEV_WAIT_EXPIRED);
+    if (*abort_flag)                                                    // the join says so in the status word
+        for (int t = threadIdx.x; t < p.rows; t += THREADS)
+            p.part[static_cast<size_t>(t) * p.slices + blockIdx.x] = make_float4(MINUS_INF, 0.f, 0.f, __int_as_float(-1));
     if (warp == 1) {
         __syncwarp();
         tc_fence_after();
@@ -752,10 +846,13 @@ struct JoinParams {
 };
 
 constexpr int JOIN_THREADS = 128;
-// A warp per token, its lanes over the slices, 32 at a time, always in the same order.
-template <bool TOP>
+// A warp per token, its lanes over the slices, 128 at a time, always in the same order.
+// FEW: the slices of the kernel for few tokens, whose lists are sorted, so that the search ends at the first rank at which no slice
+// has anything to offer.
+template <bool TOP, bool FEW>
 __global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams p) {
     const int row = blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    wait_for_last();
     if (row >= p.rows) return;
     State s{MINUS_INF, 0.f, 0.f};
     List list;
@@ -771,26 +868,53 @@ __global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams 
     }
     const float4* part = p.part + static_cast<size_t>(row) * p.slices;
     const uint2* cand = p.cand + static_cast<size_t>(row) * p.slices * (TOP ? p.top : 0);
-    for (int i0 = 0; i0 < p.slices; i0 += 32) {
-        const int i = i0 + lane;
-        float4 q = make_float4(MINUS_INF, 0.f, 0.f, 0.f);
-        if (i < p.slices) q = part[i];
-        State o{q.x, q.y, q.z};
-        const float m = fmaxf(s.m, o.m);
-        move(s, m, p.scale);
-        move(o, m, p.scale);
-        s.z += o.z;
-        s.u += o.u;
+    constexpr int UNROLL = FEW ? 5 : 4;                             // 5 x 32 lanes: all slices of the kernel for few tokens
+    bool expired = false;
+    for (int i0 = 0; i0 < p.slices; i0 += 32 * UNROLL) {
+        float4 q[UNROLL];
+#pragma unroll
+        for (int k = 0; k < UNROLL; ++k) {
+            const int i = i0 + 32 * k + lane;
+            q[k] = i < p.slices ? part[i] : make_float4(MINUS_INF, 0.f, 0.f, 0.f);
+        }
+        int n[UNROLL], most = 0;
+#pragma unroll
+        for (int k = 0; k < UNROLL; ++k) {
+            State o{q[k].x, q[k].y, q[k].z};
+            const float m = fmaxf(s.m, o.m);
+            move(s, m, p.scale);
+            move(o, m, p.scale);
+            s.z += o.z;
+            s.u += o.u;
+            n[k] = __float_as_int(q[k].w);
+            expired = expired || n[k] < 0;
+            most = max(most, n[k]);
+        }
         if (TOP) {
-            const int n = i < p.slices ? __float_as_int(q.w) : 0;
-            const int most = __reduce_max_sync(0xffffffffu, n);
+            most = __reduce_max_sync(0xffffffffu, most);
+            uint2 next[UNROLL];
+            auto load = [&](int j) {
+#pragma unroll
+                for (int k = 0; k < UNROLL; ++k) if (j < n[k]) next[k] = cand[static_cast<size_t>(i0 + 32 * k + lane) * p.top + j];
+            };
+            load(0);
             for (int j = 0; j < most; ++j) {
-                uint2 e = make_uint2(0u, 0u);
-                if (j < n) e = cand[static_cast<size_t>(i) * p.top + j];
-                list.offer(j < n, __uint_as_float(e.x), static_cast<int>(e.y));
+                float x[UNROLL];
+                int c[UNROLL];
+#pragma unroll
+                for (int k = 0; k < UNROLL; ++k) { x[k] = __uint_as_float(next[k].x); c[k] = static_cast<int>(next[k].y); }
+                load(j + 1);
+                unsigned any = 0;
+#pragma unroll
+                for (int k = 0; k < UNROLL; ++k) {
+                    any |= list.todo(j < n[k], x[k], c[k]);
+                    offer<1>(&list, j < n[k] ? 1u : 0u, x + k, c + k);
+                }
+                if (FEW && any == 0) break;
             }
         }
     }
+    if (FEW && __any_sync(0xffffffffu, expired) && lane == 0) atomicOr(p.status, VPCE_DEV_WAIT_EXPIRED);
     // over the lanes
     float m = s.m;
 #pragma unroll
