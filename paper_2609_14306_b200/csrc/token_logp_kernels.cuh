@@ -513,8 +513,28 @@ template <int N> __device__ __forceinline__ void in_order(float* x, int* c, int 
         if (List::better(x[i], c[i], ox, oc) != better_first) { x[i] = ox; c[i] = oc; }
     }
 }
+// Merges a warp's 32 candidates into each list: sorts them (15 steps), then the better half of the list and the turned-round newcomers
+// is a bitonic sequence (6 steps).
+template <int N> __device__ __forceinline__ void sort_in(List* list, float* x, int* c) {
+    const int lane = list[0].lane;
+#pragma unroll
+    for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+        for (int j = k >> 1; j > 0; j >>= 1) in_order<N>(x, c, j, ((lane & j) == 0) == ((lane & k) == 0));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float ox = __shfl_xor_sync(0xffffffffu, x[i], 31);
+        const int oc = __shfl_xor_sync(0xffffffffu, c[i], 31);
+        x[i] = list[i].val; c[i] = list[i].id;
+        if (List::better(ox, oc, x[i], c[i])) { x[i] = ox; c[i] = oc; }
+    }
+#pragma unroll
+    for (int j = 16; j > 0; j >>= 1) in_order<N>(x, c, j, (lane & j) == 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) { list[i].val = x[i]; list[i].id = c[i]; }
+}
 // Every lane offers (x[i], c[i]) to list i where bit i of `has` is set.  A few candidates are inserted one after the other (a chain of
-// three dependent exchanges each); more are sorted, all lists' at once, and merged (15 and 6 steps).
+// three dependent exchanges each); more are sorted and merged, all lists' at once.
 template <int N> __device__ __forceinline__ void offer(List* list, unsigned has, float* x, int* c) {
     unsigned todo[N];
     int most = 0;
@@ -529,22 +549,102 @@ template <int N> __device__ __forceinline__ void offer(List* list, unsigned has,
     const int lane = list[0].lane;
 #pragma unroll
     for (int i = 0; i < N; ++i) if (!((todo[i] >> lane) & 1u)) { x[i] = MINUS_INF; c[i] = INT_MAX; }
+    sort_in<N>(list, x, c);
+}
+
+// The same for 128 columns c0 ... of which the first `valid` exist, lane l holding column c0 + 32 q + l of list i in x[q][i].
+// What may matter is told by a bound from below, the list's last entry or, while the list is young, the top-th largest of the lanes'
+// maxima; the candidates above it (about as many as the list is long in the first tile, few later on) are brought together through
+// `scratch` (64 floats of shared memory for each list, `pitch` apart), sorted and merged at once.
+template <int N> __device__ __forceinline__ void offer_tile(List* list, unsigned has, float (*x)[N], int c0, int valid, float* scratch, int pitch) {
+    const int lane = list[0].lane, top = list[0].top;
+    float bound[N];
+    unsigned left[N][4];                                            // candidates not yet taken, by quarter
+    int most = 0;
+    auto filter = [&](bool again) {
+        most = 0;
 #pragma unroll
-    for (int k = 2; k <= 32; k <<= 1)
+        for (int i = 0; i < N; ++i) {
+            const float last = __shfl_sync(0xffffffffu, list[i].val, top - 1);
+            const int last_id = __shfl_sync(0xffffffffu, list[i].id, top - 1);
+            int n = 0;
 #pragma unroll
-        for (int j = k >> 1; j > 0; j >>= 1) in_order<N>(x, c, j, ((lane & j) == 0) == ((lane & k) == 0));
-    // the better half of the list and the turned-round newcomers is a bitonic sequence
+            for (int q = 0; q < 4; ++q) {
+                const int c = c0 + 32 * q + lane;
+                const bool in = ((has >> i) & 1u) && 32 * q + lane < valid && x[q][i] >= bound[i] && List::better(x[q][i], c, last, last_id);
+                const unsigned now = __ballot_sync(0xffffffffu, in);
+                left[i][q] = again ? left[i][q] & now : now;
+                n += __popc(left[i][q]);
+            }
+            most = max(most, n);
+        }
+    };
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float ox = __shfl_xor_sync(0xffffffffu, x[i], 31);
-        const int oc = __shfl_xor_sync(0xffffffffu, c[i], 31);
-        x[i] = list[i].val; c[i] = list[i].id;
-        if (List::better(ox, oc, x[i], c[i])) { x[i] = ox; c[i] = oc; }
+    for (int i = 0; i < N; ++i) bound[i] = MINUS_INF;
+    filter(false);
+    if (most > 32) {
+        float m[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            m[i] = MINUS_INF;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) if (32 * q + lane < valid) m[i] = fmaxf(m[i], x[q][i]);
+        }
+#pragma unroll
+        for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+            for (int j = k >> 1; j > 0; j >>= 1) {
+                const bool larger = ((lane & j) == 0) == ((lane & k) == 0);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float o = __shfl_xor_sync(0xffffffffu, m[i], j);
+                    m[i] = larger ? fmaxf(m[i], o) : fminf(m[i], o);
+                }
+            }
+#pragma unroll
+        for (int i = 0; i < N; ++i) bound[i] = __shfl_sync(0xffffffffu, m[i], top - 1);
+        filter(false);
     }
+    while (most > 0) {
+        if (most <= 4) {
 #pragma unroll
-    for (int j = 16; j > 0; j >>= 1) in_order<N>(x, c, j, (lane & j) == 0);
+            for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int i = 0; i < N; ++i) { list[i].val = x[i]; list[i].id = c[i]; }
+                for (int q = 0; q < 4; ++q) list[i].insert(left[i][q], x[q][i], c0 + 32 * q + lane);
+            return;
+        }
+        // up to 32 of each list's candidates, lane by lane
+        const unsigned before = (1u << lane) - 1u;
+        float y[N];
+        int c[N];
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            int rank = 0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int mine = rank + __popc(left[i][q] & before);
+                rank += __popc(left[i][q]);
+                const bool goes = ((left[i][q] >> lane) & 1u) && mine < 32;
+                if (goes) {
+                    scratch[i * pitch + mine] = x[q][i];
+                    scratch[i * pitch + 32 + mine] = __int_as_float(c0 + 32 * q + lane);
+                }
+                left[i][q] &= ~__ballot_sync(0xffffffffu, goes);
+            }
+            y[i] = rank;                                            // how many there were
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const bool some = lane < static_cast<int>(y[i]);
+            y[i] = some ? scratch[i * pitch + lane] : MINUS_INF;
+            c[i] = some ? __float_as_int(scratch[i * pitch + 32 + lane]) : INT_MAX;
+        }
+        sort_in<N>(list, y, c);
+        if (most <= 32) return;
+        filter(true);
+    }
 }
 
 // ------------------------------------------------------------------------------------ the kernel for few tokens
@@ -725,9 +825,18 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
                 }
             } else {
                 const float* ws = p.ws + static_cast<size_t>(min(p.col0 + r + quad * 32 + lane, p.V - 1) / 128) * p.kbs;
-                float f = __ldg(ws);
+                constexpr int AHEAD = 4;                                // factors of the next k-blocks, under way
+                float fw[AHEAD];
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) fw[i] = i < p.kbs ? __ldg(ws + i) : 0.f;
+                f2 sum[HALF / 2];
+#pragma unroll
+                for (int j = 0; j < HALF / 2; ++j) sum[j] = 0ull;
                 for (int kb = 0; kb < p.kbs; ++kb) {
-                    const float next = kb + 1 < p.kbs ? __ldg(ws + kb + 1) : 0.f;
+                    const f2 f = pair(fw[0], fw[0]);
+#pragma unroll
+                    for (int i = 0; i + 1 < AHEAD; ++i) fw[i] = fw[i + 1];
+                    if (kb + AHEAD < p.kbs) fw[AHEAD - 1] = __ldg(ws + kb + AHEAD);
                     const int ab = unit % BUFS;
                     if (!wait(ab)) break;
                     tc_fence_after();
@@ -739,13 +848,12 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
 #pragma unroll
                     for (int j = 0; j < HALF / 4; ++j) {
                         const float4 h = hs[j];
-                        acc[4 * j] = fmaf(v[4 * j], f * h.x, acc[4 * j]);
-                        acc[4 * j + 1] = fmaf(v[4 * j + 1], f * h.y, acc[4 * j + 1]);
-                        acc[4 * j + 2] = fmaf(v[4 * j + 2], f * h.z, acc[4 * j + 2]);
-                        acc[4 * j + 3] = fmaf(v[4 * j + 3], f * h.w, acc[4 * j + 3]);
+                        sum[2 * j] = fma2(pair(v[4 * j], v[4 * j + 1]), mul2(f, pair(h.x, h.y)), sum[2 * j]);
+                        sum[2 * j + 1] = fma2(pair(v[4 * j + 2], v[4 * j + 3]), mul2(f, pair(h.z, h.w)), sum[2 * j + 1]);
                     }
-                    f = next;
                 }
+#pragma unroll
+                for (int j = 0; j < HALF / 2; ++j) { const float2 t = split(sum[j]); acc[2 * j] = t.x; acc[2 * j + 1] = t.y; }
             }
 #pragma unroll
             for (int j = 0; j < HALF; ++j) tile[(half * HALF + j) * S::PITCH + quad * 32 + lane] = acc[j];
@@ -781,18 +889,10 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
                     }
                 }
                 if (TOP) {
+                    unsigned has = 0;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int c = r + 32 * q + lane;
-                        unsigned has = 0;
-                        int id[BATCH];
-#pragma unroll
-                        for (int i = 0; i < BATCH; ++i) {
-                            id[i] = p.col0 + c;
-                            if (c < v1 && (i0 + i) * EPI_WARPS + ew < p.rows) has |= 1u << i;
-                        }
-                        offer<BATCH>(list + i0, has, x[q], id);
-                    }
+                    for (int i = 0; i < BATCH; ++i) if ((i0 + i) * EPI_WARPS + ew < p.rows) has |= 1u << i;
+                    offer_tile<BATCH>(list + i0, has, x, p.col0 + r, v1 - r, tile + (i0 * EPI_WARPS + ew) * S::PITCH, EPI_WARPS * S::PITCH);
                 }
             }
             epi_sync();                                                 // the tile may be written again
