@@ -61,7 +61,7 @@ bool plan(int64_t T, int64_t d, int64_t V, int top, int d_unit, int64_t d_most, 
     p->floor = off;    off = up(off + sizeof(unsigned) * p->chunk);
     p->chosen = off;   off = up(off + sizeof(float) * p->chunk);
     p->run = off;      off = up(off + sizeof(float4) * p->chunk);
-    p->run_list = off; off = up(off + sizeof(uint2) * p->chunk * top);
+    p->run_list = off; off = up(off + sizeof(Key) * p->chunk * top);
     p->part = off;     off = up(off + sizeof(float4) * p->chunk * p->slices);
     p->cand = off;     off = up(off + sizeof(uint2) * p->chunk * p->slices * top);
     p->total = off;
@@ -130,7 +130,7 @@ template <int NT, bool F8, bool TOP> cudaError_t launch_few(const CUtensorMap& h
     auto kern = tl_few_kernel<NT, F8, TOP>;
     static std::atomic<bool> done[64];
     if (cudaError_t e = raise_smem(kern, done); e != cudaSuccess) return e;
-    kern<<<p.slices, THREADS, Few<NT, F8>::SMEM_FIXED + (F8 ? NT * p.kbs * 4 : 0), st>>>(h, w, p);
+    kern<<<p.slices, Few<NT, F8>::THREADS, Few<NT, F8>::SMEM_FIXED + (F8 ? NT * p.kbs * 4 : 0), st>>>(h, w, p);
     return cudaGetLastError();
 }
 template <bool F8, bool TOP> cudaError_t launch_few(int nt, const CUtensorMap& h, const CUtensorMap& w, const Params& p, cudaStream_t st) {
@@ -196,7 +196,7 @@ int forward(const void* H, const float* Hs, const void* W, const float* Ws, cons
     j.slices = pl.slices; j.top = top; j.scale = p.scale; j.inv_temp = static_cast<float>(1.0 / temperature);
     j.part = p.part; j.cand = p.cand; j.floor = p.floor; j.chosen = p.chosen;
     j.run = reinterpret_cast<float4*>(ws + pl.run);
-    j.run_list = reinterpret_cast<uint2*>(ws + pl.run_list);
+    j.run_list = reinterpret_cast<Key*>(ws + pl.run_list);
     j.ignore_index = ignore_index; j.V = p.V; j.status = p.status;
 
     for (int64_t t0 = 0; t0 < T; t0 += pl.chunk) {

@@ -8,8 +8,6 @@
 // Then lse = m / temperature + ln z and the entropy is ln z - ln 2 u / z: no difference of large numbers anywhere.
 #pragma once
 
-#include <climits>
-
 #include "sm100_ptx.cuh"
 #include "vp_ce.h"
 
@@ -479,100 +477,84 @@ tl_strip_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__
 }
 
 // ------------------------------------------------------------------------------------ a token's list, held by one warp
-// Lane j has the (j + 1)-th best entry, larger logits first, among equals the lower column.
+// A logit with its column as one number, the better the larger: larger logits first, among equals the lower column.  0: nothing.
+using Key = unsigned long long;
+__device__ __forceinline__ Key key_of(float x, int c) {
+    return static_cast<Key>(ordered(x + 0.f)) << 32 | static_cast<unsigned>(~c);            // + 0: a zero is a zero
+}
+__device__ __forceinline__ float logit_of(Key k) { return from_ordered(static_cast<unsigned>(k >> 32)); }
+__device__ __forceinline__ int column_of(Key k) { return static_cast<int>(~static_cast<unsigned>(k)); }
+
+// Lane j has the (j + 1)-th best entry.
 struct List {
-    float val;
-    int id;
+    Key key;
     int lane, top;
-    __device__ __forceinline__ void clear() { val = MINUS_INF; id = INT_MAX; }
-    __device__ __forceinline__ static bool better(float a, int ia, float b, int ib) { return a > b || (a == b && ia < ib); }
-    __device__ __forceinline__ unsigned todo(bool has, float x, int c) const {
-        const float last = __shfl_sync(0xffffffffu, val, top - 1);
-        const int last_id = __shfl_sync(0xffffffffu, id, top - 1);
-        return __ballot_sync(0xffffffffu, has && better(x, c, last, last_id));
-    }
-    __device__ __forceinline__ void insert(unsigned from_lanes, float x, int c) {
+    __device__ __forceinline__ Key last() const { return __shfl_sync(0xffffffffu, key, top - 1); }
+    // Takes the candidates of the given lanes, one after the other: a chain of three dependent exchanges each.
+    __device__ __forceinline__ void insert(unsigned from_lanes, Key k) {
         while (from_lanes) {
             const int from = __ffs(from_lanes) - 1;
             from_lanes &= from_lanes - 1;
-            const float nx = __shfl_sync(0xffffffffu, x, from);
-            const int nc = __shfl_sync(0xffffffffu, c, from);
-            const int at = __popc(__ballot_sync(0xffffffffu, better(val, id, nx, nc)));
-            const float up = __shfl_up_sync(0xffffffffu, val, 1);
-            const int up_id = __shfl_up_sync(0xffffffffu, id, 1);
-            if (lane >= at) { val = lane == at ? nx : up; id = lane == at ? nc : up_id; }
+            const Key now = __shfl_sync(0xffffffffu, k, from);
+            const int at = __popc(__ballot_sync(0xffffffffu, key > now));
+            const Key up = __shfl_up_sync(0xffffffffu, key, 1);
+            if (lane >= at) key = lane == at ? now : up;
         }
     }
 };
 // A step of a bitonic network over the warp, for N independent sequences: lanes `mask` apart are put in order.
-template <int N> __device__ __forceinline__ void in_order(float* x, int* c, int mask, bool better_first) {
+template <int N> __device__ __forceinline__ void in_order(Key* k, int mask, bool better_first) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float ox = __shfl_xor_sync(0xffffffffu, x[i], mask);
-        const int oc = __shfl_xor_sync(0xffffffffu, c[i], mask);
-        if (List::better(x[i], c[i], ox, oc) != better_first) { x[i] = ox; c[i] = oc; }
+        const Key o = __shfl_xor_sync(0xffffffffu, k[i], mask);
+        if ((k[i] > o) != better_first) k[i] = o;
     }
 }
 // Merges a warp's 32 candidates into each list: sorts them (15 steps), then the better half of the list and the turned-round newcomers
 // is a bitonic sequence (6 steps).
-template <int N> __device__ __forceinline__ void sort_in(List* list, float* x, int* c) {
+template <int N> __device__ __forceinline__ void sort_in(List* list, Key* k) {
     const int lane = list[0].lane;
 #pragma unroll
-    for (int k = 2; k <= 32; k <<= 1)
+    for (int w = 2; w <= 32; w <<= 1)
 #pragma unroll
-        for (int j = k >> 1; j > 0; j >>= 1) in_order<N>(x, c, j, ((lane & j) == 0) == ((lane & k) == 0));
+        for (int j = w >> 1; j > 0; j >>= 1) in_order<N>(k, j, ((lane & j) == 0) == ((lane & w) == 0));
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float ox = __shfl_xor_sync(0xffffffffu, x[i], 31);
-        const int oc = __shfl_xor_sync(0xffffffffu, c[i], 31);
-        x[i] = list[i].val; c[i] = list[i].id;
-        if (List::better(ox, oc, x[i], c[i])) { x[i] = ox; c[i] = oc; }
+        const Key o = __shfl_xor_sync(0xffffffffu, k[i], 31);
+        k[i] = o > list[i].key ? o : list[i].key;
     }
 #pragma unroll
-    for (int j = 16; j > 0; j >>= 1) in_order<N>(x, c, j, (lane & j) == 0);
+    for (int j = 16; j > 0; j >>= 1) in_order<N>(k, j, (lane & j) == 0);
 #pragma unroll
-    for (int i = 0; i < N; ++i) { list[i].val = x[i]; list[i].id = c[i]; }
+    for (int i = 0; i < N; ++i) list[i].key = k[i];
 }
-// Every lane offers (x[i], c[i]) to list i where bit i of `has` is set.  A few candidates are inserted one after the other (a chain of
-// three dependent exchanges each); more are sorted and merged, all lists' at once.
-template <int N> __device__ __forceinline__ void offer(List* list, unsigned has, float* x, int* c) {
-    unsigned todo[N];
-    int most = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) { todo[i] = list[i].todo((has >> i) & 1u, x[i], c[i]); most = max(most, __popc(todo[i])); }
-    if (most == 0) return;
-    if (most <= 4) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) list[i].insert(todo[i], x[i], c[i]);
-        return;
-    }
-    const int lane = list[0].lane;
-#pragma unroll
-    for (int i = 0; i < N; ++i) if (!((todo[i] >> lane) & 1u)) { x[i] = MINUS_INF; c[i] = INT_MAX; }
-    sort_in<N>(list, x, c);
+// Every lane offers a key (0: none); a few are inserted, more sorted and merged.  Returns whether there were any.
+__device__ __forceinline__ bool offer(List& list, Key k) {
+    const unsigned todo = __ballot_sync(0xffffffffu, k > list.last());
+    if (todo == 0) return false;
+    if (__popc(todo) <= 4) list.insert(todo, k);
+    else sort_in<1>(&list, &k);
+    return true;
 }
 
-// The same for 128 columns c0 ... of which the first `valid` exist, lane l holding column c0 + 32 q + l of list i in x[q][i].
-// What may matter is told by a bound from below, the list's last entry or, while the list is young, the top-th largest of the lanes'
-// maxima; the candidates above it (about as many as the list is long in the first tile, few later on) are brought together through
-// `scratch` (64 floats of shared memory for each list, `pitch` apart), sorted and merged at once.
+// Offers N lists 128 columns c0 ... each, of which the first `valid` exist, lane l holding column c0 + 32 q + l of list i in x[q][i];
+// all columns are above those of earlier calls.  What may matter is told by a bound from below: the list's last entry or, while the
+// list is young, the top-th largest of the lanes' maxima.  The candidates above it (about as many as the list is long in the first
+// tile, few later on) are brought together through `scratch` (64 floats of shared memory for each list, `pitch` apart) and merged at
+// once.
 template <int N> __device__ __forceinline__ void offer_tile(List* list, unsigned has, float (*x)[N], int c0, int valid, float* scratch, int pitch) {
     const int lane = list[0].lane, top = list[0].top;
-    float bound[N];
+    float above[N];
     unsigned left[N][4];                                            // candidates not yet taken, by quarter
     int most = 0;
     auto filter = [&](bool again) {
         most = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float last = __shfl_sync(0xffffffffu, list[i].val, top - 1);
-            const int last_id = __shfl_sync(0xffffffffu, list[i].id, top - 1);
             int n = 0;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int c = c0 + 32 * q + lane;
-                const bool in = ((has >> i) & 1u) && 32 * q + lane < valid && x[q][i] >= bound[i] && List::better(x[q][i], c, last, last_id);
-                const unsigned now = __ballot_sync(0xffffffffu, in);
+                const unsigned now = __ballot_sync(0xffffffffu, ((has >> i) & 1u) && 32 * q + lane < valid && x[q][i] > above[i]);
                 left[i][q] = again ? left[i][q] & now : now;
                 n += __popc(left[i][q]);
             }
@@ -580,7 +562,7 @@ template <int N> __device__ __forceinline__ void offer_tile(List* list, unsigned
         }
     };
 #pragma unroll
-    for (int i = 0; i < N; ++i) bound[i] = MINUS_INF;
+    for (int i = 0; i < N; ++i) above[i] = logit_of(list[i].last());
     filter(false);
     if (most > 32) {
         float m[N];
@@ -602,7 +584,7 @@ template <int N> __device__ __forceinline__ void offer_tile(List* list, unsigned
                 }
             }
 #pragma unroll
-        for (int i = 0; i < N; ++i) bound[i] = __shfl_sync(0xffffffffu, m[i], top - 1);
+        for (int i = 0; i < N; ++i) above[i] = fmaxf(above[i], below(__shfl_sync(0xffffffffu, m[i], top - 1)));
         filter(false);
     }
     while (most > 0) {
@@ -610,21 +592,20 @@ template <int N> __device__ __forceinline__ void offer_tile(List* list, unsigned
 #pragma unroll
             for (int i = 0; i < N; ++i)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) list[i].insert(left[i][q], x[q][i], c0 + 32 * q + lane);
+                for (int q = 0; q < 4; ++q) list[i].insert(left[i][q], key_of(x[q][i], c0 + 32 * q + lane));
             return;
         }
         // up to 32 of each list's candidates, lane by lane
         const unsigned before = (1u << lane) - 1u;
-        float y[N];
-        int c[N];
+        int n[N];
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            int rank = 0;
+            n[i] = 0;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int mine = rank + __popc(left[i][q] & before);
-                rank += __popc(left[i][q]);
+                const int mine = n[i] + __popc(left[i][q] & before);
+                n[i] += __popc(left[i][q]);
                 const bool goes = ((left[i][q] >> lane) & 1u) && mine < 32;
                 if (goes) {
                     scratch[i * pitch + mine] = x[q][i];
@@ -632,17 +613,16 @@ template <int N> __device__ __forceinline__ void offer_tile(List* list, unsigned
                 }
                 left[i][q] &= ~__ballot_sync(0xffffffffu, goes);
             }
-            y[i] = rank;                                            // how many there were
         }
         __syncwarp();
+        Key k[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const bool some = lane < static_cast<int>(y[i]);
-            y[i] = some ? scratch[i * pitch + lane] : MINUS_INF;
-            c[i] = some ? __float_as_int(scratch[i * pitch + 32 + lane]) : INT_MAX;
-        }
-        sort_in<N>(list, y, c);
+        for (int i = 0; i < N; ++i)
+            k[i] = lane < n[i] ? key_of(scratch[i * pitch + lane], __float_as_int(scratch[i * pitch + 32 + lane])) : 0ull;
+        sort_in<N>(list, k);
         if (most <= 32) return;
+#pragma unroll
+        for (int i = 0; i < N; ++i) above[i] = logit_of(list[i].last());
         filter(true);
     }
 }
@@ -656,6 +636,8 @@ constexpr int FEW_TOKENS = 64, FEW_ROWS = 32;                       // W's rows 
 template <int NT, bool F8> struct Few {
     static constexpr int STAGES = NT == 64 ? 6 : 8;
     static constexpr int BUFS = NT == 16 ? 16 : 8;                  // accumulators: 8 bits use one per k-block
+    static constexpr int WARPS = NT == 16 ? 8 : 16;                 // of the epilogue; more of them hide the lists' exchanges
+    static constexpr int THREADS = EPI_FIRST + 32 * WARPS;
     static constexpr int STAGE_BYTES = TILE_M * KB_BYTES + NT * KB_BYTES;
     static constexpr int BARS = 2 * STAGES + 2 * BUFS + 1;
     static constexpr int PITCH = TILE_M + 4;                        // floats between tokens of the logits' tile
@@ -667,14 +649,12 @@ template <int NT, bool F8> struct Few {
 };
 constexpr int FEW_MAX_KBS = 128;                                    // 8 bits: scales of 64 tokens in 32 KB
 
-__device__ __forceinline__ void epi_sync() { asm volatile("bar.sync 1, %0;" ::"n"(EPI_THREADS) : "memory"); }
-
 template <int NT, bool F8, bool TOP>
-__global__ void __launch_bounds__(THREADS, 1)
+__global__ void __launch_bounds__(Few<NT, F8>::THREADS, 1)
 tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ CUtensorMap tmW, const Params p) {
     using S = Few<NT, F8>;
-    constexpr int STAGES = S::STAGES, BUFS = S::BUFS, KE = F8 ? 128 : 64, HALF = NT / 2;
-    constexpr int PER_WARP = NT / EPI_WARPS, BATCH = PER_WARP < 4 ? PER_WARP : 4;     // tokens of a warp, at a time
+    constexpr int STAGES = S::STAGES, BUFS = S::BUFS, KE = F8 ? 128 : 64, WARPS = S::WARPS;
+    constexpr int PART = NT / (WARPS / 4), PER_WARP = NT / WARPS;   // columns that a warp reads of an accumulator, tokens of a warp
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     uint8_t* const smem = smem_raw + (base - raw);
@@ -693,7 +673,7 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
         *abort_flag = 0;
         if (blockIdx.x == 0) *p.status = 0;             // only the join, which comes later, sets bits in it
         for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-        for (int a = 0; a < BUFS; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), EPI_WARPS); }
+        for (int a = 0; a < BUFS; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), WARPS); }
         mbar_init(drain_bar, 1);
         fence_barrier_init();
         fence_proxy_async();
@@ -706,7 +686,7 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
     }
     float* const scales = reinterpret_cast<float*>(smem + S::SCALES);
     if (F8)
-        for (int i = threadIdx.x; i < NT * p.kbs; i += THREADS) {
+        for (int i = threadIdx.x; i < NT * p.kbs; i += S::THREADS) {
             const int kb = i / NT, t = i - kb * NT;
             scales[i] = t < p.rows ? p.hs[static_cast<size_t>(p.row0 + t) * p.kbs + kb] : 0.f;
         }
@@ -780,8 +760,9 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
             }
         }
     } else if (warp >= EPI_FIRST / 32) {
-        const int quad = warp & 3, half = (warp - EPI_FIRST / 32) >> 2, ew = warp - EPI_FIRST / 32;
-        const uint32_t tmem_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + half * HALF;
+        const int quad = warp & 3, ew = warp - EPI_FIRST / 32, col = (ew >> 2) * PART;
+        auto epi_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory"); };
+        const uint32_t tmem_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + col;
         float* const tile = reinterpret_cast<float*>(smem + S::TILE);
         State s[PER_WARP];
         List list[PER_WARP];
@@ -789,14 +770,13 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
 #pragma unroll
         for (int i = 0; i < PER_WARP; ++i) {
             s[i] = State{MINUS_INF, 0.f, 0.f};
-            list[i].lane = lane; list[i].top = p.top; list[i].clear();
-            const int t = i * EPI_WARPS + ew;
+            list[i].lane = lane; list[i].top = p.top; list[i].key = 0ull;
+            const int t = i * WARPS + ew;
             token[i] = p.tokens && t < p.rows ? p.tokens[t] : -1;
         }
-        auto load_half = [&](uint32_t at, float* v) {
-            if constexpr (HALF == 8) tmem_ld8(at, v);
-            else if constexpr (HALF == 16) tmem_ld16(at, v);
-            else tmem_ld32(at, v);
+        auto load_part = [&](uint32_t at, float* v) {
+            if constexpr (PART == 8) tmem_ld8(at, v);
+            else tmem_ld16(at, v);
             tmem_ld_wait();
         };
         auto release = [&](int ab) {
@@ -808,9 +788,9 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
         int unit = 0;
         // A warp whose wait has run out goes on through the barriers with the others, without waiting or reading.
         for (int r = v0; r < v1; r += TILE_M) {
-            float acc[HALF];
+            float acc[PART];
 #pragma unroll
-            for (int j = 0; j < HALF; ++j) acc[j] = 0.f;
+            for (int j = 0; j < PART; ++j) acc[j] = 0.f;
             auto wait = [&](int ab) {
                 if (ok) ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(ab), (unit / BUFS) & 1, abort_flag, p.wait_limit_ns));
                 return ok;
@@ -819,7 +799,7 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
                 const int ab = unit % BUFS;
                 if (wait(ab)) {
                     tc_fence_after();
-                    load_half(tmem_row + ab * NT, acc);
+                    load_part(tmem_row + ab * NT, acc);
                     ++unit;
                     release(ab);
                 }
@@ -829,9 +809,9 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
                 float fw[AHEAD];
 #pragma unroll
                 for (int i = 0; i < AHEAD; ++i) fw[i] = i < p.kbs ? __ldg(ws + i) : 0.f;
-                f2 sum[HALF / 2];
+                f2 sum[PART / 2];
 #pragma unroll
-                for (int j = 0; j < HALF / 2; ++j) sum[j] = 0ull;
+                for (int j = 0; j < PART / 2; ++j) sum[j] = 0ull;
                 for (int kb = 0; kb < p.kbs; ++kb) {
                     const f2 f = pair(fw[0], fw[0]);
 #pragma unroll
@@ -840,42 +820,43 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
                     const int ab = unit % BUFS;
                     if (!wait(ab)) break;
                     tc_fence_after();
-                    float v[HALF];
-                    load_half(tmem_row + ab * NT, v);
+                    float v[PART];
+                    load_part(tmem_row + ab * NT, v);
                     ++unit;
                     release(ab);
-                    const float4* hs = reinterpret_cast<const float4*>(scales + kb * NT + half * HALF);
+                    const float4* hs = reinterpret_cast<const float4*>(scales + kb * NT + col);
 #pragma unroll
-                    for (int j = 0; j < HALF / 4; ++j) {
+                    for (int j = 0; j < PART / 4; ++j) {
                         const float4 h = hs[j];
                         sum[2 * j] = fma2(pair(v[4 * j], v[4 * j + 1]), mul2(f, pair(h.x, h.y)), sum[2 * j]);
                         sum[2 * j + 1] = fma2(pair(v[4 * j + 2], v[4 * j + 3]), mul2(f, pair(h.z, h.w)), sum[2 * j + 1]);
                     }
                 }
 #pragma unroll
-                for (int j = 0; j < HALF / 2; ++j) { const float2 t = split(sum[j]); acc[2 * j] = t.x; acc[2 * j + 1] = t.y; }
+                for (int j = 0; j < PART / 2; ++j) { const float2 t = split(sum[j]); acc[2 * j] = t.x; acc[2 * j + 1] = t.y; }
             }
 #pragma unroll
-            for (int j = 0; j < HALF; ++j) tile[(half * HALF + j) * S::PITCH + quad * 32 + lane] = acc[j];
+            for (int j = 0; j < PART; ++j) tile[(col + j) * S::PITCH + quad * 32 + lane] = acc[j];
             epi_sync();
+            if (ew < p.rows) {
+                float x[4][PER_WARP];
+                unsigned has = 0;
 #pragma unroll
-            for (int i0 = 0; i0 < PER_WARP; i0 += BATCH) {
-                if (i0 * EPI_WARPS + ew >= p.rows) break;
-                float x[4][BATCH];
+                for (int i = 0; i < PER_WARP; ++i) {
+                    if (i * WARPS + ew < p.rows) has |= 1u << i;
 #pragma unroll
-                for (int i = 0; i < BATCH; ++i)
+                    for (int q = 0; q < 4; ++q) x[q][i] = tile[(i * WARPS + ew) * S::PITCH + 32 * q + lane];
+                }
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) x[q][i] = tile[((i0 + i) * EPI_WARPS + ew) * S::PITCH + 32 * q + lane];
-#pragma unroll
-                for (int i = 0; i < BATCH; ++i) {
-                    State& st = s[i0 + i];
+                for (int i = 0; i < PER_WARP; ++i) {
+                    State& st = s[i];
                     float m = st.m;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const int c = r + 32 * q + lane;
                         if (c < v1) {
                             m = fmaxf(m, x[q][i]);
-                            if (p.col0 + c == token[i0 + i]) p.chosen[(i0 + i) * EPI_WARPS + ew] = x[q][i];
+                            if (p.col0 + c == token[i]) p.chosen[i * WARPS + ew] = x[q][i];
                         }
                     }
                     move(st, m, p.scale);
@@ -888,12 +869,7 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
                         }
                     }
                 }
-                if (TOP) {
-                    unsigned has = 0;
-#pragma unroll
-                    for (int i = 0; i < BATCH; ++i) if ((i0 + i) * EPI_WARPS + ew < p.rows) has |= 1u << i;
-                    offer_tile<BATCH>(list + i0, has, x, p.col0 + r, v1 - r, tile + (i0 * EPI_WARPS + ew) * S::PITCH, EPI_WARPS * S::PITCH);
-                }
+                if (TOP) offer_tile<PER_WARP>(list, has, x, p.col0 + r, v1 - r, tile + ew * S::PITCH, WARPS * S::PITCH);
             }
             epi_sync();                                                 // the tile may be written again
         }
@@ -901,7 +877,7 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
         if (ok) {
 #pragma unroll
             for (int i = 0; i < PER_WARP; ++i) {
-                const int t = i * EPI_WARPS + ew;
+                const int t = i * WARPS + ew;
                 if (t < p.rows) {
                     float m = s[i].m;
 #pragma unroll
@@ -914,9 +890,9 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
                         u += __shfl_xor_sync(0xffffffffu, u, o);
                     }
                     const size_t at = static_cast<size_t>(t) * p.slices + blockIdx.x;
-                    const int n = TOP ? __popc(__ballot_sync(0xffffffffu, lane < p.top && list[i].id != INT_MAX)) : 0;
+                    const int n = TOP ? __popc(__ballot_sync(0xffffffffu, lane < p.top && list[i].key != 0ull)) : 0;
                     if (lane == 0) p.part[at] = make_float4(m, z, u, __int_as_float(n));
-                    if (TOP && lane < n) p.cand[at * p.top + lane] = make_uint2(__float_as_uint(list[i].val), static_cast<unsigned>(list[i].id));
+                    if (TOP && lane < n) p.cand[at * p.top + lane] = make_uint2(__float_as_uint(logit_of(list[i].key)), static_cast<unsigned>(column_of(list[i].key)));
                 }
             }
         }
@@ -925,7 +901,7 @@ tl_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
     tc_fence_before();
     __syncthreads();
     if (*abort_flag)                                                    // the join says so in the status word
-        for (int t = threadIdx.x; t < p.rows; t += THREADS)
+        for (int t = threadIdx.x; t < p.rows; t += S::THREADS)
             p.part[static_cast<size_t>(t) * p.slices + blockIdx.x] = make_float4(MINUS_INF, 0.f, 0.f, __int_as_float(-1));
     if (warp == 1) {
         __syncwarp();
@@ -941,7 +917,7 @@ struct JoinParams {
     const float4* part;
     const uint2* cand;
     float4* run;                                // [rows]: state over the launches so far
-    uint2* run_list;                            // [rows][top]
+    Key* run_list;                              // [rows][top]
     unsigned* floor;
     const int32_t* tokens;
     const float* chosen;
@@ -962,14 +938,12 @@ __global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams 
     if (row >= p.rows) return;
     State s{MINUS_INF, 0.f, 0.f};
     List list;
-    list.lane = lane; list.top = TOP ? p.top : 1; list.clear();
+    list.lane = lane; list.top = TOP ? p.top : 1; list.key = 0ull;
     if (!p.first) {
         const float4 r = p.run[row];
         if (lane == 0) s = State{r.x, r.y, r.z};
         if (TOP && lane < p.top) {
-            const uint2 e = p.run_list[static_cast<size_t>(row) * p.top + lane];
-            list.val = __uint_as_float(e.x);
-            list.id = static_cast<int>(e.y);
+            list.key = p.run_list[static_cast<size_t>(row) * p.top + lane];
         }
     }
     const float4* part = p.part + static_cast<size_t>(row) * p.slices;
@@ -1005,18 +979,14 @@ __global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams 
             };
             load(0);
             for (int j = 0; j < most; ++j) {
-                float x[UNROLL];
-                int c[UNROLL];
+                Key now[UNROLL];
 #pragma unroll
-                for (int k = 0; k < UNROLL; ++k) { x[k] = __uint_as_float(next[k].x); c[k] = static_cast<int>(next[k].y); }
+                for (int k = 0; k < UNROLL; ++k) now[k] = j < n[k] ? key_of(__uint_as_float(next[k].x), static_cast<int>(next[k].y)) : 0ull;
                 load(j + 1);
-                unsigned any = 0;
+                bool any = false;
 #pragma unroll
-                for (int k = 0; k < UNROLL; ++k) {
-                    any |= list.todo(j < n[k], x[k], c[k]);
-                    offer<1>(&list, j < n[k] ? 1u : 0u, x + k, c + k);
-                }
-                if (FEW && any == 0) break;
+                for (int k = 0; k < UNROLL; ++k) any = offer(list, now[k]) || any;
+                if (FEW && !any) break;
             }
         }
     }
@@ -1035,8 +1005,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams 
     if (!p.last) {
         if (lane == 0) p.run[row] = make_float4(m, z, u, 0.f);
         if (TOP) {
-            if (lane < p.top) p.run_list[static_cast<size_t>(row) * p.top + lane] = make_uint2(__float_as_uint(list.val), static_cast<unsigned>(list.id));
-            if (lane == p.top - 1 && list.id != INT_MAX) p.floor[row] = ordered(list.val);
+            if (lane < p.top) p.run_list[static_cast<size_t>(row) * p.top + lane] = list.key;
+            if (lane == p.top - 1 && list.key != 0ull) p.floor[row] = static_cast<unsigned>(list.key >> 32);
         }
         return;
     }
@@ -1055,9 +1025,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams 
         }
     }
     if (TOP && lane < p.top) {
-        const bool some = list.id != INT_MAX;
-        p.top_logp[static_cast<size_t>(row) * p.top + lane] = some ? (list.val - m) * p.inv_temp - lz : MINUS_INF;
-        p.top_ids[static_cast<size_t>(row) * p.top + lane] = some ? list.id : -1;
+        const bool some = list.key != 0ull;
+        p.top_logp[static_cast<size_t>(row) * p.top + lane] = some ? (logit_of(list.key) - m) * p.inv_temp - lz : MINUS_INF;
+        p.top_ids[static_cast<size_t>(row) * p.top + lane] = some ? column_of(list.key) : -1;
     }
 }
 
