@@ -3,11 +3,11 @@
 // Bound: memory.  Forward reads x and r and writes z and y (four passes; 8-bit output: three and a half), backward reads z, dy and dz
 // and writes dx (four).  The kernels are built like the layer norm's (row_kernels.cuh):
 //   rows     a group of 1 to 16 warps owns a row at a time, rows arrive by bulk copies in a ring in shared memory, several rows
-//            ahead; one barrier per row (the warps' sums of squares, or of a z); weights as fp32 in shared memory.  Forward, a thread
-//            keeps its 8 to 32 elements of z in registers from the addition to the store; backward, it reads z and dy from the ring
-//            twice and keeps the column sums of dy zh in registers over all rows of its group, one partial sum per block.
+//            ahead; one barrier per row (the warps' sums of squares, or of a z); weights as fp32 in shared memory.  A thread keeps its 8
+//            to 32 elements of a row in registers from the ring to the store: forward as fp32, backward z, dy and dz in their own type
+//            beside the column sums of dy zh over all rows of its group (one partial sum per block at the end).
 //   narrow   aligned rows of up to 512 bytes (a norm over one head): 8, 16 or 32 lanes a row, several rows to a warp, no ring
-//   generic  rows too wide for two of them in shared memory: a block per row, 128 columns to a warp at a time
+//   generic  rows too wide for shared memory: a block per row, 128 columns to a warp at a time, 0.1 to 0.15 of the memory's rate
 // The largest magnitude of 128 columns is a maximum over 16 lanes (16-bit rows: 8 neighbours a lane) or a warp, in registers: the
 // 8-bit output costs no pass of its own.
 
@@ -233,10 +233,43 @@ __global__ void __maxnreg__(FORWARD_REGS) rms_forward_rows(const RmsArgs a) {
     }
 }
 
+// Part q (8 elements) of a thread's columns of a row in shared memory as they are, and as pairs.
+template <typename T> constexpr int PART_WORDS = 2 * static_cast<int>(sizeof(T));
+template <typename T, bool VEC, typename C> __device__ __forceinline__ void read_words(const C& cols, uint32_t row, int q, uint32_t* w) {
+    const uint32_t at = row + (cols.first + C::STEP * q * C::PART) * static_cast<int>(sizeof(T));
+    if constexpr (VEC) {
+#pragma unroll
+        for (int k = 0; k < C::PART; ++k) {
+            w[4 * k] = w[4 * k + 1] = w[4 * k + 2] = w[4 * k + 3] = 0u;
+            if (cols.has(q * C::PART + k))
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4 * k]), "=r"(w[4 * k + 1]), "=r"(w[4 * k + 2]), "=r"(w[4 * k + 3]) : "r"(at + k * 512));
+        }
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            w[k] = 0u;
+            if (cols.has(q * C::PART + k)) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[k]) : "r"(at + k * 128));
+        }
+    } else {
+        uint16_t h[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            h[k] = 0;
+            if (cols.has(q * C::PART + k)) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h[k]) : "r"(at + k * 64));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = static_cast<uint32_t>(h[2 * i]) | static_cast<uint32_t>(h[2 * i + 1]) << 16;
+    }
+}
+template <typename T> __device__ __forceinline__ f2 word_pair(const uint32_t* w, int i) {
+    if constexpr (sizeof(T) == 4) return pair(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    else return widen<T>(w[i]);
+}
+
 template <typename T, bool VEC, int EPT, bool RES>
 __global__ void __maxnreg__(BACKWARD_REGS) rms_backward_rows(const RmsArgs a) {
     extern __shared__ __align__(128) uint8_t raw[];
-    constexpr int NA = RES ? 3 : 2;
+    constexpr int NA = RES ? 3 : 2, W = PART_WORDS<T>;
     const Group g = group_setup<T, VEC, NA, true>(a, raw);
     using C = Columns<T, VEC, EPT, false>;
     const C cols(g.warp, g.lane, a.d);
@@ -249,71 +282,60 @@ __global__ void __maxnreg__(BACKWARD_REGS) rms_backward_rows(const RmsArgs a) {
     f2 dg[C::PAIRS];
 #pragma unroll
     for (int i = 0; i < C::PAIRS; ++i) dg[i] = 0ull;
-    // The row is read from the ring twice, before and after the group's sum: the registers that would keep it hold the column
-    // sums.  The first reading of a row comes before the second reading of the row before it, so the group's barrier finds everyone
-    // with work in between.
-    auto slot_of = [&](int s) { return g.ring + s * a.slot; };
-    auto first_reading = [&](int r, int s, uint32_t parity, float* to) {
-        const uint32_t slot = vpce::smem_u32(slot_of(s));
+    // A row is read from the ring once and stays in registers in its own type, beside the column sums, so that its slot is free for
+    // another row at the group's barrier.
+    int s = 0, pass = 0, turn = 0;                                          // the warps take turns at starting copies
+    uint32_t parity = 0;
+    for (int r = g.first; r < a.rows; r += g.step) {
+        const uint32_t slot = vpce::smem_u32(g.ring + s * a.slot);
         const uint32_t zr = slot + (VEC ? 0u : a.in[0].shift(r)), dyr = slot + a.cap + (VEC ? 0u : a.in[1].shift(r));
+        const uint32_t dzr = slot + 2 * a.cap + (VEC || !RES ? 0u : a.in[2].shift(r));
         wait_row(g.bars + 8 * s, parity);
+        uint32_t zw[EPT / 8 * W], uw[EPT / 8 * W], ww[RES ? EPT / 8 * W : 1];
         f2 s0 = 0ull, s1 = 0ull;
 #pragma unroll
         for (int q = 0; q < EPT / 8; ++q) {
-            f2 z[4], u[4], gq[4];
-            cols.read(zr, q, z);
-            cols.read(dyr, q, u);
+            f2 gq[4];
+            read_words<T, VEC>(cols, zr, q, zw + q * W);
+            read_words<T, VEC>(cols, dyr, q, uw + q * W);
+            if constexpr (RES) read_words<T, VEC>(cols, dzr, q, ww + q * W);
             cols.weights(gw, q, gq);
-            s0 = fma2(mul2(u[0], gq[0]), z[0], s0); s1 = fma2(mul2(u[1], gq[1]), z[1], s1);
-            s0 = fma2(mul2(u[2], gq[2]), z[2], s0); s1 = fma2(mul2(u[3], gq[3]), z[3], s1);
+            s0 = fma2(mul2(word_pair<T>(uw + q * W, 0), gq[0]), word_pair<T>(zw + q * W, 0), s0);
+            s1 = fma2(mul2(word_pair<T>(uw + q * W, 1), gq[1]), word_pair<T>(zw + q * W, 1), s1);
+            s0 = fma2(mul2(word_pair<T>(uw + q * W, 2), gq[2]), word_pair<T>(zw + q * W, 2), s0);
+            s1 = fma2(mul2(word_pair<T>(uw + q * W, 3), gq[3]), word_pair<T>(zw + q * W, 3), s1);
         }
+        const float rs = ld_shared(slot + NA * a.cap);
         const float2 p = split(add2(s0, s1));
-        const float v = warp_sum(p.x + p.y);
-        if (g.lane == 0) to[g.warp] = v;
-    };
-    if (g.first < a.rows) {
-        int s = 0, pass = 0, turn = 0;
-        uint32_t parity = 0;
-        first_reading(g.first, 0, 0u, part[0]);
-        for (int r = g.first; r < a.rows; r += g.step) {
-            group_sync(g.id, a.warps);
-            const float sum = half_warp_sum((g.lane & 15) < a.warps ? part[pass][g.lane & 15] : 0.f);
-            pass ^= 1;
-            const int here = s;
-            if (++s == a.stages) { s = 0; parity ^= 1u; }
-            // the slot of the row before is spent: it takes the next row that is not under way yet
-            if (g.warp == turn && g.lane == 0 && r > g.first && r + (a.stages - 1) * g.step < a.rows) {
-                const int before = here == 0 ? a.stages - 1 : here - 1;
-                fetch_row<T, VEC, NA, true>(a, r + (a.stages - 1) * g.step, slot_of(before), g.bars + 8 * before);
-            }
-            if (++turn == a.warps) turn = 0;
-            if (r + g.step < a.rows) first_reading(r + g.step, s, parity, part[pass]);
-            const uint32_t slot = vpce::smem_u32(slot_of(here));
-            const uint32_t zr = slot + (VEC ? 0u : a.in[0].shift(r)), dyr = slot + a.cap + (VEC ? 0u : a.in[1].shift(r));
-            const uint32_t dzr = slot + 2 * a.cap + (VEC || !RES ? 0u : a.in[2].shift(r));
-            const float rs = ld_shared(slot + NA * a.cap);
-            // zh mean(a zh) rstd = zh (rstd^2 mean(a z)): the three factors apart, since rstd^3 leaves fp32's range early
-            const float mx = -rs * (rs * (sum * inv_d));
-            const f2 rs2 = pair(rs, rs), mx2 = pair(mx, mx);
-            T* dx = static_cast<T*>(a.out) + r * a.out_stride;
+        const float mine = warp_sum(p.x + p.y);
+        if (g.lane == 0) part[pass][g.warp] = mine;
+        group_sync(g.id, a.warps);
+        if (g.warp == turn && g.lane == 0 && r + a.stages * g.step < a.rows)
+            fetch_row<T, VEC, NA, true>(a, r + a.stages * g.step, g.ring + s * a.slot, g.bars + 8 * s);
+        if (++turn == a.warps) turn = 0;
+        if (++s == a.stages) { s = 0; parity ^= 1u; }
+        const float sum = half_warp_sum((g.lane & 15) < a.warps ? part[pass][g.lane & 15] : 0.f);
+        pass ^= 1;
+        // zh mean(a zh) rstd = zh (rstd^2 mean(a z)): the three factors apart, since rstd^3 leaves fp32's range early
+        const float mx = -rs * (rs * (sum * inv_d));
+        const f2 rs2 = pair(rs, rs), mx2 = pair(mx, mx);
+        T* dx = static_cast<T*>(a.out) + r * a.out_stride;
 #pragma unroll
-            for (int q = 0; q < EPT / 8; ++q) {
-                f2 z[4], u[4], gq[4], w[4];
-                cols.read(zr, q, z);
-                cols.read(dyr, q, u);
-                cols.weights(gw, q, gq);
-                if constexpr (RES) cols.read(dzr, q, w);
+        for (int q = 0; q < EPT / 8; ++q) {
+            f2 gq[4], o[4];
+            cols.weights(gw, q, gq);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f2 zh = mul2(z[i], rs2);
-                    dg[4 * q + i] = fma2(u[i], zh, dg[4 * q + i]);
-                    z[i] = fma2(mul2(u[i], gq[i]), rs2, RES ? fma2(zh, mx2, w[i]) : mul2(zh, mx2));
-                }
-                if (a.out) cols.store(dx, q, z);
+            for (int i = 0; i < 4; ++i) {
+                const f2 zh = mul2(word_pair<T>(zw + q * W, i), rs2), u = word_pair<T>(uw + q * W, i);
+                dg[4 * q + i] = fma2(u, zh, dg[4 * q + i]);
+                if constexpr (RES) o[i] = fma2(mul2(u, gq[i]), rs2, fma2(zh, mx2, word_pair<T>(ww + q * W, i)));
+                else o[i] = fma2(mul2(u, gq[i]), rs2, mul2(zh, mx2));
             }
+            if (a.out) cols.store(dx, q, o);
         }
     }
     if (!a.partial) return;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");         // the sums' last step may be brought up
     // The block's sums: every group leaves its own in the ring (all copies have landed and been read), then all threads add
     // them, the groups in order.
     float* sums = reinterpret_cast<float*>(raw + a.ring);
@@ -461,6 +483,7 @@ __global__ void __launch_bounds__(NARROW_THREADS, 2) rms_backward_narrow(const R
         }
     }
     if (!a.partial) return;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     // the warp's rows at once, then the block's warps in order
 #pragma unroll
     for (int i = 0; i < P::PAIRS; ++i) {
@@ -597,6 +620,7 @@ rms_backward_finish(const float* __restrict__ partial, int slices, long d, W* __
     const int cc = threadIdx.x % COL_TILE, rr = threadIdx.x / COL_TILE;
     const long c = static_cast<long>(blockIdx.x) * COL_TILE + cc;
     float s = 0.f;
+    asm volatile("griddepcontrol.wait;" ::: "memory");                      // for the end of the kernel before
     if (c < d) {
 #pragma unroll 4
         for (int i = rr; i < slices; i += FIN_ROWS) s += partial[static_cast<long>(i) * d + c];
@@ -619,13 +643,18 @@ struct RowShape { int ept, threads, grid, smem; };
 RowShape row_shape(RmsArgs* a, size_t elem, int na, bool backward) {
     RowShape s;
     // Elements per thread: a warp costs about 8 instructions for each of its threads' elements and 110 for the rest of a row
-    // (waits, sums over the warp and the group).
-    s.ept = 8;
+    // (waits, sums over the warp and the group).  Backward, three rows in their own type and the column sums stay in registers: 24
+    // elements are the most without spills (2^25 bf16 elements, with dz: 52 to 58 us at 1024 to 12288 columns; 32 elements: 62 to
+    // 66), so 32 are taken only for 16-bit rows that 24 cannot hold.
+    const int widest = backward && (elem == 4 || na == 3) ? 24 : 32;
+    s.ept = 0;
     int best = 1 << 30;
-    for (int ept : {8, 16, 32}) {
+    for (int ept : {8, 16, widest}) {
         const int warps = (a->d + 32 * ept - 1) / (32 * ept), cost = warps * (8 * ept + 110);
         if (warps <= MAX_GROUP_WARPS && cost < best) { best = cost; s.ept = ept; a->warps = warps; }
     }
+    if (s.ept == 0 && elem == 2) { s.ept = 32; a->warps = (a->d + 1023) / 1024; }
+    if (s.ept == 0) { s.grid = 0; return s; }
     const int most = (backward ? BACKWARD_WARPS : FORWARD_WARPS) / a->warps;
     a->groups = std::max(1, a->warps > 1 ? std::min(most, 15) : most);          // named barriers 1 to 15
     while (a->groups > 1 && static_cast<int64_t>(a->groups - 1) * sm_count() >= a->rows) --a->groups;   // few rows: spread over the SMs
@@ -639,7 +668,7 @@ RowShape row_shape(RmsArgs* a, size_t elem, int na, bool backward) {
     s.smem = a->ring + a->groups * a->stages * a->slot;
     if (backward) s.smem = std::max<int>(s.smem, a->ring + 4 * a->d * a->groups);   // the groups' sums take its place
     const int64_t blocks = (a->rows + a->groups - 1) / a->groups;
-    s.grid = a->stages >= 2 && s.smem <= MAX_SMEM ? static_cast<int>(std::min<int64_t>(blocks, std::min(sm_count(), MAX_SLICES))) : 0;
+    s.grid = a->stages >= 1 && s.smem <= MAX_SMEM ? static_cast<int>(std::min<int64_t>(blocks, std::min(sm_count(), MAX_SLICES))) : 0;
     return s;
 }
 
@@ -665,7 +694,8 @@ template <typename T, bool VEC, bool RES> cudaError_t backward_rows(const RmsArg
     switch (s.ept) {
         case 8: return launch_rows<rms_backward_rows<T, VEC, 8, RES>>(a, s, st);
         case 16: return launch_rows<rms_backward_rows<T, VEC, 16, RES>>(a, s, st);
-        default: return launch_rows<rms_backward_rows<T, VEC, 32, RES>>(a, s, st);
+        case 24: return launch_rows<rms_backward_rows<T, VEC, 24, RES>>(a, s, st);
+        default: return launch_rows<rms_backward_rows<T, VEC, sizeof(T) == 4 ? 24 : 32, RES>>(a, s, st);     // fp32: at most 24
     }
 }
 
@@ -727,13 +757,25 @@ struct Backward {
     int w_dtype; const float* rstd; void* dx; int64_t dxs; void* dg; float* partial; cudaStream_t st;
 };
 
-void finish(const Backward& b, int slices) {
-    const unsigned tiles = static_cast<unsigned>((b.d + COL_TILE - 1) / COL_TILE);
+// The last step of the sums over rows, brought up while the kernel before it still runs (2 us less in a small backward pass).
+cudaError_t finish(const Backward& b, int slices) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>((b.d + COL_TILE - 1) / COL_TILE));
+    cfg.blockDim = dim3(COL_TILE * FIN_ROWS);
+    cfg.stream = b.st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cudaError_t e = cudaSuccess;
     with_type(b.w_dtype, [&](auto* w) {
         using W = std::remove_pointer_t<decltype(w)>;
-        rms_backward_finish<W><<<tiles, COL_TILE * FIN_ROWS, 0, b.st>>>(b.partial, slices, b.d, static_cast<W*>(b.dg));
+        const float* partial = b.partial;
+        e = cudaLaunchKernelEx(&cfg, rms_backward_finish<W>, partial, slices, static_cast<long>(b.d), static_cast<W*>(b.dg));
         return 0;
     });
+    return e;
 }
 
 template <typename T, bool RES> int backward_typed(const Backward& b) {
@@ -753,14 +795,14 @@ template <typename T, bool RES> int backward_typed(const Backward& b) {
             if (lanes == 8) rms_backward_narrow<T, 8, RES><<<grid, NARROW_THREADS, 0, b.st>>>(a);
             else if (lanes == 16) rms_backward_narrow<T, 16, RES><<<grid, NARROW_THREADS, 0, b.st>>>(a);
             else rms_backward_narrow<T, 32, RES><<<grid, NARROW_THREADS, 0, b.st>>>(a);
-            if (a.partial) finish(b, grid);
+            if (a.partial && finish(b, grid) != cudaSuccess) return VPCE_CUDA_ERROR;
             return code(cudaGetLastError());
         }
         const RowShape s = row_shape(&a, e, RES ? 3 : 2, true);
         if (s.grid > 0) {
             if (cudaError_t err = vec ? backward_rows<T, true, RES>(a, s, b.st) : backward_rows<T, false, RES>(a, s, b.st); err != cudaSuccess)
                 return VPCE_CUDA_ERROR;
-            if (a.partial) finish(b, s.grid);
+            if (a.partial && finish(b, s.grid) != cudaSuccess) return VPCE_CUDA_ERROR;
             return code(cudaGetLastError());
         }
     }
@@ -768,7 +810,7 @@ template <typename T, bool RES> int backward_typed(const Backward& b) {
         const unsigned tiles = static_cast<unsigned>((b.d + COL_TILE - 1) / COL_TILE);
         rms_backward_columns<T><<<dim3(tiles, slices), COL_TILE * COL_ROWS, 0, b.st>>>(
             static_cast<const T*>(b.dy), b.dys, static_cast<const T*>(b.z), b.zs, b.rows, b.d, b.rstd, b.partial);
-        finish(b, slices);
+        if (finish(b, slices) != cudaSuccess) return VPCE_CUDA_ERROR;
     }
     if (b.dx && b.rows > 0) {                               // after the column sums: dx may be dy itself
         GenArgs a{};

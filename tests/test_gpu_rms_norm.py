@@ -117,6 +117,15 @@ def test_matches_definition(rows, d, dtype, wdtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("rows,d", [(300, 12288), (301, 12289), (150, 14336), (5, 16385), (1200, 5120), (2000, 769)])
+def test_widths_at_the_switches_between_kernels(rows, d, dtype):
+    (x, r, dy, dz), w = make(rows, d, dtype, torch.float32, seed=d)
+    z, rstd = check_forward(x, r, w)
+    check_backward(dy, dz, z, w, rstd)
+    check_backward(dy, None, z, w, rstd)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
 @pytest.mark.parametrize("rows,d,pad,offset", [(40, 256, 8, 0), (40, 256, 5, 0), (33, 1000, 24, 3), (65, 2880, 2880, 8), (21, 513, 1, 1),
                                                (300, 3, 0, 1), (50, 1, 2, 0), (7, 20001, 3, 0)])
 def test_strides_and_offsets(rows, d, pad, offset, dtype):
