@@ -27,7 +27,8 @@ using namespace vptl;
 
 constexpr int64_t CHUNK = 4096;                     // tokens whose hidden states stay in L2 beside a strip of the weight
 constexpr size_t SLICE_BYTES = size_t{64} << 20;    // partial states and candidates of a launch
-constexpr int FEW_CTAS = 148;                       // slices of the kernel for few tokens
+constexpr int FEW_CTAS = 148;                       // slices of the kernel for few tokens: a CTA per SM
+static_assert(FEW_CTAS <= JOIN_FEW_SLICES, "the join takes them all at once");
 
 std::atomic<int> g_drop{-1};
 
@@ -140,17 +141,17 @@ template <bool F8, bool TOP> cudaError_t launch_few(int nt, const CUtensorMap& h
 }
 
 // Brought up while the kernel before it still runs (it waits for that one's end before it reads anything).
-template <bool TOP, bool FEW> cudaError_t launch_join(int blocks, const JoinParams& j, cudaStream_t st) {
+template <bool TOP> cudaError_t launch_join(bool few, const JoinParams& j, cudaStream_t st) {
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(blocks);
-    cfg.blockDim = dim3(JOIN_THREADS);
+    cfg.gridDim = dim3(few ? j.rows : (j.rows + JOIN_THREADS / 32 - 1) / (JOIN_THREADS / 32));
+    cfg.blockDim = dim3(few ? JOIN_FEW_THREADS : JOIN_THREADS);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, tl_join_kernel<TOP, FEW>, j);
+    return cudaLaunchKernelEx(&cfg, few ? tl_join_few_kernel<TOP> : tl_join_kernel<TOP>, j);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -224,9 +225,7 @@ int forward(const void* H, const float* Hs, const void* W, const float* Ws, cons
             if (e != cudaSuccess) return VPCE_CUDA_ERROR;
             j.first = c0 == 0;
             j.last = c0 + strip >= V;
-            const int blocks = (j.rows + JOIN_THREADS / 32 - 1) / (JOIN_THREADS / 32);
-            if (pl.few) e = top ? launch_join<true, true>(blocks, j, st) : launch_join<false, true>(blocks, j, st);
-            else e = top ? launch_join<true, false>(blocks, j, st) : launch_join<false, false>(blocks, j, st);
+            e = top ? launch_join<true>(pl.few, j, st) : launch_join<false>(pl.few, j, st);
             if (e != cudaSuccess) return VPCE_CUDA_ERROR;
             p.drop_kb = -1;
         }

@@ -927,11 +927,95 @@ struct JoinParams {
     int* status;
 };
 
+// A token's results from its state and list, by one warp.
+template <bool TOP> __device__ __forceinline__ void emit(const JoinParams& p, int row, float m, float z, float u, const List& list) {
+    const int lane = list.lane;
+    const float lz = logf(z);
+    if (lane == 0) {
+        if (p.lse) p.lse[row] = fmaf(m, p.inv_temp, lz);
+        if (p.entropy) p.entropy[row] = fmaxf(lz - LN2_F * (u / z), 0.f) + (z == z ? 0.f : z);      // fmaxf passes a NaN over
+        if (p.logp) {
+            const int t = p.tokens[row];
+            float out = 0.f;
+            if (t != p.ignore_index) {
+                if (static_cast<unsigned>(t) < static_cast<unsigned>(p.V)) out = (p.chosen[row] - m) * p.inv_temp - lz;
+                else atomicOr(p.status, VPCE_DEV_LABEL_OUT_OF_RANGE);
+            }
+            p.logp[row] = out;
+        }
+    }
+    if (TOP && lane < p.top) {
+        const bool some = list.key != 0ull;
+        p.top_logp[static_cast<size_t>(row) * p.top + lane] = some ? (logit_of(list.key) - m) * p.inv_temp - lz : MINUS_INF;
+        p.top_ids[static_cast<size_t>(row) * p.top + lane] = some ? column_of(list.key) : -1;
+    }
+}
+// The lanes' states as one.
+__device__ __forceinline__ State over_lanes(State s, float scale) {
+    float m = s.m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    move(s, m, scale);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        s.z += __shfl_xor_sync(0xffffffffu, s.z, o);
+        s.u += __shfl_xor_sync(0xffffffffu, s.u, o);
+    }
+    return s;
+}
+
+// The slices of the kernel for few tokens: a block per token, a warp for 32 slices.  Their lists are sorted, so the search ends at the
+// first rank at which no slice has anything to offer; the warps' lists are then merged in a row (6 steps each).  8 to 10 us became
+// 5 against one warp per token.
+constexpr int JOIN_FEW_WARPS = 5, JOIN_FEW_THREADS = 32 * JOIN_FEW_WARPS, JOIN_FEW_SLICES = 32 * JOIN_FEW_WARPS;
+template <bool TOP> __global__ void __launch_bounds__(JOIN_FEW_THREADS) tl_join_few_kernel(const JoinParams p) {
+    __shared__ float4 states[JOIN_FEW_WARPS];
+    __shared__ Key keys[JOIN_FEW_WARPS][32];
+    const int row = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, i = threadIdx.x;
+    wait_for_last();
+    const float4 q = i < p.slices ? p.part[static_cast<size_t>(row) * p.slices + i] : make_float4(MINUS_INF, 0.f, 0.f, 0.f);
+    const int n = __float_as_int(q.w);
+    const State s = over_lanes(State{q.x, q.y, q.z}, p.scale);
+    const bool expired = __any_sync(0xffffffffu, n < 0);
+    List list;
+    list.lane = lane; list.top = TOP ? p.top : 1; list.key = 0ull;
+    if (TOP) {
+        const uint2* cand = p.cand + (static_cast<size_t>(row) * p.slices + i) * p.top;
+        const int most = __reduce_max_sync(0xffffffffu, n);
+        uint2 next = make_uint2(0u, 0u);
+        if (0 < n) next = cand[0];
+        for (int j = 0; j < most; ++j) {
+            const Key now = j < n ? key_of(__uint_as_float(next.x), static_cast<int>(next.y)) : 0ull;
+            if (j + 1 < n) next = cand[j + 1];
+            if (!offer(list, now)) break;
+        }
+        keys[warp][lane] = list.key;
+    }
+    if (lane == 0) states[warp] = make_float4(s.m, s.z, s.u, expired ? 1.f : 0.f);
+    __syncthreads();
+    if (warp) return;
+    State all{MINUS_INF, 0.f, 0.f};
+    if (lane < JOIN_FEW_WARPS) {
+        const float4 t = states[lane];
+        all = State{t.x, t.y, t.z};
+        if (t.w != 0.f) atomicOr(p.status, VPCE_DEV_WAIT_EXPIRED);
+    }
+    all = over_lanes(all, p.scale);
+    if (TOP) {
+#pragma unroll
+        for (int w = 1; w < JOIN_FEW_WARPS; ++w) {
+            const Key o = keys[w][31 - lane];
+            if (o > list.key) list.key = o;
+#pragma unroll
+            for (int j = 16; j > 0; j >>= 1) in_order<1>(&list.key, j, (lane & j) == 0);
+        }
+    }
+    emit<TOP>(p, row, all.m, all.z, all.u, list);
+}
+
 constexpr int JOIN_THREADS = 128;
 // A warp per token, its lanes over the slices, 128 at a time, always in the same order.
-// FEW: the slices of the kernel for few tokens, whose lists are sorted, so that the search ends at the first rank at which no slice
-// has anything to offer.
-template <bool TOP, bool FEW>
+template <bool TOP>
 __global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams p) {
     const int row = blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     wait_for_last();
@@ -948,8 +1032,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams 
     }
     const float4* part = p.part + static_cast<size_t>(row) * p.slices;
     const uint2* cand = p.cand + static_cast<size_t>(row) * p.slices * (TOP ? p.top : 0);
-    constexpr int UNROLL = FEW ? 5 : 4;                             // 5 x 32 lanes: all slices of the kernel for few tokens
-    bool expired = false;
+    constexpr int UNROLL = 4;
     for (int i0 = 0; i0 < p.slices; i0 += 32 * UNROLL) {
         float4 q[UNROLL];
 #pragma unroll
@@ -967,7 +1050,6 @@ __global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams 
             s.z += o.z;
             s.u += o.u;
             n[k] = __float_as_int(q[k].w);
-            expired = expired || n[k] < 0;
             most = max(most, n[k]);
         }
         if (TOP) {
@@ -983,52 +1065,21 @@ __global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams 
 #pragma unroll
                 for (int k = 0; k < UNROLL; ++k) now[k] = j < n[k] ? key_of(__uint_as_float(next[k].x), static_cast<int>(next[k].y)) : 0ull;
                 load(j + 1);
-                bool any = false;
 #pragma unroll
-                for (int k = 0; k < UNROLL; ++k) any = offer(list, now[k]) || any;
-                if (FEW && !any) break;
+                for (int k = 0; k < UNROLL; ++k) offer(list, now[k]);
             }
         }
     }
-    if (FEW && __any_sync(0xffffffffu, expired) && lane == 0) atomicOr(p.status, VPCE_DEV_WAIT_EXPIRED);
-    // over the lanes
-    float m = s.m;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    move(s, m, p.scale);
-    float z = s.z, u = s.u;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        z += __shfl_xor_sync(0xffffffffu, z, o);
-        u += __shfl_xor_sync(0xffffffffu, u, o);
-    }
+    s = over_lanes(s, p.scale);
     if (!p.last) {
-        if (lane == 0) p.run[row] = make_float4(m, z, u, 0.f);
+        if (lane == 0) p.run[row] = make_float4(s.m, s.z, s.u, 0.f);
         if (TOP) {
             if (lane < p.top) p.run_list[static_cast<size_t>(row) * p.top + lane] = list.key;
             if (lane == p.top - 1 && list.key != 0ull) p.floor[row] = static_cast<unsigned>(list.key >> 32);
         }
         return;
     }
-    const float lz = logf(z);
-    if (lane == 0) {
-        if (p.lse) p.lse[row] = fmaf(m, p.inv_temp, lz);
-        if (p.entropy) p.entropy[row] = fmaxf(lz - LN2_F * (u / z), 0.f) + (z == z ? 0.f : z);
-        if (p.logp) {
-            const int t = p.tokens[row];
-            float out = 0.f;
-            if (t != p.ignore_index) {
-                if (static_cast<unsigned>(t) < static_cast<unsigned>(p.V)) out = (p.chosen[row] - m) * p.inv_temp - lz;
-                else atomicOr(p.status, VPCE_DEV_LABEL_OUT_OF_RANGE);
-            }
-            p.logp[row] = out;
-        }
-    }
-    if (TOP && lane < p.top) {
-        const bool some = list.key != 0ull;
-        p.top_logp[static_cast<size_t>(row) * p.top + lane] = some ? (logit_of(list.key) - m) * p.inv_temp - lz : MINUS_INF;
-        p.top_ids[static_cast<size_t>(row) * p.top + lane] = some ? column_of(list.key) : -1;
-    }
+    emit<TOP>(p, row, s.m, s.z, s.u, list);
 }
 
 }  // namespace vptl
