@@ -14,7 +14,7 @@
  * VPCE_DEV_LABEL_OUT_OF_RANGE in the status word); lse, entropy (with its gradient) and alternatives do not depend on the token.
  * Products are exact products of the inputs accumulated in fp32; statistics are fp32 and joined in a fixed order: the same call gives
  * the same bits every time.  A NaN among a token's logits makes its lse, logp and entropy NaN and is not an alternative; alternatives
- * that do not exist for that reason have id -1 and value -inf.
+ * that do not exist for that reason have id -1 and value -inf.  An infinite logit (of an overflow) makes the entropy NaN.
  *
  * 8-bit operands: e4m3 numbers with fp32 scales, one for each 128 columns of a row of H and for each 128 x 128 block of W
  *     x_v = sum over blocks b of 128 columns:  Hs[n, b] Ws[v / 128, b] (sum over k in b of Hq[n, k] Wq[v, k])
@@ -41,7 +41,7 @@ size_t vp_token_logp_fp8_workspace_bytes(int64_t T, int64_t d, int64_t V, int to
 
 /*
  * H [T, d] and W [V, d] bf16.  tokens and logp may both be NULL; lse, entropy may be NULL; top_logp [T, top] fp32 and top_ids [T, top]
- * int32 are needed where top > 0 (0 <= top <= min(V, VP_TOKEN_LOGP_MAX_TOP)).  temperature > 0.  T == 0 launches nothing.
+ * int32 are needed where top > 0 (0 <= top <= min(V, VP_TOKEN_LOGP_MAX_TOP)).  temperature: 1e-6 to 1e6.  T == 0 launches nothing.
  */
 int vp_token_logp_forward(const void* H, const void* W, const int32_t* tokens, int64_t T, int64_t d, int64_t V, double temperature,
                           int32_t ignore_index, float* logp, float* lse, float* entropy, float* top_logp, int32_t* top_ids, int top,

@@ -162,7 +162,7 @@ template <bool F8>
 int forward(const void* H, const float* Hs, const void* W, const float* Ws, const int32_t* tokens, int64_t T, int64_t d, int64_t V,
             double temperature, int32_t ignore_index, float* logp, float* lse, float* entropy, float* top_logp, int32_t* top_ids, int top,
             void* workspace, size_t workspace_bytes, cudaStream_t st) {
-    if (T < 0 || d <= 0 || V <= 0 || top < 0 || top > MAX_TOP || top > V || !(temperature > 0.0) || !(temperature < 1e30)) return VPCE_INVALID_ARG;
+    if (T < 0 || d <= 0 || V <= 0 || top < 0 || top > MAX_TOP || top > V || !(temperature >= 1e-6) || !(temperature <= 1e6)) return VPCE_INVALID_ARG;
     if ((logp != nullptr) != (tokens != nullptr) && T > 0) return VPCE_INVALID_ARG;
     if (T == 0) return VPCE_OK;
     if (!H || !W || (F8 && (!Hs || !Ws)) || !workspace || (top > 0 && (!top_logp || !top_ids))) return VPCE_INVALID_ARG;

@@ -53,10 +53,10 @@ __device__ __forceinline__ unsigned ordered(float v) {
 __device__ __forceinline__ float from_ordered(unsigned o) {
     return o == 0u ? MINUS_INF : __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu));
 }
-// The number just below v: "> below(v)" accepts v itself.
+// The number just below v: "> below(v)" accepts v itself (of either sign where it is a zero).
 __device__ __forceinline__ float below(float v) {
-    const unsigned o = ordered(v);
-    return v == MINUS_INF || o == 0u ? MINUS_INF : from_ordered(o - 1u);
+    if (v == 0.f) return -1.40129846e-45f;
+    return v == MINUS_INF ? MINUS_INF : from_ordered(ordered(v) - 1u);
 }
 
 using f2 = unsigned long long;

@@ -176,6 +176,19 @@ def test_ties_go_to_the_lowest_id(T):
     assert torch.equal(top_ids, torch.arange(V - 40, V - 20, device="cuda", dtype=torch.int32).expand(T, 20))
 
 
+@pytest.mark.parametrize("T", [5, 100, 600])
+def test_zero_rows(T):
+    """Hidden states of padding: every logit is a zero, some of them negative ones."""
+    V, d = 40000, 64
+    H = torch.zeros(T, d, device="cuda", dtype=torch.bfloat16)
+    H[1::2] = -0.0
+    W = torch.randn(V, d, generator=torch.Generator(device="cuda").manual_seed(0), device="cuda").to(torch.bfloat16)
+    _, _, entropy, top_logp, top_ids = run(H, W, torch.zeros(T, dtype=torch.int32, device="cuda"), 20)
+    assert torch.equal(top_ids, torch.arange(20, device="cuda", dtype=torch.int32).expand(T, 20))
+    assert float((entropy.double() - torch.log(torch.tensor(float(V), dtype=torch.float64))).abs().max()) < 1e-5
+    assert float((top_logp + entropy[:, None]).abs().max()) < 1e-5
+
+
 @pytest.mark.parametrize("T", [7, 300])
 def test_rising_logits(T):
     """The worst order for the lists: every column is better than all before it."""
@@ -335,6 +348,33 @@ def test_autograd():
         g.sum().backward()
 
 
+def test_captured_gradients():
+    """Forward and backward in one graph, replayed on new inputs.  (No eager graph of the same leaves may live meanwhile: torch keeps
+    their accumulation on the stream of that one, outside the capture.)"""
+    H, W, tokens = bf16_grid(130, 64, 700, seed=4)
+    H.requires_grad_(), W.requires_grad_()
+    x, r = torch.randn(130, 64, device="cuda", dtype=torch.bfloat16, requires_grad=True), torch.randn(130, 64, device="cuda", dtype=torch.bfloat16)
+
+    def step():
+        y, z = vp.rms_norm(x, None, r)
+        out = vp.token_log_probs(H + y, W, tokens, top_k=2, block_v=256)
+        return torch.autograd.grad(out.logp.sum() + 0.1 * out.entropy.sum() + z.sum(), (H, W, x))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    with torch.no_grad():
+        H.neg_(), r.mul_(2)
+    graph.replay()
+    got = [g.clone() for g in captured]
+    assert all(torch.equal(a, b) for a, b in zip(got, step()))
+
+
 def test_empty():
     H, W = torch.empty(0, 64, device="cuda", dtype=torch.bfloat16), torch.zeros(10, 64, device="cuda", dtype=torch.bfloat16)
     W.requires_grad_()
@@ -381,7 +421,7 @@ def test_refusals():
         vp.vp_token_logp_forward(H, W, None, 1.0, IGN, *outs, ws)
     with pytest.raises(ValueError):
         vp.vp_token_logp_forward(H, W[:, :56], tokens, 1.0, IGN, *outs, ws)
-    for bad in (0.0, -1.0, float("nan")):
+    for bad in (0.0, -1.0, float("nan"), 1e-7, 1e7):
         with pytest.raises(vp.VpceError):
             vp.vp_token_logp_forward(H, W, tokens, bad, IGN, *outs, ws)
     with pytest.raises(vp.VpceError):
@@ -431,6 +471,15 @@ def test_quantize_blocks(rows, d, pad, dtype):
     assert ((back - clean).abs() <= err).all()
     if rows > 256:
         assert (s[1] == 1).all() and (back[128:256] == 0).all()
+
+
+def test_quantize_more_rows_than_one_launch_takes():
+    rows = 65535 * 128 + 130
+    w = torch.ones(rows, 1, device="cuda", dtype=torch.bfloat16)
+    w[-130:] = 3
+    q, s = vp.quantize_blocks_fp8(w)
+    assert (q.float() == 448).all() and (s[:-2] == torch.tensor(1.0) / 448).all()
+    assert ((s[-2:] - 3 / 448).abs() <= 3 / 448 * 4 * U).all()
 
 
 def test_quantize_blocks_refusals():
