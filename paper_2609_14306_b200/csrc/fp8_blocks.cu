@@ -1,6 +1,6 @@
 // A weight to 8 bits in blocks of 128 x 128 with a scale each (fp8_blocks.h).
 //
-// Bound: memory, 2 + 1 bytes an element from 16-bit types.  A CTA of 8 warps has a block: a warp 16 of its rows, which it holds in
+// Bound: memory, 2 + 1 bytes an element from 16-bit types: 201088 x 2880 bf16 in 272 us, 6.4 TB/s (a plain copy: 6.56).  A CTA of 8 warps has a block: a warp 16 of its rows, which it holds in
 // registers in the input's type from the load to the store, so the block is read once; its largest magnitude goes over the warps through
 // shared memory.  Rows of 16-byte pieces where every row starts on a 16-byte boundary, else single elements.
 

@@ -10,6 +10,9 @@
 //   generic  rows too wide for shared memory: a block per row, 128 columns to a warp at a time, 0.1 to 0.15 of the memory's rate
 // The largest magnitude of 128 columns is a maximum over 16 lanes (16-bit rows: 8 neighbours a lane) or a warp, in registers: the
 // 8-bit output costs no pass of its own.
+// Measured: 16384 x 2880 bf16 with a residual 59 us forward, 62 backward (58 each at a plain copy's rate), 140 for both and the sums
+// in repetition; 32768 x 7168 bf16 to 8 bits 268 us (252); rows off every 16-byte boundary 0.5 to 0.65 of the aligned rate in 16 bits (0.4 to
+// 8 bits, whose stores are single bytes), 0.8 to 0.95 in fp32.
 
 #include <cuda_fp8.h>
 

@@ -209,9 +209,15 @@ struct Best {
 // Two CTAs of a cluster per 256 x 256 tile (cta_group::2), persistent, tiles dealt round robin with the token tiles fastest (the tokens
 // of a launch stay in L2, the weight streams).  An epilogue thread has one token's 128 columns.
 //   bf16   the accumulator of a tile is complete in tensor memory; two of them, so the epilogue of one runs beside the products of
-//          the next
+//          the next.  Bound: the tensor cores under the power cap; 4096 x 2880 x 201088 with 8 alternatives in 3.48 ms, 1360 TFLOP/s
+//          (0.98 of cuBLAS's sustained rate).  Alternatives cost 3 % there, most of it in the first strip, where everything is new.
 //   8 bits every k-block of 128 has its own scale, so its product is its own accumulator, and the epilogue threads add it to their
-//          128 sums in registers with fp32 factors; the two buffers alternate by k-block
+//          128 sums in registers with fp32 factors; the two buffers alternate by k-block.  Bound: that hand-over, 0.57 us a k-block
+//          where the product alone takes 0.44 (4096 x 7168 x 32768: 0.89 ms, 0.69 with one accumulator per tile, which is not the
+//          operator); 8192 x 7168 x 129280 in 7.7 ms, 1960 TFLOP/s.  Not better: four buffers of 128 columns (1.07 ms: narrower
+//          products, twice the hand-overs), 16 epilogue warps of 64 columns (0.95), scales through shared memory from a warp of their
+//          own (0.91), one signal for accumulator and stage (0.93), spinning waits (0.92).  A few spilled registers in the warps
+//          before the epilogue cost 15 %.
 constexpr int SMEM_MAX = 227 * 1024;
 constexpr int STAGE = TILE_M * KB_BYTES + HALF_N * KB_BYTES;       // 32 KB
 constexpr int LIST_BYTES = EPI_THREADS * MAX_TOP * 5, SCRATCH_BYTES = EPI_THREADS * 8 * 4;
@@ -632,6 +638,8 @@ template <int N> __device__ __forceinline__ void offer_tile(List* list, unsigned
 // so no tensor-core work is spent on rows that are not there, and every CTA streams its own share of the vocabulary (a
 // multiple of 32 rows) through a ring of 6 to 8 stages.  The logits of a tile go through shared memory, so that a warp has a token's
 // 128 logits side by side: it keeps the token's state (a lane its own part) and list in registers from tile to tile.
+// One token of 2880 x 201088 with 8 alternatives: 184 us with the join, 6.3 TB/s (0.96 of a plain copy's rate); 16 tokens of 7168 x 129280
+// in 8 bits 157 us, 5.9 TB/s; 61 tokens of 2048 x 32771 with 20 alternatives 48 us, 34 without (two tiles a CTA: start, end and the lists).
 constexpr int FEW_TOKENS = 64, FEW_ROWS = 32;                       // W's rows per copy
 template <int NT, bool F8> struct Few {
     static constexpr int STAGES = NT == 64 ? 6 : 8;
