@@ -14,7 +14,8 @@
  * VPCE_DEV_LABEL_OUT_OF_RANGE in the status word); lse, entropy (with its gradient) and alternatives do not depend on the token.
  * Products are exact products of the inputs accumulated in fp32; statistics are fp32 and joined in a fixed order: the same call gives
  * the same bits every time.  A NaN among a token's logits makes its lse, logp and entropy NaN and is not an alternative; alternatives
- * that do not exist for that reason have id -1 and value -inf.  An infinite logit (of an overflow) makes the entropy NaN.
+ * that do not exist for that reason have id -1 and value -inf.  Where a logit is infinite (an
+ * overflow, or an infinity among the inputs), that token's lse, logp and entropy are undefined; other tokens' are not touched.
  *
  * 8-bit operands: e4m3 numbers with fp32 scales, one for each 128 columns of a row of H and for each 128 x 128 block of W
  *     x_v = sum over blocks b of 128 columns:  Hs[n, b] Ws[v / 128, b] (sum over k in b of Hq[n, k] Wq[v, k])

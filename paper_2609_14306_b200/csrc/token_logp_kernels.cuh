@@ -941,7 +941,8 @@ template <bool TOP> __device__ __forceinline__ void emit(const JoinParams& p, in
     const float lz = logf(z);
     if (lane == 0) {
         if (p.lse) p.lse[row] = fmaf(m, p.inv_temp, lz);
-        if (p.entropy) p.entropy[row] = fmaxf(lz - LN2_F * (u / z), 0.f) + (z == z ? 0.f : z);      // fmaxf passes a NaN over
+        const float h = lz - LN2_F * (u / z);
+        if (p.entropy) p.entropy[row] = h < 0.f ? 0.f : h;                  // a rounding below zero; a NaN stays
         if (p.logp) {
             const int t = p.tokens[row];
             float out = 0.f;
