@@ -658,9 +658,9 @@ RowShape row_shape(RmsArgs* a, size_t elem, int na, bool backward) {
     }
     if (s.ept == 0 && elem == 2) { s.ept = 32; a->warps = (a->d + 1023) / 1024; }
     if (s.ept == 0) { s.grid = 0; return s; }
-    const int most = (backward ? BACKWARD_WARPS : FORWARD_WARPS) / a->warps;
+    const int most = (backward ? BACKWARD_WARPS : FORWARD_WARPS) / a->warps, sms = sm_count();
     a->groups = std::max(1, a->warps > 1 ? std::min(most, 15) : most);          // named barriers 1 to 15
-    while (a->groups > 1 && static_cast<int64_t>(a->groups - 1) * sm_count() >= a->rows) --a->groups;   // few rows: spread over the SMs
+    while (a->groups > 1 && static_cast<int64_t>(a->groups - 1) * sms >= a->rows) --a->groups;   // few rows: spread over the SMs
     a->cap = static_cast<int>((a->d * elem + 15) / 16 * 16 + 16);
     a->slot = na * a->cap + (backward ? 16 : 0);
     auto ring = [&] { return FULL_BYTES + a->groups * PART_BYTES + 4 * 32 * s.ept * a->warps; };
@@ -671,7 +671,7 @@ RowShape row_shape(RmsArgs* a, size_t elem, int na, bool backward) {
     s.smem = a->ring + a->groups * a->stages * a->slot;
     if (backward) s.smem = std::max<int>(s.smem, a->ring + 4 * a->d * a->groups);   // the groups' sums take its place
     const int64_t blocks = (a->rows + a->groups - 1) / a->groups;
-    s.grid = a->stages >= 1 && s.smem <= MAX_SMEM ? static_cast<int>(std::min<int64_t>(blocks, std::min(sm_count(), MAX_SLICES))) : 0;
+    s.grid = a->stages >= 1 && s.smem <= MAX_SMEM ? static_cast<int>(std::min<int64_t>(blocks, std::min(sms, MAX_SLICES))) : 0;
     return s;
 }
 

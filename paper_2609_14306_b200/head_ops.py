@@ -54,12 +54,13 @@ def fp8_blocks(n: int) -> int:
 
 
 # --------------------------------------------------------------------------- RMS norm (rms_norm.h)
-def _rms_types(x, *weights):
-    if x.dtype not in _DTYPE_CODE:
-        raise TypeError(f"x must be bfloat16, float16 or float32, got {x.dtype}")
-    wdt = next((w.dtype for w in weights if w is not None), x.dtype)
-    if wdt is not x.dtype and wdt is not _F32:
-        raise TypeError(f"weight and its gradient must be {x.dtype} or float32, got {wdt}")
+def _rms_types(dt, weight):
+    """The weight's element type, checked against the rows' type dt."""
+    if dt not in _DTYPE_CODE:
+        raise TypeError(f"x must be bfloat16, float16 or float32, got {dt}")
+    wdt = dt if weight is None else weight.dtype
+    if wdt is not dt and wdt is not _F32:
+        raise TypeError(f"weight and its gradient must be {dt} or float32, got {wdt}")
     return wdt
 
 
@@ -74,7 +75,8 @@ def _rms_inputs(x, residual, weight, z, rstd):
     if residual is None and z is not None:
         raise ValueError("z is the sum with a residual: without one it is x itself")
     rows, d = x.shape
-    wdt, dt = _rms_types(x, weight), x.dtype
+    dt = x.dtype
+    wdt = _rms_types(dt, weight)
     xp, xs = _rows(x, dt, "x", rows, d, dev)
     rp, rs = _opt_rows(residual, dt, "residual", rows, d, dev)
     zp, zs = _opt_rows(z, dt, "z", rows, d, dev)
@@ -111,7 +113,8 @@ def vp_rms_backward(dy, dz, z, weight, rstd, dx, dweight, workspace, stream=None
     if z.dim() != 2:
         raise ValueError("z must be [rows, d]")
     rows, d = z.shape
-    wdt, dt = _rms_types(z, weight, dweight), z.dtype
+    dt = z.dtype
+    wdt = _rms_types(dt, dweight if weight is None else weight)
     zp, zs = _rows(z, dt, "z", rows, d, dev)
     dyp, dys = _rows(dy, dt, "dy", rows, d, dev)
     dzp, dzs = _opt_rows(dz, dt, "dz", rows, d, dev)
