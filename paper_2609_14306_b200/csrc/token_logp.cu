@@ -143,7 +143,8 @@ template <bool F8, bool TOP> cudaError_t launch_few(int nt, const CUtensorMap& h
 // Brought up while the kernel before it still runs (it waits for that one's end before it reads anything).
 template <bool TOP> cudaError_t launch_join(bool few, const JoinParams& j, cudaStream_t st) {
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(few ? j.rows : (j.rows + JOIN_THREADS / 32 - 1) / (JOIN_THREADS / 32));
+    const bool many = j.rows >= JOIN_MANY;
+    cfg.gridDim = dim3(few || !many ? j.rows : (j.rows + JOIN_WARPS - 1) / JOIN_WARPS);
     cfg.blockDim = dim3(few ? JOIN_FEW_THREADS : JOIN_THREADS);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -151,7 +152,7 @@ template <bool TOP> cudaError_t launch_join(bool few, const JoinParams& j, cudaS
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, few ? tl_join_few_kernel<TOP> : tl_join_kernel<TOP>, j);
+    return cudaLaunchKernelEx(&cfg, few ? tl_join_few_kernel<TOP> : many ? tl_join_kernel<TOP, 1> : tl_join_kernel<TOP, JOIN_WARPS>, j);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

@@ -143,16 +143,18 @@ __device__ __forceinline__ void move(State& s, float m, float scale) {
     s.m = m;
 }
 
-// Folds 32 logits (columns of which the first `valid` exist) into the state.
-__device__ __forceinline__ float fold32(State& s, float* v, int valid, float scale) {
+// Folds 32 logits (columns of which the first `valid` exist) into the state; leaves the maxima of each four in quads[8].
+__device__ __forceinline__ void fold32(State& s, float* v, int valid, float scale, float* quads) {
     if (valid < 32) {
 #pragma unroll
         for (int j = 0; j < 32; ++j) if (j >= valid) v[j] = MINUS_INF;
     }
-    float cmax = v[0];
+    float m = s.m;
 #pragma unroll
-    for (int j = 1; j < 32; ++j) cmax = fmaxf(cmax, v[j]);
-    const float m = fmaxf(s.m, cmax);
+    for (int j = 0; j < 8; ++j) {
+        quads[j] = fmaxf(fmaxf(v[4 * j], v[4 * j + 1]), fmaxf(v[4 * j + 2], v[4 * j + 3]));
+        m = fmaxf(m, quads[j]);
+    }
     const f2 scale2 = pair(scale, scale), minus = pair(-m, -m);
     f2 z0 = 0ull, u0 = 0ull, z1 = 0ull, u1 = 0ull;
     if (valid < 32) {
@@ -177,7 +179,6 @@ __device__ __forceinline__ float fold32(State& s, float* v, int valid, float sca
     move(s, m, scale);
     s.z += z.x + z.y;
     s.u += u.x + u.y;
-    return cmax;
 }
 
 // A thread's best `top` logits of its slice, unordered, in shared memory: entry j of a thread at j * EPI_THREADS (both arrays).
@@ -204,6 +205,43 @@ struct Best {
         lim = least;
     }
 };
+
+// Which of a slice's 128 columns may matter, by groups of eight: the bits of those with an entry above best.lim.  Where many are (a
+// token's first slices, before its bound has settled), that is first raised to what the slice itself says: the top-th largest
+// of its 32 quads' maxima is a bound for its top-th logit.  Inserting into lists one by one what that keeps out took 50 to 90 us of 285
+// for 65 tokens x 201088.
+__device__ __forceinline__ unsigned groups_above(Best& best, const float* quads) {
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) n += quads[j] > best.lim ? 1 : 0;
+    if (!__any_sync(0xffffffffu, n > 0)) return 0u;
+    if (__any_sync(0xffffffffu, n > best.top)) {
+        float t[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) t[j] = quads[j];
+        // a bitonic network in registers, larger first
+#pragma unroll
+        for (int w = 2; w <= 32; w <<= 1)
+#pragma unroll
+            for (int k = w >> 1; k > 0; k >>= 1)
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if ((j & k) == 0) {
+                        const float a = t[j], b = t[j | k];
+                        const bool down = (j & w) == 0;
+                        t[j] = down ? fmaxf(a, b) : fminf(a, b);
+                        t[j | k] = down ? fminf(a, b) : fmaxf(a, b);
+                    }
+        float bound = t[MAX_TOP - 1];
+#pragma unroll
+        for (int j = MAX_TOP - 2; j >= 0; --j) if (best.top <= j + 1) bound = t[j];
+        best.lim = fmaxf(best.lim, below(bound));
+    }
+    unsigned mine = 0u;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) mine |= fmaxf(quads[2 * j], quads[2 * j + 1]) > best.lim ? 1u << j : 0u;
+    return __reduce_or_sync(0xffffffffu, mine);
+}
 
 // ------------------------------------------------------------------------------------ the strip kernel
 // Two CTAs of a cluster per 256 x 256 tile (cta_group::2), persistent, tiles dealt round robin with the token tiles fastest (the tokens
@@ -378,25 +416,39 @@ tl_strip_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t acc = tmem_row + ab * TILE_N;
-#pragma unroll 1
-                for (int c = 0; c < HALF_N; c += 32) {
-                    if (c >= valid) break;
+                auto fold = [&](int c, float* quads) {
                     float v[32];
                     __syncwarp();
                     tmem_ld32(acc + c, v);
                     tmem_ld_wait();
                     pick(v, c);
-                    const float cmax = fold32(s, v, valid - c, p.scale);
-                    if (TOP && __any_sync(0xffffffffu, cmax > best.lim)) {
-#pragma unroll 1
-                        for (int h = c; h < c + 32; h += 8) {
-                            float w[8];
-                            tmem_ld8(acc + h, w);
-                            tmem_ld_wait();
+                    fold32(s, v, valid - c, p.scale, quads);
+                };
+                if constexpr (TOP) {
+                    float quads[32];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) if (h + j < valid) best.offer(w[j], h + j);
-                            __syncwarp();
+                    for (int c = 0; c < HALF_N; c += 32) {
+                        if (c < valid) fold(c, quads + c / 4);
+                        else {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) quads[c / 4 + j] = MINUS_INF;
                         }
+                    }
+                    for (unsigned todo = groups_above(best, quads); todo; todo &= todo - 1) {
+                        const int h = 8 * (__ffs(todo) - 1);
+                        float w[8];
+                        __syncwarp();
+                        tmem_ld8(acc + h, w);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) if (h + j < valid) best.offer(w[j], h + j);
+                    }
+                    __syncwarp();
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < HALF_N && c < valid; c += 32) {
+                        float quads[8];
+                        fold(c, quads);
                     }
                 }
                 ++unit;
@@ -436,24 +488,38 @@ tl_strip_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__
                     ++unit;
                 }
                 if (!ok) break;
+                float quads[TOP ? 32 : 8];
 #pragma unroll
                 for (int c = 0; c < HALF_N; c += 32) {
+                    float* const to = quads + (TOP ? c / 4 : 0);
                     if (c < valid) {
                         float v[32];
 #pragma unroll
                         for (int j = 0; j < 16; ++j) { const float2 t = split(acc[c / 2 + j]); v[2 * j] = t.x; v[2 * j + 1] = t.y; }
                         pick(v, c);
-                        const float cmax = fold32(s, v, valid - c, p.scale);
-                        if (TOP && __any_sync(0xffffffffu, cmax > best.lim)) {
+                        fold32(s, v, valid - c, p.scale, to);
+                    } else if (TOP) {
 #pragma unroll
-                            for (int h = c; h < c + 32; h += 8) {
+                        for (int j = 0; j < 8; ++j) to[j] = MINUS_INF;
+                    }
+                }
+                if constexpr (TOP) {
+                    const unsigned todo = groups_above(best, quads);
+                    if (todo) {
 #pragma unroll
-                                for (int j = 0; j < 8; ++j) scratch[j * EPI_THREADS] = v[h - c + j];
+                        for (int h = 0; h < HALF_N; h += 8) {
+                            if (todo >> (h / 8) & 1u) {
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    const float2 t = split(acc[h / 2 + j]);
+                                    scratch[2 * j * EPI_THREADS] = t.x;
+                                    scratch[(2 * j + 1) * EPI_THREADS] = t.y;
+                                }
 #pragma unroll 1
                                 for (int j = 0; j < 8; ++j) if (h + j < valid) best.offer(scratch[j * EPI_THREADS], h + j);
                             }
-                            __syncwarp();
                         }
+                        __syncwarp();
                     }
                 }
             }
@@ -973,9 +1039,20 @@ __device__ __forceinline__ State over_lanes(State s, float scale) {
     return s;
 }
 
+// The first warp's list with those that the others have left in shared memory: sorted ones, so six steps each.
+template <int WARPS> __device__ __forceinline__ void merge_lists(List& list, const Key (*keys)[32]) {
+#pragma unroll
+    for (int w = 1; w < WARPS; ++w) {
+        const Key o = keys[w][31 - list.lane];
+        if (o > list.key) list.key = o;
+#pragma unroll
+        for (int j = 16; j > 0; j >>= 1) in_order<1>(&list.key, j, (list.lane & j) == 0);
+    }
+}
+
 // The slices of the kernel for few tokens: a block per token, a warp for 32 slices.  Their lists are sorted, so the search ends at the
-// first rank at which no slice has anything to offer; the warps' lists are then merged in a row (6 steps each).  8 to 10 us became
-// 5 against one warp per token.
+// first rank at which no slice has anything to offer; the warps' lists are then merged in a row.  8 to 10 us became 5 against one
+// warp per token.
 constexpr int JOIN_FEW_WARPS = 5, JOIN_FEW_THREADS = 32 * JOIN_FEW_WARPS, JOIN_FEW_SLICES = 32 * JOIN_FEW_WARPS;
 template <bool TOP> __global__ void __launch_bounds__(JOIN_FEW_THREADS) tl_join_few_kernel(const JoinParams p) {
     __shared__ float4 states[JOIN_FEW_WARPS];
@@ -1010,39 +1087,34 @@ template <bool TOP> __global__ void __launch_bounds__(JOIN_FEW_THREADS) tl_join_
         if (t.w != 0.f) atomicOr(p.status, VPCE_DEV_WAIT_EXPIRED);
     }
     all = over_lanes(all, p.scale);
-    if (TOP) {
-#pragma unroll
-        for (int w = 1; w < JOIN_FEW_WARPS; ++w) {
-            const Key o = keys[w][31 - lane];
-            if (o > list.key) list.key = o;
-#pragma unroll
-            for (int j = 16; j > 0; j >>= 1) in_order<1>(&list.key, j, (lane & j) == 0);
-        }
-    }
+    if (TOP) merge_lists<JOIN_FEW_WARPS>(list, keys);
     emit<TOP>(p, row, all.m, all.z, all.u, list);
 }
 
-constexpr int JOIN_THREADS = 128;
-// A warp per token, its lanes over the slices, 128 at a time, always in the same order.
-template <bool TOP>
+// The strips' slices: WARPS warps per token, their lanes over the slices, 32 x 4 a warp at a time, always in the same order.  One warp a
+// token where there are tokens enough to fill the SMs (8 us a strip of 4096), eight below (65 tokens x 201088 with 8 alternatives: 56
+// us with one).
+constexpr int JOIN_WARPS = 8, JOIN_THREADS = 32 * JOIN_WARPS, JOIN_MANY = 2048;
+template <bool TOP, int WARPS>
 __global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams p) {
-    const int row = blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    __shared__ float4 states[JOIN_WARPS];
+    __shared__ Key keys[JOIN_WARPS][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = WARPS == 1 ? 0 : warp;
+    const int row = WARPS == 1 ? blockIdx.x * JOIN_WARPS + warp : blockIdx.x;
     wait_for_last();
     if (row >= p.rows) return;
     State s{MINUS_INF, 0.f, 0.f};
     List list;
     list.lane = lane; list.top = TOP ? p.top : 1; list.key = 0ull;
-    if (!p.first) {
+    if (!p.first && w == 0) {
         const float4 r = p.run[row];
         if (lane == 0) s = State{r.x, r.y, r.z};
-        if (TOP && lane < p.top) {
-            list.key = p.run_list[static_cast<size_t>(row) * p.top + lane];
-        }
+        if (TOP && lane < p.top) list.key = p.run_list[static_cast<size_t>(row) * p.top + lane];
     }
     const float4* part = p.part + static_cast<size_t>(row) * p.slices;
     const uint2* cand = p.cand + static_cast<size_t>(row) * p.slices * (TOP ? p.top : 0);
     constexpr int UNROLL = 4;
-    for (int i0 = 0; i0 < p.slices; i0 += 32 * UNROLL) {
+    for (int i0 = w * 32 * UNROLL; i0 < p.slices; i0 += WARPS * 32 * UNROLL) {
         float4 q[UNROLL];
 #pragma unroll
         for (int k = 0; k < UNROLL; ++k) {
@@ -1080,6 +1152,16 @@ __global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams 
         }
     }
     s = over_lanes(s, p.scale);
+    if constexpr (WARPS > 1) {
+        if (lane == 0) states[warp] = make_float4(s.m, s.z, s.u, 0.f);
+        keys[warp][lane] = list.key;
+        __syncthreads();
+        if (warp) return;
+        State all{MINUS_INF, 0.f, 0.f};
+        if (lane < WARPS) { const float4 t = states[lane]; all = State{t.x, t.y, t.z}; }
+        s = over_lanes(all, p.scale);
+        if (TOP) merge_lists<WARPS>(list, keys);
+    }
     if (!p.last) {
         if (lane == 0) p.run[row] = make_float4(s.m, s.z, s.u, 0.f);
         if (TOP) {
