@@ -3,8 +3,8 @@
 //
 // Up to 64 tokens: one pass over the weight, then one over the 148 slices that it leaves per token.  More: chunks of up to 4096 tokens,
 // whose hidden states stay in L2 while the vocabulary goes by in strips; each strip leaves (m, z, u) per token and 128 columns, and
-// the candidates for the alternatives, and the join folds them into the token's running state.  Candidates cost little: what one
-// slice has found bounds the token's list from below (`floor`), and slices that come later compare 32 logits' maximum with it.
+// the candidates for the alternatives, and the join folds them into the token's running state.  Candidates cost little: what slices
+// have found so far bounds the token's list from below (`floor`, `marks`), and slices that come later compare their maxima with it.
 // The strips' width follows from the workspace that partial states and candidates may take (64 MB).
 
 #include <cuda.h>
@@ -38,7 +38,7 @@ struct Plan {
     int64_t chunk;                                  // tokens per launch
     int strip_tiles, slices;                        // 256-column tiles per launch; slices per token and launch
     bool few;
-    size_t floor, chosen, run, run_list, part, cand, total;
+    size_t floor, marks, chosen, run, run_list, part, cand, total;
 };
 
 bool plan(int64_t T, int64_t d, int64_t V, int top, int d_unit, int64_t d_most, Plan* p) {
@@ -60,6 +60,7 @@ bool plan(int64_t T, int64_t d, int64_t V, int top, int d_unit, int64_t d_most, 
     }
     size_t off = 256;                                                       // the status word
     p->floor = off;    off = up(off + sizeof(unsigned) * p->chunk);
+    p->marks = off;    off = up(off + (p->few || top == 0 ? 0 : 32 * sizeof(unsigned) * p->chunk));
     p->chosen = off;   off = up(off + sizeof(float) * p->chunk);
     p->run = off;      off = up(off + sizeof(float4) * p->chunk);
     p->run_list = off; off = up(off + sizeof(Key) * p->chunk * top);
@@ -219,6 +220,7 @@ int forward(const void* H, const float* Hs, const void* W, const float* Ws, cons
             p.col0 = static_cast<int>(c0);
             p.cols = static_cast<int>(std::min(strip, V - c0));
             p.n_tiles = (p.cols + TILE_N - 1) / TILE_N;
+            p.marks = top > 0 && c0 == 0 ? reinterpret_cast<unsigned*>(ws + pl.marks) : nullptr;
             if (!pl.few) p.slices = j.slices = 2 * p.n_tiles;
             cudaError_t e;
             if (pl.few) e = top ? launch_few<F8, true>(nt, tmH, tmW, p, st) : launch_few<F8, false>(nt, tmH, tmW, p, st);

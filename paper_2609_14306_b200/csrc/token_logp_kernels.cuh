@@ -37,7 +37,10 @@ struct Params {
     float4* part;                           // [rows][slices]: m, z, u, number of candidates
     uint2* cand;                            // [rows][slices][top]: logit, column
     int top;
-    unsigned* floor;                        // [rows]: a lower bound on the token's top-th largest logit (ordered bits; 0: none)
+    // Bounds from below on a token's top-th largest logit, as ordered bits (0: none): from the strips before, and of the first strip the
+    // largest logits of its slices so far, by the slice's number modulo 32 (null in later strips).  The top-th largest of those is
+    // one: each stands in another column.
+    unsigned *floor, *marks;                // [rows], [rows][32]
     float* chosen;                          // [rows]: logit of the given token
     const float *hs, *ws;                   // 8 bits: scales of H's rows [.][kbs], of W's blocks [.][kbs]
     int* status;
@@ -206,6 +209,41 @@ struct Best {
     }
 };
 
+// The top-th largest of 32 numbers (in whose place they are sorted, larger first, by a bitonic network in registers).
+template <typename T> __device__ __forceinline__ T top_th(T* t, int top) {
+#pragma unroll
+    for (int w = 2; w <= 32; w <<= 1)
+#pragma unroll
+        for (int k = w >> 1; k > 0; k >>= 1)
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if ((j & k) == 0) {
+                    const T a = t[j], b = t[j | k], more = a > b ? a : b, less = a > b ? b : a;
+                    const bool down = (j & w) == 0;
+                    t[j] = down ? more : less;
+                    t[j | k] = down ? less : more;
+                }
+    T r = t[MAX_TOP - 1];
+#pragma unroll
+    for (int j = MAX_TOP - 2; j >= 0; --j) if (top <= j + 1) r = t[j];
+    return r;
+}
+// A token's bound, as a number to be above.
+__device__ __forceinline__ float above_floor(const Params& p, int row) {
+    unsigned o = __ldcg(p.floor + row);
+    if (p.marks) {
+        unsigned t[32];
+        const uint4* from = reinterpret_cast<const uint4*>(p.marks) + 8 * static_cast<size_t>(row);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint4 q = __ldcg(from + i);
+            t[4 * i] = q.x; t[4 * i + 1] = q.y; t[4 * i + 2] = q.z; t[4 * i + 3] = q.w;
+        }
+        o = max(o, top_th(t, p.top));
+    }
+    return below(from_ordered(o));
+}
+
 // Which of a slice's 128 columns may matter, by groups of eight: the bits of those with an entry above best.lim.  Where many are (a
 // token's first slices, before its bound has settled), that is first raised to what the slice itself says: the top-th largest
 // of its 32 quads' maxima is a bound for its top-th logit.  Inserting into lists one by one what that keeps out took 50 to 90 us of 285
@@ -219,22 +257,7 @@ __device__ __forceinline__ unsigned groups_above(Best& best, const float* quads)
         float t[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) t[j] = quads[j];
-        // a bitonic network in registers, larger first
-#pragma unroll
-        for (int w = 2; w <= 32; w <<= 1)
-#pragma unroll
-            for (int k = w >> 1; k > 0; k >>= 1)
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if ((j & k) == 0) {
-                        const float a = t[j], b = t[j | k];
-                        const bool down = (j & w) == 0;
-                        t[j] = down ? fmaxf(a, b) : fminf(a, b);
-                        t[j | k] = down ? fminf(a, b) : fmaxf(a, b);
-                    }
-        float bound = t[MAX_TOP - 1];
-#pragma unroll
-        for (int j = MAX_TOP - 2; j >= 0; --j) if (best.top <= j + 1) bound = t[j];
+        const float bound = top_th(t, best.top);
         best.lim = fmaxf(best.lim, below(bound));
     }
     unsigned mine = 0u;
@@ -401,7 +424,7 @@ tl_strip_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__
             const int token = p.tokens && row_ok ? p.tokens[row] : -1;
             const int rel = token - (p.col0 + c0);                      // the token's column within this thread's, if 0 <= rel < 128
             State s{MINUS_INF, 0.f, 0.f};
-            if (TOP) { best.n = 0; best.lim = row_ok ? below(from_ordered(__ldcg(p.floor + row))) : __builtin_huge_valf(); }
+            if (TOP) { best.n = 0; best.lim = row_ok ? above_floor(p, row) : __builtin_huge_valf(); }
             auto pick = [&](const float* v, int c) {                    // c: first of 32 columns
                 if (static_cast<unsigned>(rel - c) < 32u && rel < valid) {
                     float x = 0.f;
@@ -531,6 +554,7 @@ tl_strip_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__
                     for (int j = 0; j < best.n; ++j)
                         to[j] = make_uint2(__float_as_uint(best.val[j * EPI_THREADS]), static_cast<unsigned>(p.col0 + c0 + best.col[j * EPI_THREADS]));
                     if (best.n == p.top) atomicMax(p.floor + row, ordered(best.lim));
+                    if (p.marks && best.n > 0) atomicMax(p.marks + 32 * static_cast<size_t>(row) + ((2 * nt + half) & 31), ordered(s.m));
                 }
             }
         }
