@@ -246,8 +246,8 @@ __device__ __forceinline__ float above_floor(const Params& p, int row) {
 
 // Which of a slice's 128 columns may matter, by groups of eight: the bits of those with an entry above best.lim.  Where many are (a
 // token's first slices, before its bound has settled), that is first raised to what the slice itself says: the top-th largest
-// of its 32 quads' maxima is a bound for its top-th logit.  Inserting into lists one by one what that keeps out took 50 to 90 us of 285
-// for 65 tokens x 201088.
+// of its 32 quads' maxima is a bound for its top-th logit.  (65 tokens of 2880 x 201088 with 20 alternatives: 413 us without this and
+// the marks, 275 with both.)
 __device__ __forceinline__ unsigned groups_above(Best& best, const float* quads) {
     int n = 0;
 #pragma unroll
@@ -270,8 +270,9 @@ __device__ __forceinline__ unsigned groups_above(Best& best, const float* quads)
 // Two CTAs of a cluster per 256 x 256 tile (cta_group::2), persistent, tiles dealt round robin with the token tiles fastest (the tokens
 // of a launch stay in L2, the weight streams).  An epilogue thread has one token's 128 columns.
 //   bf16   the accumulator of a tile is complete in tensor memory; two of them, so the epilogue of one runs beside the products of
-//          the next.  Bound: the tensor cores under the power cap; 4096 x 2880 x 201088 with 8 alternatives in 3.48 ms, 1360 TFLOP/s
-//          (0.98 of cuBLAS's sustained rate).  Alternatives cost 3 % there, most of it in the first strip, where everything is new.
+//          the next.  Bound: the tensor cores under the power cap; 4096 x 2880 x 201088 with 8 alternatives in 3.3 to 3.5 ms (boards
+//          differ), 1360 to 1440 TFLOP/s: cuBLAS's sustained rate.  Alternatives are 5 % of it, most of that in the first strip, where
+//          everything is new; of 65 tokens 240 us with 8 alternatives and 275 with 20, 220 without.
 //   8 bits every k-block of 128 has its own scale, so its product is its own accumulator, and the epilogue threads add it to their
 //          128 sums in registers with fp32 factors; the two buffers alternate by k-block.  Bound: that hand-over, 0.57 us a k-block
 //          where the product alone takes 0.44 (4096 x 7168 x 32768: 0.89 ms, 0.69 with one accumulator per tile, which is not the
