@@ -110,6 +110,7 @@ CASES = [  # T, d, V, top, temperature
     (1, 8, 1, 1, 1.0), (1, 64, 5, 5, 1.0), (2, 72, 31, 3, 0.5), (3, 256, 33, 20, 1.0), (1, 2880, 40001, 8, 1.0), (15, 512, 4099, 20, 1.3),
     (16, 64, 127, 1, 1.0), (17, 200, 128, 8, 0.7), (32, 1024, 129, 20, 1.0), (33, 256, 4736, 4, 1.0), (63, 136, 5000, 0, 1.0), (64, 768, 19000, 20, 2.0),
     (65, 64, 1, 1, 1.0), (65, 8, 255, 20, 1.0), (66, 256, 256, 8, 1.0), (128, 512, 257, 20, 0.6), (255, 72, 4099, 5, 1.0), (256, 256, 1000, 0, 1.0),
+    (4096, 64, 132000, 0, 1.0), (4100, 64, 70000, 3, 1.0),
     (257, 256, 40000, 20, 1.0), (500, 2880, 9000, 8, 1.0), (1000, 128, 20000, 20, 1.0), (4097, 64, 3000, 8, 1.0), (4500, 192, 17000, 20, 1.0),
 ]
 
