@@ -5,6 +5,8 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 REPO_DIR = os.path.dirname(PKG_DIR)
@@ -46,12 +48,24 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     """Compile csrc/*.cu into libvpce.so next to this file; returns the library path."""
     if not force and not is_stale():
         return LIB_PATH
-    cmd = [find_nvcc(), *NVCC_FLAGS, "-I", os.path.join(REPO_DIR, "include"), "-o", LIB_PATH, *SOURCES]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+    nvcc = find_nvcc()
+
+    def run(*args: str) -> str:
+        res = subprocess.run([nvcc, *args], capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+        return res.stdout + res.stderr
+
+    # one process per source: the longest decides
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(src) + ".o") for src in SOURCES]
+        flags = [f for f in NVCC_FLAGS if f != "--shared"]
+        compile_one = lambda src, obj: run(*flags, "-c", "-I", os.path.join(REPO_DIR, "include"), "-o", obj, src)  # noqa: E731
+        with ThreadPoolExecutor(max_workers=min(len(SOURCES), os.cpu_count() or 1)) as pool:
+            log = "".join(pool.map(compile_one, SOURCES, objects))
+        log += run(*NVCC_FLAGS, "-o", LIB_PATH, *objects)
     if verbose:
-        sys.stderr.write(res.stdout + res.stderr)
+        sys.stderr.write(log)
     return LIB_PATH
 
 
