@@ -150,9 +150,9 @@ class _RmsNorm(torch.autograd.Function):
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         z = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
         rstd = torch.empty(x2.shape[0], dtype=_F32, device=x.device)
-        z2 = x2 if z is None else z.view(x2.shape)
-        vp_rms_forward(x2, r2, weight, eps, y.view(x2.shape), None if z is None else z2, rstd)
-        ctx.save_for_backward(z2, weight, rstd)
+        vp_rms_forward(x2, r2, weight, eps, y.view(x2.shape), None if z is None else z.view(x2.shape), rstd)
+        # the sum as it is returned: a saved view of it would hold its own node, which nothing frees without a backward pass
+        ctx.save_for_backward(x2 if z is None else z, weight, rstd)
         ctx.shape = x.shape
         ctx.set_materialize_grads(False)
         return y if z is None else (y, z)
@@ -161,6 +161,7 @@ class _RmsNorm(torch.autograd.Function):
     @first_derivative_only
     def backward(ctx, dy, dz=None):
         z, weight, rstd = ctx.saved_tensors
+        z = z.reshape(-1, z.shape[-1])
         rows, d = z.shape
         need_x, need_w, need_r, _ = ctx.needs_input_grad
         need_w = need_w and weight is not None

@@ -333,3 +333,30 @@ def test_other_stream_and_graph():
         step()
     torch.cuda.current_stream().wait_stream(s)
     assert torch.equal(y, want[0])
+
+
+@pytest.mark.parametrize("with_residual", [False, True])
+@pytest.mark.parametrize("shape", [(64, 1024), (4, 16, 1024)])
+def test_forward_without_backward_frees_its_memory(shape, with_residual):
+    """A graph that is dropped without a backward pass holds nothing afterwards."""
+    x, r = (torch.randn(shape, device="cuda", dtype=torch.bfloat16, requires_grad=True) for _ in range(2))
+    w = torch.ones(shape[-1], device="cuda", requires_grad=True)
+
+    def step():
+        vp.rms_norm(x, w, r if with_residual else None)
+
+    step()
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    for _ in range(4):
+        step()
+    assert torch.cuda.memory_allocated() == before
+
+
+def test_backward_refuses_a_sum_that_was_written_to():
+    x, r = (torch.randn(8, 256, device="cuda", requires_grad=True) for _ in range(2))
+    y, z = vp.rms_norm(x, None, r)
+    with torch.no_grad():
+        z.add_(1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()

@@ -494,3 +494,19 @@ def test_quantize_blocks_refusals():
         vp.vp_fp8_quantize_blocks(w, q, torch.zeros(2, device="cuda"))
     q2, s2 = vp.quantize_blocks_fp8(torch.nn.Parameter(w.t()))
     assert q2.shape == (64, 4) and s2.shape == (1, 1) and (s2 == 1).all()
+
+
+def test_forward_without_backward_frees_its_memory():
+    """A graph that is dropped without a backward pass holds nothing afterwards."""
+    H, W = (torch.randn(n, 256, device="cuda", dtype=torch.bfloat16, requires_grad=True) for n in (96, 1000))
+    tokens = torch.arange(96, device="cuda")
+
+    def step():
+        vp.token_log_probs(H, W, tokens, top_k=4)
+
+    step()
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    for _ in range(4):
+        step()
+    assert torch.cuda.memory_allocated() == before
