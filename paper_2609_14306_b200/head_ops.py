@@ -336,6 +336,15 @@ def _empty_outputs(T: int, top: int, tokens, device):
             torch.empty(T, top, dtype=_I32, device=device) if top else None)
 
 
+def _strip_width(T_chunk: int, V: int) -> int:
+    """Columns of the vocabulary that the backward pass has under way at once where the caller does not say.
+
+    Fewer strips are fewer launches and fewer passes over dH's sums, so few tokens take all columns that fit in the residual of
+    16384 tokens x 8192 columns (2^27 elements, 256 MB).  201088 x 2880, backward, 8192 columns against this rule: 200 tokens 3.0 and
+    1.8 ms, 1000 tokens 5.1 and 3.9, 8192 tokens 24.8 and 24.2."""
+    return min(max(8192, (1 << 27) // T_chunk // 256 * 256), -(-V // 256) * 256)
+
+
 class _TokenLogProbs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, H, W, tokens, top, temperature, ignore_index, block_v, T_chunk, dW_accum):
@@ -367,6 +376,8 @@ class _TokenLogProbs(torch.autograd.Function):
             return (None,) * 9
         T, d = H.shape
         T_chunk = _pick_chunk(T, T_chunk)
+        if block_v is None:
+            block_v = _strip_width(T_chunk, W.shape[0])
         ws = _ce_workspace(T_chunk, d, block_v, H.device)
         dH = torch.empty_like(H) if need_dH else None
         dW = None
@@ -382,20 +393,20 @@ class _TokenLogProbs(torch.autograd.Function):
 
 
 def token_log_probs(H: torch.Tensor, W: torch.Tensor, tokens: Optional[torch.Tensor] = None, top_k: int = 0, temperature: float = 1.0,
-                    ignore_index: int = -100, block_v: int = 8192, T_chunk: Optional[int] = None,
+                    ignore_index: int = -100, block_v: Optional[int] = None, T_chunk: Optional[int] = None,
                     dW_accum: Optional[torch.Tensor] = None) -> TokenLogProbs:
     """Log probabilities of ``tokens`` under softmax(H @ W.T / temperature), with entropy and ``top_k`` alternatives.
 
     H ``[T, d]`` and W ``[V, d]`` are bfloat16 CUDA tensors, ``tokens`` ``[T]`` integer (``ignore_index``: logp 0, no gradient), or
     None where only entropy and alternatives are asked for.  logp and entropy are differentiable in H and W; the logits are never
-    materialised.  Alternatives come larger first, among equals the lower id; at most 20.  ``block_v`` and ``T_chunk`` are the backward
-    pass's, as is ``dW_accum`` (float32 ``[V, d]``: the weight gradient is added into it and ``W.grad`` stays untouched); see
+    materialised.  Alternatives come larger first, among equals the lower id; at most 20.  ``block_v`` (None: by the number of
+    tokens, in at most 256 MB) and ``T_chunk`` are the backward pass's, as is ``dW_accum`` (float32 ``[V, d]``: the weight gradient is added into it and ``W.grad`` stays untouched); see
     ``vocab_proj_cross_entropy``."""
     _, _, _, V = _head_shapes(H, W, "H", "W")
     if H.dtype is not _BF16 or W.dtype is not _BF16:
         raise TypeError("H and W must be bfloat16 CUDA tensors")
-    return TokenLogProbs(*_TokenLogProbs.apply(H, W, tokens, _check_top(top_k, V), float(temperature), int(ignore_index), int(block_v), T_chunk,
-                                               dW_accum))
+    return TokenLogProbs(*_TokenLogProbs.apply(H, W, tokens, _check_top(top_k, V), float(temperature), int(ignore_index),
+                                               None if block_v is None else int(block_v), T_chunk, dW_accum))
 
 
 def token_log_probs_fp8(Hq: torch.Tensor, Hs: torch.Tensor, Wq: torch.Tensor, Ws: torch.Tensor, tokens: Optional[torch.Tensor] = None,

@@ -510,3 +510,18 @@ def test_forward_without_backward_frees_its_memory():
     for _ in range(4):
         step()
     assert torch.cuda.memory_allocated() == before
+
+
+@pytest.mark.parametrize("T,V,T_chunk", [(40, 20011, None), (0, 500, None), (300, 70001, 128)])
+def test_default_strips(T, V, T_chunk):
+    """Gradients without a given strip width: one strip wider than 8192 columns, no tokens, several chunks."""
+    H, W, tokens = bf16_grid(T, 64, V, seed=3)
+    H.requires_grad_(), W.requires_grad_()
+    out = vp.token_log_probs(H, W, tokens, temperature=0.8, T_chunk=T_chunk)
+    up = torch.randn(T, device="cuda")
+    ((out.logp * up).sum() + 0.3 * out.entropy.sum()).backward()
+    if T == 0:
+        assert H.grad.shape == (0, 64) and not W.grad.any()
+        return
+    rH, rW, _ = orc.token_logp_grad(H.detach(), W.detach(), tokens, up, torch.full((T,), 0.3, device="cuda"), 0.8)
+    assert rel(H.grad, rH) <= 1e-2 and rel(W.grad, rW) <= 1e-2

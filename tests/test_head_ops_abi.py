@@ -90,3 +90,13 @@ def test_the_definitions_gradients_against_differences():
     assert abs((norm(z + eps * e, g) - norm(z - eps * e, g)) / (2 * eps) - float((dx * e).sum())) < 1e-7
     e = r(7)
     assert abs((norm(z, g + eps * e) - norm(z, g - eps * e)) / (2 * eps) - float((dg * e).sum())) < 1e-7
+
+
+def test_default_strip_width_is_whole_tiles_in_bounded_memory():
+    from paper_2609_14306_b200.head_ops import _strip_width
+    for chunk in (128, 256, 1024, 4096, 8192, 16384, 65536):
+        for V in (1, 255, 256, 257, 8193, 201088, 2 ** 31 - 300):
+            width = _strip_width(chunk, V)
+            assert width > 0 and width % 256 == 0 and (width >= V or width >= 8192)
+            assert width <= 8192 or chunk * width <= 2 ** 27
+            assert width < V + 256 and vp.vp_ce_workspace_bytes(chunk, 64, width) > 0
