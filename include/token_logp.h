@@ -21,6 +21,9 @@
  *     x_v = sum over blocks b of 128 columns:  Hs[n, b] Ws[v / 128, b] (sum over k in b of Hq[n, k] Wq[v, k])
  * (what vp_rms_forward_fp8 and vp_fp8_quantize_blocks write).  The scales are applied in fp32 to each block's sum.
  *
+ * Where a wait in a forward call runs out (VPCE_DEV_WAIT_EXPIRED, vp_ce_set_wait_limit_ns), every token that it may concern gets NaN as
+ * lse, entropy and logp (0 without a token) and no alternatives (-1, -inf), so that it shows where the status word is not read, too.
+ *
  * Conventions (alignment, streams, status codes) are vp_ce.h's: tensors are contiguous device memory and 16-byte aligned; bf16: d a
  * multiple of 8; 8 bits: d a multiple of 16, at most 16384.  The workspace's first word is the status word of vp_ce_device_status.
  */

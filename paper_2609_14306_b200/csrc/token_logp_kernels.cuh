@@ -1050,6 +1050,13 @@ template <bool TOP> __device__ __forceinline__ void emit(const JoinParams& p, in
         p.top_ids[static_cast<size_t>(row) * p.top + lane] = some ? column_of(list.key) : -1;
     }
 }
+// What a token gets where a wait has run out: NaN, and no alternatives.
+template <bool TOP> __device__ __forceinline__ void emit_nothing(const JoinParams& p, int row, int lane) {
+    List none;
+    none.key = 0ull; none.lane = lane; none.top = p.top;
+    const float nan = __int_as_float(0x7fffffff);
+    emit<TOP>(p, row, nan, nan, nan, none);
+}
 // The lanes' states as one.
 __device__ __forceinline__ State over_lanes(State s, float scale) {
     float m = s.m;
@@ -1085,9 +1092,9 @@ template <bool TOP> __global__ void __launch_bounds__(JOIN_FEW_THREADS) tl_join_
     const int row = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, i = threadIdx.x;
     wait_for_last();
     const float4 q = i < p.slices ? p.part[static_cast<size_t>(row) * p.slices + i] : make_float4(MINUS_INF, 0.f, 0.f, 0.f);
-    const int n = __float_as_int(q.w);
+    const bool expired = __any_sync(0xffffffffu, __float_as_int(q.w) < 0);
+    const int n = min(__float_as_int(q.w), p.top);
     const State s = over_lanes(State{q.x, q.y, q.z}, p.scale);
-    const bool expired = __any_sync(0xffffffffu, n < 0);
     List list;
     list.lane = lane; list.top = TOP ? p.top : 1; list.key = 0ull;
     if (TOP) {
@@ -1106,10 +1113,16 @@ template <bool TOP> __global__ void __launch_bounds__(JOIN_FEW_THREADS) tl_join_
     __syncthreads();
     if (warp) return;
     State all{MINUS_INF, 0.f, 0.f};
+    bool gone = false;
     if (lane < JOIN_FEW_WARPS) {
         const float4 t = states[lane];
         all = State{t.x, t.y, t.z};
-        if (t.w != 0.f) atomicOr(p.status, VPCE_DEV_WAIT_EXPIRED);
+        gone = t.w != 0.f;
+    }
+    if (__any_sync(0xffffffffu, gone)) {
+        if (lane == 0) atomicOr(p.status, VPCE_DEV_WAIT_EXPIRED);
+        emit_nothing<TOP>(p, row, lane);
+        return;
     }
     all = over_lanes(all, p.scale);
     if (TOP) merge_lists<JOIN_FEW_WARPS>(list, keys);
@@ -1128,6 +1141,11 @@ __global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams 
     const int row = WARPS == 1 ? blockIdx.x * JOIN_WARPS + warp : blockIdx.x;
     wait_for_last();
     if (row >= p.rows) return;
+    // A pair that has given up leaves its slices as they were: neither states nor counts of candidates are read then.
+    if (__ldcg(p.status) & VPCE_DEV_WAIT_EXPIRED) {
+        if (p.last && w == 0) emit_nothing<TOP>(p, row, lane);
+        return;
+    }
     State s{MINUS_INF, 0.f, 0.f};
     List list;
     list.lane = lane; list.top = TOP ? p.top : 1; list.key = 0ull;
@@ -1155,7 +1173,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) tl_join_kernel(const JoinParams 
             move(o, m, p.scale);
             s.z += o.z;
             s.u += o.u;
-            n[k] = __float_as_int(q[k].w);
+            n[k] = min(__float_as_int(q[k].w), p.top);
             most = max(most, n[k]);
         }
         if (TOP) {
