@@ -256,7 +256,7 @@ __device__ __forceinline__ unsigned groups_above(Best& best, const float* quads)
     if (__any_sync(0xffffffffu, n > best.top)) {
         float t[32];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) t[j] = quads[j];
+        for (int j = 0; j < 32; ++j) t[j] = fmaxf(quads[j], MINUS_INF);    // four NaN have a NaN as their maximum: it has no place in an order
         const float bound = top_th(t, best.top);
         best.lim = fmaxf(best.lim, below(bound));
     }

@@ -1,9 +1,9 @@
-"""Token log probabilities where a wait runs out, on workspaces that hold anything."""
+"""Token log probabilities where a wait runs out on workspaces that hold anything, and beside NaN."""
 import pytest
 import torch
 
 import paper_2609_14306_b200 as vp
-from test_gpu_token_logp import F8, IGN, bf16_grid, fp8_grid, outputs  # noqa: F401
+from test_gpu_token_logp import F8, IGN, bf16_grid, fp8_grid, outputs, run, run8
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +45,28 @@ def test_a_lost_copy_on_a_workspace_of_arbitrary_bytes(T, d, V, top, fp8):
     call(*args, tokens, 1.0, IGN, *again, ws)
     assert vp.vp_ce_device_status(ws) == 0
     assert all(a is None or torch.equal(a, b) for a, b in zip(want, again))
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T,V,top", [(7, 128, 5), (65, 128, 5), (300, 128, 20), (200, 256, 5), (1000, 1000, 8)])
+def test_alternatives_beside_columns_of_nan(T, V, top, fp8):
+    """A NaN is not an alternative and takes no other column's place: four neighbours of NaN (all that one bound looks at) at every
+    place, and single ones.  Ids are the definition's, the sums being exact."""
+    (hq, hs, wq, ws), (full_h, full_w), tokens = fp8_grid(T, 128, V, seed=T + V)
+    H, W, _ = bf16_grid(T, 128, V, seed=T + V)
+    x = full_h @ full_w.mT if fp8 else H.double() @ W.double().mT
+    for first in (0, 28, 64, 124):
+        gone = torch.zeros(V, dtype=torch.bool, device="cuda")
+        gone[first:first + 4] = True
+        gone[::17] = True
+        if fp8:
+            bad = wq.view(torch.uint8).clone()
+            bad[gone, 3] = 0x7f
+            _, lse, _, top_logp, top_ids = run8((hq, hs, bad.view(F8), ws), tokens, top)
+        else:
+            bad = W.clone()
+            bad[gone, 3] = float("nan")
+            _, lse, _, top_logp, top_ids = run(H, bad, tokens, top)
+        want = torch.sort(x.masked_fill(gone, -float("inf")), dim=1, descending=True, stable=True)[1][:, :top]
+        assert torch.equal(top_ids.long(), want)
+        assert torch.isnan(lse).all() and torch.isnan(top_logp).all()
