@@ -60,6 +60,12 @@ int vp_token_logp_fp8_forward(const void* Hq, const float* Hs, const void* Wq, c
  * dH [T, d] bf16 (overwritten) and dW [V, d] fp32 (overwritten, or added to when accumulate_dW) from the forward call's lse and
  * entropy (needed with dent only).  dlogp or dent [T] may be NULL (zeros), as may dH or dW (not computed), one of each at least given.
  * block_v, T_chunk, chunk_index_base and the workspace (vp_ce_workspace_bytes) are those of vp_ce_backward, which this call extends.
+ *
+ * temperature: 0.01 to 100, narrower than the forward call's.  p is formed anew as exp(x - lse) from lse in one fp32 number, so that it is off
+ * by up to 2^-22 (|lse| + |log p| + 1) relative (7e-4 at temperature 0.01 and logits of 30), and log p + entropy by up to
+ * 2^-21 (|lse| + |log p| + entropy) absolute.
+ * dx is rounded to bf16 before both products (half a step, 2^-8 of each entry; the token's own entry is put back exactly), as in
+ * vp_ce_backward; sums and dW are fp32, dH is rounded once.
  */
 int vp_token_logp_backward(const void* H, const void* W, const int32_t* tokens, const float* lse, const float* entropy,
                            const float* dlogp, const float* dent, void* dH, float* dW, int64_t T, int64_t d, int64_t V, double temperature,

@@ -1154,7 +1154,9 @@ extern "C" int vp_token_logp_backward(const void* H, const void* W, const int32_
                                       const float* dlogp, const float* dent, void* dH, float* dW, int64_t T, int64_t d, int64_t V,
                                       double temperature, int64_t block_v, int32_t ignore_index, int64_t T_chunk,
                                       int64_t chunk_index_base, int accumulate_dW, void* workspace, size_t workspace_bytes, void* stream) {
-    if (!(temperature >= 1e-6) || !(temperature <= 1e6)) return VPCE_INVALID_ARG;
+    // p is formed anew from lse as one number, which leaves nothing of it where lse / temperature is large, nor of an entropy's gradient
+    // where the logits lie close together over the temperature: narrower than the forward call's range
+    if (!(temperature >= 0.01) || !(temperature <= 100.0)) return VPCE_INVALID_ARG;
     if (T > 0 && ((!dlogp && !dent) || (dent && !entropy))) return VPCE_INVALID_ARG;
     const ScoreGrad score{entropy, dent, static_cast<float>(1.0 / temperature)};
     return backward_impl(H, W, tokens, lse, dlogp, dH, dW, T, d, V, block_v, ignore_index, T_chunk, chunk_index_base, accumulate_dW, workspace,

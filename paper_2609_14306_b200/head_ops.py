@@ -236,6 +236,7 @@ def quantize_blocks_fp8(w: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
 
 # --------------------------------------------------------------------------- token log probabilities (token_logp.h)
 MAX_TOP = 20                                               # alternatives per token
+GRAD_TEMPERATURES = (0.01, 100.0)                          # of the backward pass; the forward pass takes 1e-6 to 1e6
 
 _I32 = torch.int32
 
@@ -296,8 +297,8 @@ def vp_token_logp_fp8_forward(Hq, Hs, Wq, Ws, tokens, temperature: float, ignore
 def vp_token_logp_backward(H, W, tokens, lse, entropy, dlogp, dent, temperature: float, ignore_index: int, dH, dW, block_v: int, T_chunk: int,
                            accumulate_dW: bool, workspace, chunk_index_base: int = 0, stream=None) -> None:
     """dH [T, d] (bfloat16) and dW [V, d] (float32, overwritten or added to) from the upstream gradients dlogp and dent [T] (one of
-    them may be None, as may dH or dW) and the forward call's lse and entropy (the latter with dent only).  workspace:
-    vp_ce_workspace_bytes(T_chunk, d, block_v).  See include/token_logp.h."""
+    them may be None, as may dH or dW) and the forward call's lse and entropy (the latter with dent only).  temperature: 0.01 to 100.
+    workspace: vp_ce_workspace_bytes(T_chunk, d, block_v).  See include/token_logp.h."""
     dev, T, d, V = _head_shapes(H, W, "H", "W")
     wsp, wsn = _workspace(workspace, dev)
     _call(_lib().vp_token_logp_backward, dev, _ptr(H, _BF16, "H", T * d, dev), _ptr(W, _BF16, "W", V * d, dev),
@@ -374,6 +375,8 @@ class _TokenLogProbs(torch.autograd.Function):
         need_dH, need_dW = ctx.needs_input_grad[0], accum is not None or ctx.needs_input_grad[1]
         if not (need_dH or need_dW) or (dlogp is None and dent is None):
             return (None,) * 9
+        if not GRAD_TEMPERATURES[0] <= temperature <= GRAD_TEMPERATURES[1]:
+            raise ValueError(f"gradients need a temperature between {GRAD_TEMPERATURES[0]} and {GRAD_TEMPERATURES[1]}, got {temperature}")
         T, d = H.shape
         T_chunk = _pick_chunk(T, T_chunk)
         if block_v is None:
@@ -398,8 +401,8 @@ def token_log_probs(H: torch.Tensor, W: torch.Tensor, tokens: Optional[torch.Ten
     """Log probabilities of ``tokens`` under softmax(H @ W.T / temperature), with entropy and ``top_k`` alternatives.
 
     H ``[T, d]`` and W ``[V, d]`` are bfloat16 CUDA tensors, ``tokens`` ``[T]`` integer (``ignore_index``: logp 0, no gradient), or
-    None where only entropy and alternatives are asked for.  logp and entropy are differentiable in H and W; the logits are never
-    materialised.  Alternatives come larger first, among equals the lower id; at most 20.  ``block_v`` (None: by the number of
+    None where only entropy and alternatives are asked for.  logp and entropy are differentiable in H and W (temperatures from 0.01 to
+    100; without gradients 1e-6 to 1e6); the logits are never materialised.  Alternatives come larger first, among equals the lower id; at most 20.  ``block_v`` (None: by the number of
     tokens, in at most 256 MB) and ``T_chunk`` are the backward pass's, as is ``dW_accum`` (float32 ``[V, d]``: the weight gradient is added into it and ``W.grad`` stays untouched); see
     ``vocab_proj_cross_entropy``."""
     _, _, _, V = _head_shapes(H, W, "H", "W")

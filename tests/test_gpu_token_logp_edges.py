@@ -1,8 +1,10 @@
-"""Token log probabilities where a wait runs out on workspaces that hold anything, and beside NaN."""
+"""Token log probabilities where a wait runs out on workspaces that hold anything, beside NaN, at the ends of the temperatures, with strips
+as wide as the default takes them, and calls that are refused."""
 import pytest
 import torch
 
 import paper_2609_14306_b200 as vp
+from oracle import head_ops_oracle as orc
 from test_gpu_token_logp import F8, IGN, bf16_grid, fp8_grid, outputs, run, run8
 
 pytestmark = pytest.mark.gpu
@@ -70,3 +72,69 @@ def test_alternatives_beside_columns_of_nan(T, V, top, fp8):
         want = torch.sort(x.masked_fill(gone, -float("inf")), dim=1, descending=True, stable=True)[1][:, :top]
         assert torch.equal(top_ids.long(), want)
         assert torch.isnan(lse).all() and torch.isnan(top_logp).all()
+
+
+@pytest.mark.parametrize("T", [70, 130])
+@pytest.mark.parametrize("temperature,unit,size", [(0.01, 2.0 ** -10, 32), (0.01, 2.0 ** -10, 512), (2.0 ** -6, 2.0 ** -10, 32), (2.0 ** -6, 2.0 ** -10, 512),
+                                                   (0.1, 2.0 ** -7, 512), (1.0, 2.0 ** -4, 32), (64.0, 2.0 ** -4, 32), (100.0, 2.0 ** -4, 32)])
+def test_gradients_at_the_ends_of_the_temperatures(T, temperature, unit, size):
+    """Logits of 32 or 512 and a spread that leaves many columns likely at each temperature, on sums that are exact; lse and entropy from the
+    definition, rounded once.
+
+    With s = x / temperature - lse the residual is (dlogp (onehot - p) - dent p (s + entropy)) / temperature, p = exp(s).  lse, its product
+    with log2(e), 1 / temperature and its product with log2(e) are rounded apart, then s: s is off by 2^-24 (2 |lse| + 2 |x / temperature| +
+    2 |s|), p by as much and 2^-22 relative (the hardware's exponential).  s + entropy comes from lse, entropy, their difference and
+    its product with dent, and logits times a twice rounded factor: 2^-24 (3 (|lse| + entropy) + 2 |x / temperature| + its own size);
+    the products 2^-21.  So every entry
+    lies between two numbers, and what bf16 makes of it between what it makes of those (the target's entry is held exactly).  To that
+    the tensor core's cuts (2^-23 a step of 16 columns or tokens) and the result's bf16 (2^-8) are added."""
+    d, V = 64, 2000
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    H = torch.randint(-12, 13, (T, d), generator=gen, device="cuda").float() / 8
+    W = torch.randint(-12, 13, (V, d), generator=gen, device="cuda").float() * unit
+    H[:, 0], W[:, 0] = size, 1
+    H, W = H.to(torch.bfloat16), W.to(torch.bfloat16)
+    tokens = torch.randint(0, V, (T,), generator=gen, device="cuda", dtype=torch.int32)
+    tokens[3] = IGN
+    u, v = torch.randn(T, generator=gen, device="cuda"), torch.randn(T, generator=gen, device="cuda")
+    ref = orc.token_logp(H, W, tokens, temperature, IGN)
+    lse, entropy = ref["lse"].float(), ref["entropy"].float()
+    s = ref["logq"]
+    p = torch.exp(s)
+    c = s + ref["entropy"][:, None]
+    e_s = 2.0 ** -24 * (2 * ref["lse"].abs()[:, None] + 2 * (ref["x"] / temperature).abs() + 2 * s.abs())
+    e_p = e_s + 2.0 ** -22
+    e_c = 2.0 ** -24 * (3 * (ref["lse"].abs() + ref["entropy"])[:, None] + 2 * (ref["x"] / temperature).abs() + c.abs())
+    ws = torch.empty(vp.vp_ce_workspace_bytes(256, d, 512), dtype=torch.uint8, device="cuda")
+    h, w = H.double().abs(), W.double().abs()
+    for a, b in ((u, None), (None, v), (u, v)):
+        dH, dW = torch.empty_like(H), torch.empty(V, d, device="cuda")
+        vp.vp_token_logp_backward(H, W, tokens, lse, entropy if b is not None else None, a, b, temperature, IGN, dH, dW, 512, 256, False, ws)
+        rH, rW, G = orc.token_logp_grad(H, W, tokens, a, b, temperature, IGN)
+        first = torch.zeros(T, dtype=torch.float64, device="cuda") if a is None else torch.where(ref["valid"], a.double().abs(), 0.0)
+        second = torch.zeros_like(first) if b is None else b.double().abs()
+        e_g = p * (e_p * (first[:, None] + second[:, None] * c.abs()) + second[:, None] * e_c) / temperature + 2.0 ** -21 * G.abs()
+        at = torch.zeros_like(G, dtype=torch.bool)
+        at[ref["valid"]] = at[ref["valid"]].scatter(1, tokens.long()[ref["valid"]][:, None], True)
+        low, high = (torch.where(at, g, g.to(torch.bfloat16).double()) for g in (G - e_g, G + e_g))
+        mid, half = (low + high) / 2, (high - low) / 2
+        steps = (512 / 16 + 8) * 2.0 ** -23
+        for got, want, free, total in ((dH, mid @ W.double(), half @ w, G.abs() @ w), (dW, mid.mT @ H.double(), half.mT @ h, G.abs().mT @ h)):
+            allowed = free + steps * total + (2.0 ** -8 * (1 + 2.0 ** -8) * want.abs() if got is dH else 0)
+            err = (got.double() - want).abs()
+            assert (err <= allowed).all(), float((err / allowed).nan_to_num().max())
+
+
+def test_gradients_outside_the_temperatures_are_refused():
+    H, W, tokens = bf16_grid(70, 64, 300, seed=1)
+    ws = torch.empty(vp.vp_ce_workspace_bytes(128, 64, 512), dtype=torch.uint8, device="cuda")
+    lse, entropy, u = (torch.zeros(70, device="cuda") for _ in range(3))
+    for temperature in (1e-6, 0.0099, 100.5, 1e6, float("nan")):
+        with pytest.raises(vp.VpceError):
+            vp.vp_token_logp_backward(H, W, tokens, lse, entropy, u, u, temperature, IGN, torch.empty_like(H), None, 512, 128, False, ws)
+    H.requires_grad_()
+    for temperature in (1e-3, 1e3):
+        out = vp.token_log_probs(H, W, tokens, temperature=temperature)     # the forward call's range is wider
+        assert torch.isfinite(out.logp).all()
+        with pytest.raises(ValueError, match="temperature"):
+            out.logp.sum().backward()
