@@ -338,12 +338,15 @@ def _empty_outputs(T: int, top: int, tokens, device):
 
 
 def _strip_width(T_chunk: int, V: int) -> int:
-    """Columns of the vocabulary that the backward pass has under way at once where the caller does not say.
+    """Columns of the vocabulary that the backward pass has under way at once where the caller does not say: 16384, or 8192 where a chunk
+    has more than 8192 tokens, in whole tiles.
 
-    Fewer strips are fewer launches and fewer passes over dH's sums, so few tokens take all columns that fit in the residual of
-    16384 tokens x 8192 columns (2^27 elements, 256 MB).  201088 x 2880, backward, 8192 columns against this rule: 200 tokens 3.0 and
-    1.8 ms, 1000 tokens 5.1 and 3.9, 8192 tokens 24.8 and 24.2."""
-    return min(max(8192, (1 << 27) // T_chunk // 256 * 256), -(-V // 256) * 256)
+    A strip's part of dH is one sum of the tensor core, which cuts off up to 2^-23 of what it holds for every 16 columns; parts are
+    added in fp32.  Wider strips save launches and passes over dH's sums, but where rows of W have a common mean (1, of a spread of 0.1; 201088
+    x 640, 200 tokens) dH is off by 1.79e-3 (Frobenius) with 8192 columns, 1.84e-3 with 16384, 2.03e-3 with 32768 and 5.5e-3 with all, of which
+    the rounding to bf16 is 1.64e-3.  201088 x 2880, backward: 200 tokens 3.0 ms with 8192 columns, 2.4 with 16384, 1.8 with all; 1000
+    tokens 5.1, 4.1 and 3.9; 8192 tokens 24.8 and 24.2."""
+    return min(16384 if T_chunk <= 8192 else 8192, -(-V // 256) * 256)
 
 
 class _TokenLogProbs(torch.autograd.Function):
@@ -402,9 +405,10 @@ def token_log_probs(H: torch.Tensor, W: torch.Tensor, tokens: Optional[torch.Ten
 
     H ``[T, d]`` and W ``[V, d]`` are bfloat16 CUDA tensors, ``tokens`` ``[T]`` integer (``ignore_index``: logp 0, no gradient), or
     None where only entropy and alternatives are asked for.  logp and entropy are differentiable in H and W (temperatures from 0.01 to
-    100; without gradients 1e-6 to 1e6); the logits are never materialised.  Alternatives come larger first, among equals the lower id; at most 20.  ``block_v`` (None: by the number of
-    tokens, in at most 256 MB) and ``T_chunk`` are the backward pass's, as is ``dW_accum`` (float32 ``[V, d]``: the weight gradient is added into it and ``W.grad`` stays untouched); see
-    ``vocab_proj_cross_entropy``."""
+    100; without gradients 1e-6 to 1e6); the logits are never materialised.  Alternatives come larger first, among equals the lower id;
+    at most 20.  ``block_v`` (None: 16384, or 8192 where a chunk has more than 8192 tokens) and ``T_chunk`` (None: up to 16384) are the
+    backward pass's, which holds T_chunk x block_v elements of bf16 at once, as is ``dW_accum`` (float32 ``[V, d]``: the weight gradient is
+    added into it and ``W.grad`` stays untouched); see ``vocab_proj_cross_entropy``."""
     _, _, _, V = _head_shapes(H, W, "H", "W")
     if H.dtype is not _BF16 or W.dtype is not _BF16:
         raise TypeError("H and W must be bfloat16 CUDA tensors")

@@ -138,3 +138,28 @@ def test_gradients_outside_the_temperatures_are_refused():
         assert torch.isfinite(out.logp).all()
         with pytest.raises(ValueError, match="temperature"):
             out.logp.sum().backward()
+
+
+def test_default_strips_hold_their_sums():
+    """dH where a strip's sum is far larger than what is left of it in the end (rows of W with a common mean): p sums to 1 over columns
+    near 1, and -1 of the target's comes against it.
+
+    A strip of n columns is n / 16 steps of the tensor core, each of which may cut off 2^-23 of the sum, itself at most A = sum |G W|: at the
+    default's most, 16384 columns, 2^-13 A.  Beside that G is rounded to bf16 (half a step, 2^-8 of each entry, evenly spread: six times
+    2^-8 / sqrt(3) sqrt(sum G^2 W^2); the target's entry exactly), the strips are added up in fp32 (13 times 2^-24 A), and the result is
+    rounded to bf16 (2^-8)."""
+    T, d, V = 200, 128, 201088
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    W = (1 + 0.1 * torch.randn(V, d, generator=gen, device="cuda")).to(torch.bfloat16)
+    H = torch.randn(T, d, generator=gen, device="cuda")
+    H = (H - H.mean(1, keepdim=True)).to(torch.bfloat16)
+    tokens = torch.randint(0, V, (T,), generator=gen, device="cuda", dtype=torch.int32)
+    H.requires_grad_()
+    vp.token_log_probs(H, W, tokens).logp.sum().backward()
+    dH, _, G = orc.token_logp_grad(H.detach(), W, tokens, torch.ones(T, device="cuda"), None, 1.0)
+    A = G.abs() @ W.double().abs()
+    G.scatter_(1, tokens.long()[:, None], 0.0)
+    Q = (G.square() @ W.double().square()).sqrt()
+    err = (H.grad.double() - dH).abs()
+    allowed = (2.0 ** -13 + 13 * 2.0 ** -24) * A + 6 * 2.0 ** -8 / 3 ** 0.5 * Q + 2.0 ** -8 * dH.abs() * (1 + 2.0 ** -8)
+    assert (err <= allowed).all(), float((err / allowed).max())
