@@ -53,6 +53,18 @@ def fp8_blocks(n: int) -> int:
     return -(-n // FP8_BLOCK)
 
 
+def _matrix(t, dtype, name: str, rows: int, cols: int, dev: int) -> int:
+    """Pointer of a contiguous [rows, cols] tensor: as many elements in another shape are in another order."""
+    p = _ptr(t, dtype, name, rows * cols, dev)
+    if t.shape != (rows, cols):
+        raise ValueError(f"{name} must be [{rows}, {cols}], got {list(t.shape)}")
+    return p
+
+
+def _opt_matrix(t, dtype, name: str, rows: int, cols: int, dev: int) -> Optional[int]:
+    return None if t is None else _matrix(t, dtype, name, rows, cols, dev)
+
+
 # --------------------------------------------------------------------------- RMS norm (rms_norm.h)
 def _rms_types(dt, weight):
     """The weight's element type, checked against the rows' type dt."""
@@ -97,7 +109,7 @@ def vp_rms_forward_fp8(x, residual, weight, eps: float, q, scales, z, rstd, stre
     include/rms_norm.h."""
     dev, rows, d, head, tail = _rms_inputs(x, residual, weight, z, rstd)
     qp, qs = _rows(q, _F8, "q", rows, d, dev)
-    _call(_lib().vp_rms_forward_fp8, dev, *head, eps, qp, qs, _ptr(scales, _F32, "scales", rows * fp8_blocks(d), dev), *tail,
+    _call(_lib().vp_rms_forward_fp8, dev, *head, eps, qp, qs, _matrix(scales, _F32, "scales", rows, fp8_blocks(d), dev), *tail,
           _stream(stream, dev))
 
 
@@ -200,7 +212,7 @@ def rms_norm_fp8(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residua
     scales = torch.empty(*x.shape[:-1], fp8_blocks(d), dtype=_F32, device=x.device)
     z = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
     vp_rms_forward_fp8(x2, None if residual is None else _as_rows(residual, d), None if weight is None else weight.contiguous(), float(eps),
-                       q.view(x2.shape), scales, None if z is None else z.view(x2.shape), None)
+                       q.view(x2.shape), scales.view(x2.shape[0], fp8_blocks(d)), None if z is None else z.view(x2.shape), None)
     return (q, scales) if z is None else (q, scales, z)
 
 
@@ -215,7 +227,7 @@ def vp_fp8_quantize_blocks(w, q, scales, stream=None) -> None:
     wp, ws = _rows(w, w.dtype, "w", rows, d, dev)
     qp, qs = _rows(q, _F8, "q", rows, d, dev)
     _call(_lib().vp_fp8_quantize_blocks, dev, wp, _DTYPE_CODE[w.dtype], rows, d, ws, qp, qs,
-          _ptr(scales, _F32, "scales", fp8_blocks(rows) * fp8_blocks(d), dev), _stream(stream, dev))
+          _matrix(scales, _F32, "scales", fp8_blocks(rows), fp8_blocks(d), dev), _stream(stream, dev))
 
 
 def quantize_blocks_fp8(w: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
@@ -268,7 +280,7 @@ def _logp_outputs(dev, T, tokens, logp, lse, entropy, top_logp, top_ids):
             raise ValueError(f"top_logp must be [{T}, alternatives], got {list(top_logp.shape)}")
         top = top_logp.shape[1]
     return top, (_opt(logp, _F32, "logp", T, dev), _opt(lse, _F32, "lse", T, dev), _opt(entropy, _F32, "entropy", T, dev),
-                 _opt(top_logp, _F32, "top_logp", T * top, dev), _opt(top_ids, _I32, "top_ids", T * top, dev), top)
+                 _opt_matrix(top_logp, _F32, "top_logp", T, top, dev), _opt_matrix(top_ids, _I32, "top_ids", T, top, dev), top)
 
 
 def vp_token_logp_forward(H, W, tokens, temperature: float, ignore_index: int, logp, lse, entropy, top_logp, top_ids, workspace,
@@ -289,8 +301,8 @@ def vp_token_logp_fp8_forward(Hq, Hs, Wq, Ws, tokens, temperature: float, ignore
     dev, T, d, V = _head_shapes(Hq, Wq, "Hq", "Wq")
     top, outs = _logp_outputs(dev, T, tokens, logp, lse, entropy, top_logp, top_ids)
     wsp, wsn = _workspace(workspace, dev)
-    _call(_lib().vp_token_logp_fp8_forward, dev, _ptr(Hq, _F8, "Hq", T * d, dev), _ptr(Hs, _F32, "Hs", T * fp8_blocks(d), dev),
-          _ptr(Wq, _F8, "Wq", V * d, dev), _ptr(Ws, _F32, "Ws", fp8_blocks(V) * fp8_blocks(d), dev), _opt(tokens, _I32, "tokens", T, dev), T, d,
+    _call(_lib().vp_token_logp_fp8_forward, dev, _ptr(Hq, _F8, "Hq", T * d, dev), _matrix(Hs, _F32, "Hs", T, fp8_blocks(d), dev),
+          _ptr(Wq, _F8, "Wq", V * d, dev), _matrix(Ws, _F32, "Ws", fp8_blocks(V), fp8_blocks(d), dev), _opt(tokens, _I32, "tokens", T, dev), T, d,
           V, temperature, ignore_index, *outs, wsp, wsn, _stream(stream, dev))
 
 
@@ -303,8 +315,8 @@ def vp_token_logp_backward(H, W, tokens, lse, entropy, dlogp, dent, temperature:
     wsp, wsn = _workspace(workspace, dev)
     _call(_lib().vp_token_logp_backward, dev, _ptr(H, _BF16, "H", T * d, dev), _ptr(W, _BF16, "W", V * d, dev),
           _ptr(tokens, _I32, "tokens", T, dev), _ptr(lse, _F32, "lse", T, dev), _opt(entropy, _F32, "entropy", T, dev),
-          _opt(dlogp, _F32, "dlogp", T, dev), _opt(dent, _F32, "dent", T, dev), _opt(dH, _BF16, "dH", T * d, dev),
-          _opt(dW, _F32, "dW", V * d, dev), T, d, V, temperature, block_v, ignore_index, T_chunk, chunk_index_base, 1 if accumulate_dW else 0,
+          _opt(dlogp, _F32, "dlogp", T, dev), _opt(dent, _F32, "dent", T, dev), _opt_matrix(dH, _BF16, "dH", T, d, dev),
+          _opt_matrix(dW, _F32, "dW", V, d, dev), T, d, V, temperature, block_v, ignore_index, T_chunk, chunk_index_base, 1 if accumulate_dW else 0,
           wsp, wsn, _stream(stream, dev))
 
 

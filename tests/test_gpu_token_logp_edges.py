@@ -163,3 +163,30 @@ def test_default_strips_hold_their_sums():
     err = (H.grad.double() - dH).abs()
     allowed = (2.0 ** -13 + 13 * 2.0 ** -24) * A + 6 * 2.0 ** -8 / 3 ** 0.5 * Q + 2.0 ** -8 * dH.abs() * (1 + 2.0 ** -8)
     assert (err <= allowed).all(), float((err / allowed).max())
+
+
+def test_scales_and_gradients_of_another_shape_are_refused():
+    """As many elements in another order are another matrix."""
+    T, d, V = 256, 384, 640                                                 # Hs [256, 3], Ws [5, 3]
+    (hq, hs, wq, ws), _, tokens = fp8_grid(T, d, V, seed=1)
+    vp.token_log_probs_fp8(hq, hs, wq, ws, tokens)
+    for bad in ((hq, hs.t(), wq, ws), (hq, hs, wq, ws.t()), (hq, hs.reshape(-1), wq, ws), (hq, hs, wq, ws.reshape(3, 5))):
+        with pytest.raises(ValueError, match="must be"):
+            vp.token_log_probs_fp8(*bad, tokens)
+    with pytest.raises(ValueError, match="must be"):
+        vp.vp_fp8_quantize_blocks(torch.zeros(V, d, device="cuda"), torch.empty_like(wq), ws.t().contiguous())
+    with pytest.raises(ValueError, match="must be"):
+        vp.vp_rms_forward_fp8(torch.zeros(T, d, device="cuda"), None, None, 1e-6, torch.empty_like(hq), hs.t().contiguous(), None, None)
+    H, W, _ = bf16_grid(T, d, V, seed=1)
+    outs = outputs(T, 2)
+    room = torch.empty(vp.vp_token_logp_workspace_bytes(T, d, V, 2), dtype=torch.uint8, device="cuda")
+    with pytest.raises(ValueError, match="must be"):
+        vp.vp_token_logp_forward(H, W, tokens, 1.0, IGN, *outs[:4], outs[4].reshape(2, T), room)
+    room = torch.empty(vp.vp_ce_workspace_bytes(256, d, 256), dtype=torch.uint8, device="cuda")
+    vp.vp_token_logp_forward(H, W, tokens, 1.0, IGN, *outs[:3], None, None, torch.empty(1 << 24, dtype=torch.uint8, device="cuda"))
+    for dH, dW in ((torch.empty(d, T, device="cuda", dtype=torch.bfloat16), None), (None, torch.zeros(d, V, device="cuda"))):
+        with pytest.raises(ValueError, match="must be"):
+            vp.vp_token_logp_backward(H, W, tokens, outs[1], None, outs[0], None, 1.0, IGN, dH, dW, 256, 256, False, room)
+    H.requires_grad_()
+    with pytest.raises(ValueError, match="must be"):
+        vp.token_log_probs(H, W, tokens, block_v=256, dW_accum=torch.zeros(d, V, device="cuda")).logp.sum().backward()
