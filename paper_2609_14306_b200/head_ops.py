@@ -433,8 +433,10 @@ def token_log_probs_fp8(Hq: torch.Tensor, Hs: torch.Tensor, Wq: torch.Tensor, Ws
     """``token_log_probs`` from 8-bit operands, without a gradient: for scoring and generation.
 
     Hq ``[T, d]`` with Hs ``[T, ceil(d / 128)]`` is what ``rms_norm_fp8`` returns, Wq ``[V, d]`` with Ws what ``quantize_blocks_fp8``
-    returns."""
+    returns.  There is no gradient: under ``torch.no_grad()``, or with scales that require none."""
     _, T, d, V = _head_shapes(Hq, Wq, "Hq", "Wq")
+    if torch.is_grad_enabled() and (Hs.requires_grad or Ws.requires_grad):
+        raise RuntimeError("token_log_probs_fp8 has no gradient: call it under torch.no_grad()")
     top = _check_top(top_k, V)
     tokens = None if tokens is None else tokens.to(_I32).contiguous()
     logp, lse, entropy, top_logp, top_ids = _empty_outputs(T, top, tokens, Hq.device)

@@ -190,3 +190,13 @@ def test_scales_and_gradients_of_another_shape_are_refused():
     H.requires_grad_()
     with pytest.raises(ValueError, match="must be"):
         vp.token_log_probs(H, W, tokens, block_v=256, dW_accum=torch.zeros(d, V, device="cuda")).logp.sum().backward()
+
+
+def test_scales_that_require_a_gradient_are_refused():
+    (hq, hs, wq, ws), _, tokens = fp8_grid(4, 128, 300, seed=1)
+    for i in (0, 1):
+        a, b = (hs.clone().requires_grad_(i == 0), ws.clone().requires_grad_(i == 1))
+        with pytest.raises(RuntimeError, match="no gradient"):
+            vp.token_log_probs_fp8(hq, a, wq, b, tokens)
+        with torch.no_grad():
+            assert torch.isfinite(vp.token_log_probs_fp8(hq, a, wq, b, tokens).logp).all()
