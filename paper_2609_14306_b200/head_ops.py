@@ -251,6 +251,7 @@ MAX_TOP = 20                                               # alternatives per to
 GRAD_TEMPERATURES = (0.01, 100.0)                          # of the backward pass; the forward pass takes 1e-6 to 1e6
 
 _I32 = torch.int32
+_TOKEN_TYPES = frozenset((torch.uint8, torch.int8, torch.int16, torch.int32, torch.int64))
 
 
 def vp_token_logp_workspace_bytes(T: int, d: int, V: int, top: int) -> int:
@@ -343,6 +344,24 @@ def _check_top(top_k: int, V: int) -> int:
     return top_k
 
 
+def _as_tokens(tokens) -> Optional[torch.Tensor]:
+    """tokens as contiguous int32; a number that 32 bits do not hold stays outside every vocabulary."""
+    if tokens is None:
+        return None
+    if not isinstance(tokens, torch.Tensor) or tokens.dtype not in _TOKEN_TYPES:
+        raise TypeError(f"tokens must be a tensor of integers, got {getattr(tokens, 'dtype', type(tokens))}")
+    if tokens.dtype is torch.int64:
+        tokens = tokens.clamp(-1 << 31, (1 << 31) - 1)
+    return tokens.to(_I32).contiguous()
+
+
+def _check_ignore_index(ignore_index) -> int:
+    ignore_index = int(ignore_index)
+    if not -1 << 31 <= ignore_index < 1 << 31:
+        raise ValueError(f"ignore_index must fit 32 bits, got {ignore_index}")
+    return ignore_index
+
+
 def _empty_outputs(T: int, top: int, tokens, device):
     f32 = lambda *shape: torch.empty(*shape, dtype=_F32, device=device)  # noqa: E731
     return (None if tokens is None else f32(T), f32(T), f32(T), f32(T, top) if top else None,
@@ -365,7 +384,7 @@ class _TokenLogProbs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, H, W, tokens, top, temperature, ignore_index, block_v, T_chunk, dW_accum):
         H, W = H.contiguous(), W.contiguous()
-        tokens = None if tokens is None else tokens.to(_I32).contiguous()
+        tokens = _as_tokens(tokens)
         T, d = H.shape
         logp, lse, entropy, top_logp, top_ids = _empty_outputs(T, top, tokens, H.device)
         n = vp_token_logp_workspace_bytes(T, d, W.shape[0], top)
@@ -415,16 +434,18 @@ def token_log_probs(H: torch.Tensor, W: torch.Tensor, tokens: Optional[torch.Ten
                     dW_accum: Optional[torch.Tensor] = None) -> TokenLogProbs:
     """Log probabilities of ``tokens`` under softmax(H @ W.T / temperature), with entropy and ``top_k`` alternatives.
 
-    H ``[T, d]`` and W ``[V, d]`` are bfloat16 CUDA tensors, ``tokens`` ``[T]`` integer (``ignore_index``: logp 0, no gradient), or
-    None where only entropy and alternatives are asked for.  logp and entropy are differentiable in H and W (temperatures from 0.01 to
-    100; without gradients 1e-6 to 1e6); the logits are never materialised.  Alternatives come larger first, among equals the lower id;
-    at most 20.  ``block_v`` (None: 16384, or 8192 where a chunk has more than 8192 tokens) and ``T_chunk`` (None: up to 16384) are the
-    backward pass's, which holds T_chunk x block_v elements of bf16 at once, as is ``dW_accum`` (float32 ``[V, d]``: the weight gradient is
-    added into it and ``W.grad`` stays untouched); see ``vocab_proj_cross_entropy``."""
+    H ``[T, d]`` and W ``[V, d]`` are bfloat16 CUDA tensors, ``tokens`` ``[T]`` integers of 8 to 64 bits (``ignore_index``, or any number
+    outside the vocabulary: logp 0, no gradient of it), or None where only entropy and alternatives are asked for.  logp and entropy are
+    differentiable in H and W (temperatures from 0.01 to 100; without gradients 1e-6 to 1e6); the logits are never materialised.
+    Alternatives come larger first, among equals the lower id; at most 20.  ``block_v`` (None: 16384, or 8192 where a chunk has more than
+    8192 tokens) and ``T_chunk`` (None: up to 16384) are the backward pass's, which holds T_chunk x block_v elements of bf16 at once, as is
+    ``dW_accum`` (float32 ``[V, d]``: the weight gradient is added into it and ``W.grad`` stays untouched); see
+    ``vocab_proj_cross_entropy``.  The device status word is left unread, as there: who has to know of tokens outside the vocabulary
+    calls ``vp_token_logp_forward`` with a workspace and ``vp_ce_device_status``; after a wait that ran out the results are NaN."""
     _, _, _, V = _head_shapes(H, W, "H", "W")
     if H.dtype is not _BF16 or W.dtype is not _BF16:
         raise TypeError("H and W must be bfloat16 CUDA tensors")
-    return TokenLogProbs(*_TokenLogProbs.apply(H, W, tokens, _check_top(top_k, V), float(temperature), int(ignore_index),
+    return TokenLogProbs(*_TokenLogProbs.apply(H, W, tokens, _check_top(top_k, V), float(temperature), _check_ignore_index(ignore_index),
                                                None if block_v is None else int(block_v), T_chunk, dW_accum))
 
 
@@ -438,11 +459,11 @@ def token_log_probs_fp8(Hq: torch.Tensor, Hs: torch.Tensor, Wq: torch.Tensor, Ws
     if torch.is_grad_enabled() and (Hs.requires_grad or Ws.requires_grad):
         raise RuntimeError("token_log_probs_fp8 has no gradient: call it under torch.no_grad()")
     top = _check_top(top_k, V)
-    tokens = None if tokens is None else tokens.to(_I32).contiguous()
+    tokens, ignore_index = _as_tokens(tokens), _check_ignore_index(ignore_index)
     logp, lse, entropy, top_logp, top_ids = _empty_outputs(T, top, tokens, Hq.device)
     n = vp_token_logp_fp8_workspace_bytes(T, d, V, top)
     if n == 0:
         raise ValueError(f"unsupported shape: d must be a multiple of 16, at most 16384, got {d}")
-    vp_token_logp_fp8_forward(Hq.contiguous(), Hs.contiguous(), Wq.contiguous(), Ws.contiguous(), tokens, float(temperature), int(ignore_index), logp,
+    vp_token_logp_fp8_forward(Hq.contiguous(), Hs.contiguous(), Wq.contiguous(), Ws.contiguous(), tokens, float(temperature), ignore_index, logp,
                               lse, entropy, top_logp, top_ids, torch.empty(n, dtype=torch.uint8, device=Hq.device))
     return TokenLogProbs(logp, entropy, top_logp, top_ids)

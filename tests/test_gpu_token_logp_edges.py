@@ -200,3 +200,34 @@ def test_scales_that_require_a_gradient_are_refused():
             vp.token_log_probs_fp8(hq, a, wq, b, tokens)
         with torch.no_grad():
             assert torch.isfinite(vp.token_log_probs_fp8(hq, a, wq, b, tokens).logp).all()
+
+
+@pytest.mark.parametrize("T", [8, 100])
+def test_tokens_that_32_bits_do_not_hold(T):
+    """A 64-bit token outside 32 bits is a token outside the vocabulary, not the one that its low half names."""
+    H, W, _ = bf16_grid(T, 64, 300, seed=T)
+    tokens = torch.arange(T, device="cuda") % 300
+    far = tokens.clone()
+    far[0], far[1], far[2], far[3], far[4] = 2 ** 32 + 5, -2 ** 32 + 5, 2 ** 31, -2 ** 31 - 1, 2 ** 63 - 1
+    a, b = vp.token_log_probs(H, W, tokens), vp.token_log_probs(H, W, far)
+    assert (b.logp[:5] == 0).all() and torch.equal(a.logp[5:], b.logp[5:]) and torch.equal(a.entropy, b.entropy)
+    H.requires_grad_()
+    vp.token_log_probs(H, W, far).logp.sum().backward()
+    assert (H.grad[:5] == 0).all() and (H.grad[5:] != 0).any(1).all()
+    ops, _, _ = fp8_grid(T, 64, 300, seed=T)
+    assert (vp.token_log_probs_fp8(*ops, far).logp[:5] == 0).all()
+    for dtype in (torch.uint8, torch.int8, torch.int16):
+        few = (torch.arange(T, device="cuda") % 100).to(dtype)
+        assert torch.equal(vp.token_log_probs(H, W, few).logp, vp.token_log_probs(H, W, few.int()).logp)
+
+
+def test_tokens_and_ignore_index_that_are_none_are_refused():
+    H, W, tokens = bf16_grid(4, 64, 300, seed=1)
+    ops, _, _ = fp8_grid(4, 64, 300, seed=1)
+    for call in (lambda t, **k: vp.token_log_probs(H, W, t, **k), lambda t, **k: vp.token_log_probs_fp8(*ops, t, **k)):
+        for bad in (tokens.float(), tokens.bool(), [1, 2, 3, 4]):
+            with pytest.raises(TypeError):
+                call(bad)
+        for bad in (2 ** 31, -2 ** 31 - 1, 2 ** 32 - 100):
+            with pytest.raises(ValueError, match="ignore_index"):
+                call(tokens, ignore_index=bad)
