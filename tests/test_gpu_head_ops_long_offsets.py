@@ -89,3 +89,30 @@ def test_token_logp(T):
     sizes = (hq.double() * orc.spread_columns(hs, d)).abs() @ last[-2:].abs().mT
     e_x = (d / 32 + 16 + 3 * d / 128) * 2.0 ** -23 * sizes.amax(1)
     assert ((((a - b).double() - want).abs()) <= 2 * e_x + 2.0 ** -21 * (a.abs() + b.abs())).all()
+
+
+@pytest.mark.parametrize("rows,d", [(270000, 8192), (2100000, 1024), (1940000, 1111), (34000000, 64), (130000, 17000)])
+def test_rms_norm_gradients_from_the_last_rows_alone(rows, d):
+    """An upstream gradient that is zero up to the last 700 rows, and the sum's: dx is dz before them, and dweight what those rows give, against
+    float64.  Every term but 700 is an exact zero, so the sums are off by (700 + 64) 2^-24 sum|dy zh|; zh by e_rs = (k / 2 + 6) 2^-24 with
+    k = d / 256 + 40."""
+    assert rows * d > 1 << 31
+    tail = slice(rows - 700, rows)
+    z, dz, w = fill(rows, d), fill(rows, d, seed=1), 1 + 0.2 * fill(d, seed=2).float()
+    dy = torch.zeros_like(z)
+    dy[tail] = fill(700, d, seed=3)
+    y, rstd = torch.empty_like(z), torch.empty(rows, device="cuda")
+    vp.vp_rms_forward(z, None, w, 1e-6, y, None, rstd)
+    dx, dw = y.fill_(float("nan")), torch.full((d,), float("nan"), device="cuda")
+    ws = torch.full((vp.vp_rms_workspace_bytes(rows, d),), 255, dtype=torch.uint8, device="cuda")
+    vp.vp_rms_backward(dy, dz, z, w, rstd, dx, dw, ws)
+    assert torch.equal(dx[:rows - 700], dz[:rows - 700])
+    alone, dw1 = torch.empty(700, d, device="cuda", dtype=torch.bfloat16), torch.empty_like(dw)
+    vp.vp_rms_backward(dy[tail].clone(), dz[tail].clone(), z[tail].clone(), w, rstd[tail].clone(), alone, dw1, ws)
+    assert torch.equal(dx[tail], alone)
+    zh = z[tail].double()
+    zh = zh / torch.sqrt((zh * zh).mean(1, keepdim=True) + 1e-6)
+    terms = dy[tail].double() * zh
+    e = 2.0 ** -24 * ((700 + 64) + (d / 256 + 40) / 2 + 6)
+    for got in (dw, dw1):
+        assert ((got.double() - terms.sum(0)).abs() <= e * terms.abs().sum(0)).all()
