@@ -5,7 +5,7 @@ import torch
 
 import paper_2609_14306_b200 as vp
 from oracle import head_ops_oracle as orc
-from test_gpu_token_logp import F8, IGN, bf16_grid, fp8_grid, outputs, run, run8
+from test_gpu_token_logp import F8, IGN, bf16_grid, check, fp8_grid, outputs, run, run8
 
 pytestmark = pytest.mark.gpu
 
@@ -231,3 +231,19 @@ def test_tokens_and_ignore_index_that_are_none_are_refused():
         for bad in (2 ** 31, -2 ** 31 - 1, 2 ** 32 - 100):
             with pytest.raises(ValueError, match="ignore_index"):
                 call(tokens, ignore_index=bad)
+
+
+@pytest.mark.parametrize("temperature", [1e-6, 1e-3, 1e6])
+@pytest.mark.parametrize("T", [5, 100])
+def test_temperatures_of_the_forward_pass(T, temperature):
+    H, W, tokens = bf16_grid(T, 64, 5000, seed=T)
+    check(run(H, W, tokens, 8, temperature), H, W, tokens, 8, temperature, torch.zeros(T, dtype=torch.float64, device="cuda"))
+    ops, full, tokens = fp8_grid(T, 64, 5000, seed=T)
+    check(run8(ops, tokens, 8, temperature), *full, tokens, 8, temperature, torch.zeros(T, dtype=torch.float64, device="cuda"))
+
+
+@pytest.mark.parametrize("T", [1, 16, 17, 64, 65])
+@pytest.mark.parametrize("d", [16, 16384])
+def test_narrowest_and_widest_rows_in_8_bits(T, d):
+    ops, full, tokens = fp8_grid(T, d, 700, seed=T)
+    check(run8(ops, tokens, 5), *full, tokens, 5, 1.0, torch.zeros(T, dtype=torch.float64, device="cuda"))
