@@ -4,7 +4,8 @@
  *
  * For every block of 128 rows by 128 columns (the last ones may be smaller):
  *     s = max|w| / 448  (at least 2^-126; 1 where the block is all zeros),     q = e4m3(w / s)
- * so that w = q s; q is rounded to nearest even from w times the fp32 reciprocal of s.  A NaN takes no part in the maximum and stays
+ * so that w = q s; s is max|w| times the fp32 number next to 1 / 448, q is rounded to nearest even from w times the fp32 reciprocal
+ * of s: each within an fp32 unit of the quotient.  A NaN takes no part in the maximum and stays
  * a NaN; where a block holds an infinity its scale is infinite, the infinities become NaN and the rest 0.
  *
  * w: VPCE_BF16, VPCE_F16 or VPCE_F32 (vp_ce_types.h), any alignment of its type; row strides in elements (bytes for q), at least d.

@@ -7,13 +7,15 @@
  * The norm is of z as it is stored, so the backward pass, which reads z, differentiates what was computed.  With the upstream
  * gradients dy of y and dz of z (the residual stream's), a = dy g and zh = z rstd:
  *     dx = dr = rstd (a - zh mean(a zh)) + dz,     dg = sum over rows of dy zh
- * All statistics, sums and products are fp32; each result is rounded once to its own type.  The sums over rows have a fixed order:
- * the same call gives the same bits every time.  A NaN or infinity in a row stays in that row's outputs (and in dg, which sums
- * over all rows).
+ * All statistics, sums and products are fp32; each result is rounded once to its own type.  So z^2 has to stay in fp32's range:
+ * elements beyond about 1e19 make rstd 0, and with eps = 0 a row of zeros or of elements below about 1e-23 makes it infinite.  The sums
+ * over rows have a fixed order: the same call gives the same bits every time.  A NaN or infinity in a row stays in that row's outputs
+ * (and in dg, which sums over all rows).
  *
  * 8-bit output: y in groups of 128 neighbouring columns (the last one may be shorter), each with its own scale
  *     s = max|y| / 448  (at least 2^-126; 1 where the group is all zeros),     q = e4m3(y / s)
- * so that y = q s; q is rounded to nearest even from the fp32 y times the fp32 reciprocal of s.  A NaN takes no part in the maximum
+ * so that y = q s; s is max|y| times the fp32 number next to 1 / 448, q is rounded to nearest even from the fp32 y times the fp32
+ * reciprocal of s: each within an fp32 unit of the quotient.  A NaN takes no part in the maximum
  * and stays a NaN; where a group holds an infinity its scale is infinite, the infinities become NaN and the rest 0.
  *
  * Element types (x_dtype, w_dtype): VPCE_BF16, VPCE_F16, VPCE_F32 of vp_ce_types.h.  x, residual, y, z, dy, dz, dx share x_dtype;

@@ -12,10 +12,11 @@
  *
  * Tokens: int32; ignore_index, or any number outside [0, V), gives logp 0 and no gradient of logp (the latter also sets
  * VPCE_DEV_LABEL_OUT_OF_RANGE in the status word); lse, entropy (with its gradient) and alternatives do not depend on the token.
- * Products are exact products of the inputs accumulated in fp32; statistics are fp32 and joined in a fixed order: the same call gives
- * the same bits every time.  A NaN among a token's logits makes its lse, logp and entropy NaN and is not an alternative; alternatives
- * that do not exist for that reason have id -1 and value -inf.  Where a logit is infinite (an
- * overflow, or an infinity among the inputs), that token's lse, logp and entropy are undefined; other tokens' are not touched.
+ * Products are exact products of the inputs accumulated in fp32; statistics are fp32 (exponentials the hardware's approximate ones, 2^-22
+ * relative) and joined in a fixed order: the same call gives the same bits every time.  A NaN among a token's logits makes its lse, logp
+ * and entropy NaN and is not an alternative; alternatives that do not exist for that reason have id -1 and value -inf.  Where a logit is infinite (an overflow, or an infinity among the inputs) or
+ * lies 2e38 x temperature or more below the token's largest one, that token's lse, logp and entropy are undefined; other tokens'
+ * are not touched.
  *
  * 8-bit operands: e4m3 numbers with fp32 scales, one for each 128 columns of a row of H and for each 128 x 128 block of W
  *     x_v = sum over blocks b of 128 columns:  Hs[n, b] Ws[v / 128, b] (sum over k in b of Hq[n, k] Wq[v, k])
@@ -65,7 +66,8 @@ int vp_token_logp_fp8_forward(const void* Hq, const float* Hs, const void* Wq, c
  * by up to 2^-22 (|lse| + |log p| + 1) relative (7e-4 at temperature 0.01 and logits of 30), and log p + entropy by up to
  * 2^-21 (|lse| + |log p| + entropy) absolute.
  * dx is rounded to bf16 before both products (half a step, 2^-8 of each entry; the token's own entry is put back exactly), as in
- * vp_ce_backward; sums and dW are fp32, dH is rounded once.
+ * vp_ce_backward: errors that average out where p varies, and add up where all of p lies within a step (nearly uniform p) and rows
+ * of W have a common mean.  Sums and dW are fp32, dH is rounded once.
  */
 int vp_token_logp_backward(const void* H, const void* W, const int32_t* tokens, const float* lse, const float* entropy,
                            const float* dlogp, const float* dent, void* dH, float* dW, int64_t T, int64_t d, int64_t V, double temperature,

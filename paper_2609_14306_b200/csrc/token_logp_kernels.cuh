@@ -730,7 +730,7 @@ template <int N> __device__ __forceinline__ void offer_tile(List* list, unsigned
 // multiple of 32 rows) through a ring of 6 to 8 stages.  The logits of a tile go through shared memory, so that a warp has a token's
 // 128 logits side by side: it keeps the token's state (a lane its own part) and list in registers from tile to tile.
 // One token of 2880 x 201088 with 8 alternatives: 184 us with the join, 6.3 TB/s (0.96 of a plain copy's rate); 16 tokens of 7168 x 129280
-// in 8 bits 157 us, 5.9 TB/s; 61 tokens of 2048 x 32771 with 20 alternatives 48 us, 34 without (two tiles a CTA: start, end and the lists).
+// in 8 bits 156 to 168 us, 5.5 to 5.9 TB/s; 61 tokens of 2048 x 32771 with 20 alternatives 48 us, 34 without (two tiles a CTA: start, end and the lists).
 constexpr int FEW_TOKENS = 64, FEW_ROWS = 32;                       // W's rows per copy
 template <int NT, bool F8> struct Few {
     static constexpr int STAGES = NT == 64 ? 6 : 8;

@@ -2,7 +2,7 @@
 //
 // The residual strip G = dloss (softmax - onehot) is staged as bf16.  For all entries but one per token that rounding
 // is random and averages out in the contractions; the target entry dloss (p_t - 1) is ~-dloss for every token, so its
-// rounding error (up to 2^-9 relative, about sqrt(V) / 512 of the whole softmax part) has the same sign whenever dloss
+// rounding error (up to 2^-8 relative, about sqrt(V) / 256 of the whole softmax part) has the same sign whenever dloss
 // is the same number.  The residual epilogue therefore records, per token, delta_n = exact - rounded of that one
 // entry (fp32), and the two kernels here add what the GEMMs missed:
 //     dX[n, :]   += delta_n W[t_n, :]          (row-wise, one CTA per token)
